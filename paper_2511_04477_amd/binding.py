@@ -103,7 +103,12 @@ def lib() -> ctypes.CDLL:
         L.spqt_cb2_gemv_rows.argtypes = [vp, i64, i64, vp, i32, vp, vp, vp, vp, sz, vp, c.POINTER(LaunchCfg)]
         L.spqt_cb8_gemv_fused.argtypes = [vp, i64, i64, vp, c.c_float, vp, vp, sz, vp, c.POINTER(LaunchCfg)]
         L.spqt_cb2_gemv_fused.argtypes = [vp, i64, i64, vp, c.c_float, vp, vp, sz, vp, c.POINTER(LaunchCfg)]
-        for name in EXPORTS[1:] + CB_EXPORTS:
+        L.spqt_kv_append.argtypes = [vp, vp, vp, i32, vp, vp]
+        L.spqt_kv_read.argtypes = [vp, vp, vp, i32, vp, vp]
+        L.spqt_kv_workspace_bytes.argtypes = [i32, i32, i32, i32, i32, i32, c.POINTER(sz)]
+        L.spqt_kv_attention.argtypes = [vp, vp, vp, vp, i32, vp, i32, c.c_float, i32, c.c_float, vp, sz, vp]
+        L.spqt_kv_evict.argtypes = [vp, i32, i32, vp, i32, vp, vp, vp]
+        for name in EXPORTS[1:] + CB_EXPORTS + ["spqt_kv_append", "spqt_kv_read", "spqt_kv_workspace_bytes", "spqt_kv_attention", "spqt_kv_evict"]:
             getattr(L, name).restype = i32
         # the device functions' addresses, for _fastcall
         L.at = {name: c.cast(getattr(L, name), vp).value for name in EXPORTS + CB_EXPORTS if "gemv" in name or "gather" in name}

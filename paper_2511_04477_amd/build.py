@@ -19,6 +19,8 @@ OBJ = os.path.join(PKG, "_build")
 LIB = os.path.join(PKG, "libspqt.so")
 SOURCES = ["pack.cpp", "quant_cb.cpp", "gather.hip", "gemv.hip", "gemv_cb.hip", "gemv_cb8.hip", "gemv_cb2.hip", "gemv_list.hip",
            "gemv_bal.hip"]
+# The key/value cache: in libspqt.so only, since it has no reducers and no stamps.
+KV_SOURCES = ["kv_append.hip", "kv_attend.hip", "kv_evict.hip"]
 CALIB_LIB = os.path.join(PKG, "libspqt_calib.so")       # benchmark-only helper kernels
 CALIB_SOURCES = ["calib.hip", "baseline_rowmajor.hip"]
 # The same kernels with wall-clock stamps per wavefront (python -m paper_2511_04477_amd.timeline).
@@ -94,7 +96,7 @@ def build(verbose: bool = False) -> str:
             _jobs(TIMELINE_LIB, SOURCES, defines=("SPQT_TIMELINE=1",), tag="tl_"),
             _jobs(GIVEUP_LIB, GIVEUP_SOURCES, defines=("SPQT_TEST_GIVE_UP=1",), tag="gu_"),
             _jobs(HANDOVER_LIB, SOURCES, defines=("SPQT_TEST_HAND_OVER=1",), tag="ho_"),
-            _jobs(LIB, SOURCES)]
+            _jobs(LIB, SOURCES + KV_SOURCES)]
     # every object of every library in one pool (longest first), then the links
     compiles = sorted((c for cs, _ in plan for c in cs), key=lambda c: -os.path.getsize(c[-1]))
     fastcall = FASTCALL_LIB + f".tmp{os.getpid()}"

@@ -1,0 +1,125 @@
+// spqt_kv_append: new tokens into the pages, 8 bits with a scale per block, head and side; spqt_kv_read: back to 16 bits.
+#include "kv_tile.hpp"
+
+namespace {
+
+using namespace spqt;
+using namespace spqt::kv;
+
+// One workgroup per block that the call writes to, head and side (keys or values); the first one does the sequence's first and last block,
+// one after the other, since the first reads from the tail what the last one overwrites there.
+template <int D, bool BF16>
+__global__ __launch_bounds__(kTileThreads) void spqt_kv_append_kernel(Cache c, Rows keys, Rows values, int rows, const int32_t *counts) {
+    __shared__ Tile<D> tile;
+    const int s = blockIdx.z, head = blockIdx.y >> 1, which = blockIdx.y & 1;
+    const int length = length_of(c, s), count = count_of(counts, s, rows);
+    if (length == 0 || count == 0) return;
+    const int row0 = length - count, start = row0 < 0 ? 0 : row0;             // position of row 0, and of the first token that there is
+    const int first = block_of(start), last = block_of(length - 1);
+    const Rows r = which ? values : keys;
+    const uint16_t *in = r.data + s * r.sequence + head * r.head;
+    uint16_t *tail = c.tail + (((size_t)s * c.kv_heads + head) * 2 + which) * (size_t)(kBlock * D);
+    const int32_t *table = c.table + (size_t)s * c.max_blocks;
+
+    int block = first + (int)blockIdx.x;
+    if (blockIdx.x > 0 && block >= last) return;
+    for (;;) {
+        const int base = block * kBlock;
+        const int from = start > base ? start - base : 0, to = length - base < kBlock ? length - base : kBlock;
+        const uint32_t page = (uint32_t)table[block];
+        const bool there = page < c.pages;
+        uint32_t pair = 0;
+        for (int p = from * (D / 8) + (int)threadIdx.x; p < to * (D / 8); p += kTileThreads) {
+            const int t = p / (D / 8), d = p % (D / 8) * 8;
+            const u32x4 x = *reinterpret_cast<const u32x4 *>(in + (base + t - row0) * r.row + d);
+            *reinterpret_cast<u32x4 *>(&tile.v[t][d]) = x;
+            pair = larger_pair(larger_pair(pair, x.x), larger_pair(x.y, larger_pair(x.z, x.w)));
+            if (block == last && to < kBlock) *reinterpret_cast<u32x4 *>(tail + p * 8) = x;
+        }
+        const float fresh = scale_of<BF16>(largest_of(tile, pair));
+        if (there) {
+            float *scales = c.scales + scale_at(c, page, head, which);
+            const float held = from > 0 ? *scales : 0.0f;
+            const float scale = held != held || fresh != fresh ? __builtin_nanf("") : __builtin_fmaxf(held, fresh);
+            const bool grown = from > 0 && !(scale == held);
+            if (grown)
+                for (int p = (int)threadIdx.x; p < from * (D / 8); p += kTileThreads)
+                    *reinterpret_cast<u32x4 *>(&tile.v[p / (D / 8)][p % (D / 8) * 8]) = *reinterpret_cast<const u32x4 *>(tail + p * 8);
+            __syncthreads();                       // the tile is whole, and everyone has the old scale
+            store_tile<D, BF16>(c, tile, page, head, which, grown ? 0 : from, to, scale);
+            if (threadIdx.x == 0) *scales = scale;
+            if (which == 0 && c.weights && (int)threadIdx.x >= from && (int)threadIdx.x < to) c.weights[weight_at(c, page, head) + threadIdx.x] = 0.0f;
+        }
+        if (blockIdx.x > 0 || block == last) return;
+        block = last;
+        __syncthreads();                           // the tile is free again
+    }
+}
+
+// One workgroup per block that the call reads from, head and side.  The codes of a block go through shared memory as they are.
+template <int D, bool BF16>
+__global__ __launch_bounds__(kTileThreads) void spqt_kv_read_kernel(Cache c, Rows keys, Rows values, int rows, const int32_t *counts) {
+    __shared__ uint8_t codes[kBlock * D];
+    const int s = blockIdx.z, head = blockIdx.y >> 1, which = blockIdx.y & 1;
+    const int length = length_of(c, s), count = count_of(counts, s, rows), row0 = length - count;
+    const int block = block_of(row0) + (int)blockIdx.x, base = block * kBlock;
+    if (base - row0 >= rows) return;
+    const Rows r = which ? values : keys;
+    uint16_t *out = r.data + s * r.sequence + head * r.head;
+    const bool any = block >= 0 && base < length;
+    uint32_t page = any ? (uint32_t)c.table[(size_t)s * c.max_blocks + block] : 0u;
+    const bool there = page < c.pages;
+    if (!there) page = 0;
+    const float scale = there ? c.scales[scale_at(c, page, head, which)] : __builtin_nanf("");
+    if (any) {
+        const uint8_t *in = c.codes + codes_at(c, page, head, which);
+        for (int p = (int)threadIdx.x * 16; p < kBlock * D; p += kTileThreads * 16) *reinterpret_cast<u32x4 *>(codes + p) = *reinterpret_cast<const u32x4 *>(in + p);
+    }
+    __syncthreads();
+    for (int p = (int)threadIdx.x; p < kBlock * (D / 8); p += kTileThreads) {
+        const int t = p / (D / 8), d = p % (D / 8) * 8, i = base + t - row0;
+        if (i < 0 || i >= rows) continue;
+        u32x4 x = {0u, 0u, 0u, 0u};
+        if (i < count && base + t >= 0)
+#pragma unroll
+            for (int j = 0; j < 8; ++j) {
+                const uint32_t byte = codes[which ? (d + j) * kBlock + place_of(t) : t * D + d + j];
+                x[j / 2] |= (uint32_t)value_of<BF16>(byte, scale) << (16 * (j % 2));
+            }
+        *reinterpret_cast<u32x4 *>(out + i * r.row + d) = x;
+    }
+}
+
+int check_call(const spqt_kv_cache *cache, bool tail, const spqt_kv_rows *k, const spqt_kv_rows *v, int rows, const int32_t *counts) {
+    int rc = check_cache(cache, tail);
+    if (rc == SPQT_OK) rc = check_rows(k);
+    if (rc == SPQT_OK) rc = check_rows(v);
+    if (rc != SPQT_OK) return rc;
+    if (rows < 1 || rows > kMaxRows) return SPQT_ESHAPE;
+    return (uintptr_t)counts % 4 != 0 ? SPQT_EALIGN : SPQT_OK;
+}
+
+}  // namespace
+
+extern "C" int spqt_kv_append(const spqt_kv_cache *cache, const spqt_kv_rows *k, const spqt_kv_rows *v, int rows, const int32_t *counts, void *stream) {
+    const int rc = check_call(cache, true, k, v, rows, counts);
+    if (rc != SPQT_OK) return rc;
+    const int most = (rows + kBlock - 2) / kBlock + 1;                    // blocks that `rows` tokens can lie in
+    const dim3 grid(most > 2 ? most - 1 : 1, 2 * cache->kv_heads, cache->sequences);
+    dispatch(*cache, [&](auto dim, auto bf16) {
+        hipLaunchKernelGGL((spqt_kv_append_kernel<decltype(dim)::value, decltype(bf16)::value>), grid, dim3(kTileThreads), 0, (hipStream_t)stream, view(*cache),
+                           view(*k), view(*v), rows, counts);
+    });
+    return launched();
+}
+
+extern "C" int spqt_kv_read(const spqt_kv_cache *cache, const spqt_kv_rows *k_out, const spqt_kv_rows *v_out, int rows, const int32_t *counts, void *stream) {
+    const int rc = check_call(cache, false, k_out, v_out, rows, counts);
+    if (rc != SPQT_OK) return rc;
+    const dim3 grid((rows + kBlock - 2) / kBlock + 1, 2 * cache->kv_heads, cache->sequences);
+    dispatch(*cache, [&](auto dim, auto bf16) {
+        hipLaunchKernelGGL((spqt_kv_read_kernel<decltype(dim)::value, decltype(bf16)::value>), grid, dim3(kTileThreads), 0, (hipStream_t)stream, view(*cache),
+                           view(*k_out), view(*v_out), rows, counts);
+    });
+    return launched();
+}
