@@ -6,7 +6,7 @@
 // needs as an operand of O^T = V^T P^T, given the order in which a page holds the values (place_of): probabilities never leave their lane.
 // Codes are exact in fp16, so the products are those of the 16-bit queries with the codes; the scale of a block goes into its scores and
 // into its probabilities.
-#include "kv_common.hpp"
+#include "kv_attend.hpp"
 
 namespace {
 
@@ -15,35 +15,6 @@ using namespace spqt::kv;
 
 constexpr int kThreads = 256, kWaves = kThreads / 64;
 constexpr uint32_t kLeast = 8;                            // blocks that a workgroup takes at least, if there are as many
-constexpr float kLog2e = 1.4426950408889634f, kLn2 = 0.6931471805599453f;
-constexpr float kNone = -__builtin_inff();
-// Probabilities go to the matrix instructions as two fp16 numbers, 22 bits in all, times 2^15: fp16's smallest number is 2^-39 of the largest one.
-constexpr float kLift = 0x1p15f;
-
-struct Call {
-    Rows q, out;
-    float *lse;
-    const int32_t *counts;
-    int rows, q_heads, group, window;
-    float scale, decay;
-};
-
-// A lane's row: its place in the call, and the tokens low .. high that it sees (none if high < low).
-struct Row {
-    int i, head;
-    int low, high;
-};
-__device__ __forceinline__ Row row_of(const Call &a, int r, int head, int length, int count) {
-    Row w;
-    w.i = r / a.group;
-    w.head = head * a.group + r % a.group;
-    const int at = length - count + w.i;
-    const bool live = w.i < count && at >= 0 && at < length;
-    w.high = live ? at : -1;
-    w.low = live ? (a.window > 0 && at - a.window + 1 > 0 ? at - a.window + 1 : 0) : 0;
-    return w;
-}
-
 __device__ __forceinline__ int lanes_max(int v) {            // over the 16 rows
 #pragma unroll
     for (int step = 1; step < 16; step *= 2) {
@@ -61,41 +32,14 @@ __device__ __forceinline__ float columns_sum(float v) {
     return v + __shfl_xor(v, 32);
 }
 
-// A row of Q as an operand, 32 elements a step: step j of a lane are elements 64 (j / 2) + 16 (lane / 16) + 8 (j % 2) on, as in load_keys.
-// bf16 rows are scaled by a power of two to have their largest element in 2^14 .. 2^15, where fp16 holds them (exactly, down to
-// 2^-30 of the largest); the factor that undoes it is returned.
+// A row of Q as an operand, 32 elements a step: step j of a lane are elements 64 (j / 2) + 16 (lane / 16) + 8 (j % 2) on, as in load_keys. Returns queries_f16's factor.
 template <int D, bool BF16>
 __device__ __forceinline__ float load_queries(f16x8 (&q)[D / 32], const uint16_t *row, bool live, int lane) {
     u32x4 w[D / 32];
 #pragma unroll
     for (int j = 0; j < D / 32; ++j)
         w[j] = live ? *reinterpret_cast<const u32x4 *>(row + 64 * (j / 2) + 16 * (lane / 16) + 8 * (j % 2)) : u32x4{0u, 0u, 0u, 0u};
-    if (!BF16) {
-#pragma unroll
-        for (int j = 0; j < D / 32; ++j) q[j] = __builtin_bit_cast(f16x8, w[j]);
-        return 1.0f;
-    }
-    uint32_t largest = 0;
-#pragma unroll
-    for (int j = 0; j < D / 32; ++j)
-#pragma unroll
-        for (int e = 0; e < 4; ++e) {
-            const uint32_t a = w[j][e] & 0x7FFFu, b = w[j][e] >> 16 & 0x7FFFu;
-            largest = largest > a ? largest : a;
-            largest = largest > b ? largest : b;
-        }
-    for (int step = 16; step < 64; step *= 2) {
-        const uint32_t o = (uint32_t)__shfl_xor((int)largest, step);
-        largest = o > largest ? o : largest;
-    }
-    // exponent field of the largest, kept where 2^(141 - e) and its inverse are numbers; an infinity or a NaN stays what it is
-    const int e = clamped((int)(largest >> 7), 20, 254);
-    const float up = as_float((uint32_t)(268 - e) << 23), down = as_float((uint32_t)(e - 14) << 23);
-#pragma unroll
-    for (int j = 0; j < D / 32; ++j)
-#pragma unroll
-        for (int x = 0; x < 8; ++x) q[j][x] = (_Float16)(as_float(x % 2 ? w[j][x / 2] & 0xFFFF0000u : w[j][x / 2] << 16) * up);
-    return down;
+    return queries_f16<BF16>(w, q, 16);
 }
 
 // 16 tokens' keys as an operand.
@@ -250,20 +194,6 @@ struct Wave {
             block(b0 + here - 1, scale_of(here - 1, 0), scale_of(here - 1, 1), lane, []() {}, []() {});
         }
     }
-};
-
-// What the rows' sums over some tokens and over others make together: (top, total, x) with x in units of 2^top.
-struct Meeting {
-    float top = kNone, total = 0.0f;
-    __device__ __forceinline__ void add(float other_top, float other_total, float &mine, float &others) {
-        const float most = __builtin_fmaxf(top, other_top), from = most == kNone ? 0.0f : most;
-        mine = __builtin_amdgcn_exp2f(top - from);
-        others = __builtin_amdgcn_exp2f(other_top - from);
-        total = total * mine + other_total * others;
-        top = most;
-    }
-    __device__ __forceinline__ float inverse() const { return total == 0.0f ? 0.0f : 1.0f / total; }
-    __device__ __forceinline__ float lse() const { return total == 0.0f ? kNone : (top == kNone ? 0.0f : top) * kLn2 + __builtin_logf(total); }
 };
 
 // A few rows over the whole cache: up to 16 rows of a kv head and sequence, a unit, share one pass over its blocks.  All units' blocks, in order, are dealt out
@@ -636,7 +566,8 @@ extern "C" int spqt_kv_attention(const spqt_kv_cache *cache, const spqt_kv_rows 
     dispatch(*cache, [&](auto dim, auto bf16) {
         constexpr int D = decltype(dim)::value;
         constexpr bool B = decltype(bf16)::value;
-        hipLaunchKernelGGL((spqt_kv_step_kernel<D, B>), dim3(kShares), dim3(step_threads(D)), 0, (hipStream_t)stream, view(*cache), a, space, cache->sequences, tiles);
+        if (is_prompt(a, D)) launch_prompt(*cache, a, (hipStream_t)stream);
+        else hipLaunchKernelGGL((spqt_kv_step_kernel<D, B>), dim3(kShares), dim3(step_threads(D)), 0, (hipStream_t)stream, view(*cache), a, space, cache->sequences, tiles);
         if (cache->weights)
             hipLaunchKernelGGL((spqt_kv_weigh_kernel<D, B>), dim3((cache->max_blocks + kWaves - 1) / kWaves, cache->kv_heads, cache->sequences), dim3(kThreads), 0,
                                (hipStream_t)stream, view(*cache), a);

@@ -1,0 +1,91 @@
+// What the attention kernels share: a call, its rows and what each of them sees, and how partial sums of rows join.
+#ifndef SPQT_KV_ATTEND_HPP
+#define SPQT_KV_ATTEND_HPP
+
+#include "kv_common.hpp"
+
+namespace spqt {
+namespace kv {
+
+constexpr float kLog2e = 1.4426950408889634f, kLn2 = 0.6931471805599453f;
+constexpr float kNone = -__builtin_inff();
+// Probabilities go to the matrix instructions as two fp16 numbers, 22 bits in all, times 2^15: fp16's smallest number is 2^-39 of the largest one.
+constexpr float kLift = 0x1p15f;
+
+struct Call {
+    Rows q, out;
+    float *lse;
+    const int32_t *counts;
+    int rows, q_heads, group, window;
+    float scale, decay;
+};
+
+// A lane's row: its place in the call, and the tokens low .. high that it sees (none if high < low).
+struct Row {
+    int i, head;
+    int low, high;
+};
+__device__ __forceinline__ Row row_of(const Call &a, int r, int head, int length, int count) {
+    Row w;
+    w.i = r / a.group;
+    w.head = head * a.group + r % a.group;
+    const int at = length - count + w.i;
+    const bool live = w.i < count && at >= 0 && at < length;
+    w.high = live ? at : -1;
+    w.low = live ? (a.window > 0 && at - a.window + 1 > 0 ? at - a.window + 1 : 0) : 0;
+    return w;
+}
+
+// What the rows' sums over some tokens and over others make together: (top, total, x) with x in units of 2^top.
+struct Meeting {
+    float top = kNone, total = 0.0f;
+    __device__ __forceinline__ void add(float other_top, float other_total, float &mine, float &others) {
+        const float most = __builtin_fmaxf(top, other_top), from = most == kNone ? 0.0f : most;
+        mine = __builtin_amdgcn_exp2f(top - from);
+        others = __builtin_amdgcn_exp2f(other_top - from);
+        total = total * mine + other_total * others;
+        top = most;
+    }
+    __device__ __forceinline__ float inverse() const { return total == 0.0f ? 0.0f : 1.0f / total; }
+    __device__ __forceinline__ float lse() const { return total == 0.0f ? kNone : (top == kNone ? 0.0f : top) * kLn2 + __builtin_logf(total); }
+};
+
+// A lane's part of a row of Q in fp16; `step` is the first distance between the lanes that share the row.  bf16 rows are scaled by a power of two to have
+// their largest element in 2^14 .. 2^15, where fp16 holds them (exactly, down to 2^-30 of the largest); the factor that undoes it is returned.
+template <bool BF16, int N>
+__device__ __forceinline__ float queries_f16(const u32x4 (&w)[N], f16x8 (&q)[N], int step) {
+    if (!BF16) {
+#pragma unroll
+        for (int j = 0; j < N; ++j) q[j] = __builtin_bit_cast(f16x8, w[j]);
+        return 1.0f;
+    }
+    uint32_t largest = 0;
+#pragma unroll
+    for (int j = 0; j < N; ++j)
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+            const uint32_t x = w[j][e] & 0x7FFFu, y = w[j][e] >> 16 & 0x7FFFu;
+            largest = largest > x ? largest : x;
+            largest = largest > y ? largest : y;
+        }
+    for (; step < 64; step *= 2) {
+        const uint32_t o = (uint32_t)__shfl_xor((int)largest, step);
+        largest = o > largest ? o : largest;
+    }
+    // exponent field of the largest, kept where 2^(141 - e) and its inverse are numbers; an infinity or a NaN stays what it is
+    const int e = clamped((int)(largest >> 7), 20, 254);
+    const float up = as_float((uint32_t)(268 - e) << 23), down = as_float((uint32_t)(e - 14) << 23);
+#pragma unroll
+    for (int j = 0; j < N; ++j)
+#pragma unroll
+        for (int x = 0; x < 8; ++x) q[j][x] = (_Float16)(as_float(x % 2 ? w[j][x / 2] & 0xFFFF0000u : w[j][x / 2] << 16) * up);
+    return down;
+}
+
+// Many rows (kv_prompt.hip); true where it is for this call.
+bool is_prompt(const Call &a, int head_dim);
+void launch_prompt(const spqt_kv_cache &cache, const Call &a, hipStream_t stream);
+
+}  // namespace kv
+}  // namespace spqt
+#endif
