@@ -1,4 +1,4 @@
-// Attention of many rows over the cache: a workgroup takes kRows of a kv head's rows and goes through the blocks of tokens that they see; the codes of a
+// Attention of many rows over the cache: a workgroup takes 256 (128) of a kv head's rows and goes through the blocks of tokens that they see; the codes of a
 // block are made fp16 once, in shared memory, for all of them.
 //
 // With S^T = K Q^T a lane of v_mfma_f32_32x32x16_f16 has one row of Q and half of each 32 tokens, and what it has of P^T is an operand of
@@ -13,48 +13,63 @@ using namespace spqt::kv;
 typedef float f32x2 __attribute__((ext_vector_type(2)));
 typedef float f32x16 __attribute__((ext_vector_type(16)));
 
-constexpr int kThreads = 256, kWaves = kThreads / 64;
-
-// Rows of a wavefront: 64, as two operands that share every read of a block, where sums and queries leave the registers for it.
+// Eight wavefronts of 32 rows, two on every SIMD; four where sums and queries of longer heads leave no registers for two.
 template <int D>
 struct Shape {
-    static constexpr int kTiles = D > 128 ? 1 : 2;
-    static constexpr int kRows = kWaves * kTiles * 32;
+    static constexpr int kThreads = D > 128 ? 256 : 512, kWaves = kThreads / 64, kRows = kWaves * 32;
     static constexpr int kKeyStride = D + 8, kValueStride = kBlock + 8;      // fp16 numbers; 16 lines are in 16 different sets of banks
 };
 
+// A thread's part of a block's keys or values, on its way from codes to numbers.
 template <int D>
-struct Staged {                          // a block's codes on their way
-    u32x4 keys[D / 64], values[(2 * D + kThreads - 1) / kThreads][2];
+struct StagedKeys {
+    static constexpr int kThreads = Shape<D>::kThreads, kParts = (D * 4 + kThreads - 1) / kThreads;
+    u32x4 part[kParts];                  // 16 elements of a token
 
-    __device__ __forceinline__ void fetch(const uint8_t *page) {
+    template <class F>
+    __device__ __forceinline__ void each(F f) {
 #pragma unroll
-        for (int i = 0; i < D / 64; ++i) keys[i] = *reinterpret_cast<const u32x4 *>(page + (threadIdx.x + i * kThreads) * 16);
-#pragma unroll
-        for (int i = 0; i < (2 * D + kThreads - 1) / kThreads; ++i) {
-            const int line = threadIdx.x + i * kThreads;      // element and half of the lanes
-            if (2 * D % kThreads != 0 && line >= 2 * D) continue;
-#pragma unroll
-            for (int x = 0; x < 2; ++x)
-                values[i][x] = *reinterpret_cast<const u32x4 *>(page + kBlock * D + (line / 2) * kBlock + (line % 2 + 2 * x) * 16);
+        for (int i = 0; i < kParts; ++i) {
+            const int at = threadIdx.x + i * kThreads;
+            if (D * 4 % kThreads == 0 || at < D * 4) f(part[i], at);
         }
     }
-    __device__ __forceinline__ void put_down(_Float16 *k, _Float16 *v) const {
+    __device__ __forceinline__ void fetch(const uint8_t *page) {
+        each([&](u32x4 &x, int at) { x = *reinterpret_cast<const u32x4 *>(page + at * 16); });
+    }
+    __device__ __forceinline__ void put_down(_Float16 *k) {
+        each([&](u32x4 &x, int at) {
+            _Float16 *to = k + at / (D / 16) * Shape<D>::kKeyStride + at % (D / 16) * 16;
+            *reinterpret_cast<f16x8 *>(to) = codes_f16(u32x2{x.x, x.y});
+            *reinterpret_cast<f16x8 *>(to + 8) = codes_f16(u32x2{x.z, x.w});
+        });
+    }
+};
+template <int D>
+struct StagedValues {
+    static constexpr int kThreads = Shape<D>::kThreads, kParts = (D * 4 + kThreads - 1) / kThreads;
+    u32x2 part[kParts][2];               // of one element: fours 0 and 2, or 1 and 3, of two of the block's 16s
+
+    template <class F>
+    __device__ __forceinline__ void each(F f) {
 #pragma unroll
-        for (int i = 0; i < D / 64; ++i) {
-            const int at = (threadIdx.x + i * kThreads) * 16;
-            _Float16 *to = k + at / D * Shape<D>::kKeyStride + at % D;
-            *reinterpret_cast<f16x8 *>(to) = codes_f16(u32x2{keys[i].x, keys[i].y});
-            *reinterpret_cast<f16x8 *>(to + 8) = codes_f16(u32x2{keys[i].z, keys[i].w});
+        for (int i = 0; i < kParts; ++i) {
+            const int at = threadIdx.x + i * kThreads;
+            if (D * 4 % kThreads == 0 || at < D * 4) f(part[i], at / 4, at / 2 % 2, at % 2);
         }
+    }
+    __device__ __forceinline__ void fetch(const uint8_t *page) {
+        each([&](u32x2 (&x)[2], int d, int half, int pair) {
 #pragma unroll
-        for (int i = 0; i < (2 * D + kThreads - 1) / kThreads; ++i) {
-            const int line = threadIdx.x + i * kThreads;
-            if (2 * D % kThreads != 0 && line >= 2 * D) continue;
-#pragma unroll
-            for (int t = 0; t < 4; ++t)
-                *reinterpret_cast<f16x8 *>(v + line / 2 * Shape<D>::kValueStride + t * 16 + line % 2 * 8) = codes_f16(u32x2{values[i][0][t], values[i][1][t]});
-        }
+            for (int y = 0; y < 2; ++y) x[y] = *reinterpret_cast<const u32x2 *>(page + kBlock * D + d * kBlock + (half + 2 * y) * 16 + pair * 8);
+        });
+    }
+    __device__ __forceinline__ void put_down(_Float16 *v) {
+        each([&](u32x2 (&x)[2], int d, int half, int pair) {
+            _Float16 *to = v + d * Shape<D>::kValueStride + pair * 32 + half * 8;
+            *reinterpret_cast<f16x8 *>(to) = codes_f16(u32x2{x[0].x, x[1].x});
+            *reinterpret_cast<f16x8 *>(to + 16) = codes_f16(u32x2{x[0].y, x[1].y});
+        });
     }
 };
 
@@ -63,10 +78,22 @@ __device__ __forceinline__ float halves_max(float v) {
     return __builtin_fmaxf(as_float(r[0]), as_float(r[1]));
 }
 
+// Waits for the workgroup's shared memory, not for what is on its way from global memory.
+__device__ __forceinline__ void meet() {
+    __builtin_amdgcn_fence(__ATOMIC_RELEASE, "workgroup", "local");
+    __builtin_amdgcn_s_barrier();
+    __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "workgroup", "local");
+}
+
+// The wavefronts of a SIMD take turns: while the first four's products run, O += V P of one block and S = K Q of the next, the other four work out the
+// probabilities of theirs, and the other way round.  In the latter turn a wavefront also makes its part of the next block's codes numbers:
+//
+//   turn        2b                              2b + 1
+//   first four  O += V P(b-1), S = K(b) Q       P(b), K(b+1), V(b)
+//   others      P(b-1), K(b+1), V(b)            O += V P(b-1), S = K(b) Q
 template <int D, bool BF16>
-__global__ __launch_bounds__(kThreads) void spqt_kv_prompt_kernel(Cache c, Call a, int tiles) {
+__global__ __launch_bounds__(Shape<D>::kThreads) void spqt_kv_prompt_kernel(Cache c, Call a, int tiles) {
     typedef Shape<D> S;
-    constexpr int kTiles = S::kTiles;
     __shared__ __attribute__((aligned(16))) _Float16 keys[2][kBlock * S::kKeyStride];
     __shared__ __attribute__((aligned(16))) _Float16 values[2][D * S::kValueStride];
     // heads first: workgroups of one head run on one XCD if there are eight; the rows that see most first
@@ -74,187 +101,188 @@ __global__ __launch_bounds__(kThreads) void spqt_kv_prompt_kernel(Cache c, Call 
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), column = lane & 31, half = lane >> 5;
     const int length = length_of(c, s), count = count_of(a.counts, s, a.rows), rows = a.rows * a.group;
 
-    // the tokens that any, and that every row of the workgroup and of the wavefront sees
+    // the blocks that any row of the workgroup sees
     const int r0 = tile * S::kRows;
     const Row first = row_of(a, r0, head, length, count);
-    int last_live = r0 + S::kRows - 1 < count * a.group - 1 ? r0 + S::kRows - 1 : count * a.group - 1;
+    const int last_live = r0 + S::kRows < count * a.group ? r0 + S::kRows - 1 : count * a.group - 1;
     const Row last = row_of(a, last_live < 0 ? 0 : last_live, head, length, count);
     const bool any = last_live >= r0 && last.high >= 0;
-    const int begin = any ? block_of(first.high >= 0 ? first.low : 0) : 0, end = any ? block_of(last.high) + 1 : 0;
+    const int begin = any ? block_of(first.high >= 0 ? first.low : 0) : 0, n = any ? block_of(last.high) + 1 - begin : 0;
 
-    Row row[kTiles];
-    f16x8 q[kTiles][D / 16];
-    float scale[kTiles], top[kTiles], total[kTiles], unit[kTiles];
-    f32x16 acc[kTiles][D / 32];
-    int full_low = 0, full_high = 0x7FFFFFFF;                 // every row of the wavefront sees these tokens
-#pragma unroll
-    for (int m = 0; m < kTiles; ++m) {
-        const int r = r0 + (wave * kTiles + m) * 32 + column;
-        row[m] = row_of(a, r, head, length, count);
-        if (r >= rows) row[m].high = -1;
-        const bool live = row[m].high >= 0;
-        const uint16_t *from = a.q.data + s * a.q.sequence + row[m].i * a.q.row + row[m].head * a.q.head;
+    const int r = r0 + wave * 32 + column;
+    Row row = row_of(a, r, head, length, count);
+    if (r >= rows) row.high = -1;
+    f16x8 q[D / 16];
+    float scale, top = kNone, total = 0.0f, unit = 1.0f;
+    {
+        const bool live = row.high >= 0;
+        const uint16_t *from = a.q.data + s * a.q.sequence + row.i * a.q.row + row.head * a.q.head;
         u32x4 w[D / 16];
 #pragma unroll
         for (int j = 0; j < D / 16; ++j) w[j] = live ? *reinterpret_cast<const u32x4 *>(from + 16 * j + 8 * half) : u32x4{0u, 0u, 0u, 0u};
-        scale[m] = a.scale * kLog2e * queries_f16<BF16, D / 16>(w, q[m], 32);
-        top[m] = kNone;
-        total[m] = 0.0f;
-        unit[m] = 1.0f;
+        scale = a.scale * kLog2e * queries_f16<BF16>(w, q, 32);
+    }
+    int full_low = row.low, full_high = row.high;             // every row of the wavefront sees these tokens
 #pragma unroll
-        for (int i = 0; i < D / 32; ++i)
-#pragma unroll
-            for (int e = 0; e < 16; ++e) acc[m][i][e] = 0.0f;
-        int low = row[m].low, high = row[m].high;
-#pragma unroll
-        for (int step = 1; step < 32; step *= 2) {
-            const int l = __shfl_xor(low, step), h = __shfl_xor(high, step);
-            low = l > low ? l : low;
-            high = h < high ? h : high;
-        }
-        full_low = low > full_low ? low : full_low;
-        full_high = high < full_high ? high : full_high;
+    for (int step = 1; step < 32; step *= 2) {
+        const int l = __shfl_xor(full_low, step), h = __shfl_xor(full_high, step);
+        full_low = l > full_low ? l : full_low;
+        full_high = h < full_high ? h : full_high;
     }
     full_low = __builtin_amdgcn_readfirstlane(full_low);
     full_high = __builtin_amdgcn_readfirstlane(full_high);
+    f32x16 acc[D / 32];
+#pragma unroll
+    for (int i = 0; i < D / 32; ++i) acc[i] = f32x16{};
 
-    const int32_t *table = c.table + (size_t)s * c.max_blocks;
-    struct Page {
-        const uint8_t *codes;
-        float scale_k, scale_v;
-    };
-    auto page_of = [&](int block) {
-        Page p;
-        uint32_t page = (uint32_t)table[block];
-        const bool there = page < c.pages;
-        if (!there) page = 0;
-        const float *scales = c.scales + scale_at(c, page, head, 0);
-        p.codes = c.codes + codes_at(c, page, head, 0);
-        p.scale_k = there ? scales[0] : __builtin_nanf("");
-        p.scale_v = there ? scales[1] : __builtin_nanf("");
-        return p;
-    };
-
-    auto attend = [&](int block, float scale_k, float scale_v, const _Float16 *k, const _Float16 *v, auto masked) {
-        f32x16 p[kTiles][2];
+    // Pages and scales of 64 blocks from `base` on, one per lane: looked up rarely, so that no turn waits for a chain of loads.
+    const int32_t *table = c.table + (size_t)s * c.max_blocks + begin;
+    uint32_t pages = 0;
+    float scales[2] = {0.0f, 0.0f};
+    int base = 0;
+    auto look_up = [&](int b) {
+        base = b;
+        const int at = b + lane < n ? b + lane : n - 1;
+        pages = (uint32_t)table[at];
+        const bool there = pages < c.pages;
+        if (!there) pages = 0;
 #pragma unroll
-        for (int t = 0; t < 2; ++t) {
-#pragma unroll
-            for (int j = 0; j < D / 16; ++j) {
-                const f16x8 x = *reinterpret_cast<const f16x8 *>(k + (32 * t + column) * S::kKeyStride + 16 * j + 8 * half);
-#pragma unroll
-                for (int m = 0; m < kTiles; ++m) {
-                    if (j == 0) p[m][t] = __builtin_amdgcn_mfma_f32_32x32x16_f16(x, q[m][j], f32x16{}, 0, 0, 0);
-                    else p[m][t] = __builtin_amdgcn_mfma_f32_32x32x16_f16(x, q[m][j], p[m][t], 0, 0, 0);
-                }
-            }
+        for (int which = 0; which < 2; ++which) {
+            scales[which] = c.scales[scale_at(c, pages, head, which)];
+            if (!there) scales[which] = __builtin_nanf("");
         }
-        f16x8 lifted[kTiles][4];
+    };
+    auto codes_of = [&](int b) { return c.codes + codes_at(c, (uint32_t)__builtin_amdgcn_readlane((int)pages, b - base), head, 0); };
+    auto scale_of = [&](int b, int which) { return as_float((uint32_t)__builtin_amdgcn_readlane((int)as_u32(scales[which]), b - base)); };
+
+    f32x16 p[2];
+    f16x8 lifted[4];
+    // O += V P of the last block and S = K Q of this one: kProducts matrix instructions in a row, whose other operands are read kAhead ahead.
+    constexpr int kAhead = 6, kValueProducts = D / 8, kProducts = kValueProducts + D / 8;
+    auto products = [&](const _Float16 *v, const _Float16 *k, auto skip, auto stop) {
+        constexpr int from = decltype(skip)::value ? kValueProducts : 0, to = decltype(stop)::value ? kValueProducts : kProducts;
+        f16x8 x[kAhead];
+        auto read = [&](int i) {
+            if (i < kValueProducts) return *reinterpret_cast<const f16x8 *>(v + (i % (D / 32) * 32 + column) * S::kValueStride + i / (D / 32) * 16 + 8 * half);
+            i -= kValueProducts;
+            return *reinterpret_cast<const f16x8 *>(k + (i % 2 * 32 + column) * S::kKeyStride + i / 2 * 16 + 8 * half);
+        };
 #pragma unroll
-        for (int m = 0; m < kTiles; ++m) {
-            const float by = scale[m] * scale_k;
-            if (decltype(masked)::value) {
+        for (int i = from; i < from + kAhead; ++i) x[i % kAhead] = read(i);
+        __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
-                for (int t = 0; t < 2; ++t)
-#pragma unroll
-                    for (int e = 0; e < 16; ++e) {
-                        const int token = block * kBlock + 32 * t + 8 * (e / 4) + 4 * half + e % 4;
-                        if (!(token >= row[m].low && token <= row[m].high)) p[m][t][e] = kNone;
-                    }
+        for (int i = from; i < to; ++i) {
+            if (i < kValueProducts) {
+                acc[i % (D / 32)] = __builtin_amdgcn_mfma_f32_32x32x16_f16(x[i % kAhead], lifted[i / (D / 32)], acc[i % (D / 32)], 0, 0, 0);
+            } else {
+                const int t = (i - kValueProducts) % 2, j = (i - kValueProducts) / 2;
+                p[t] = __builtin_amdgcn_mfma_f32_32x32x16_f16(x[i % kAhead], q[j], j == 0 ? f32x16{} : p[t], 0, 0, 0);
             }
-            float most = p[m][0][0];
+            if (i + kAhead < to) x[i % kAhead] = read(i + kAhead);
+            __builtin_amdgcn_sched_barrier(0);
+        }
+    };
+    auto probabilities = [&](int block, float scale_k, float scale_v, auto masked) {
+        const float by = scale * scale_k;
+        if (decltype(masked)::value) {
 #pragma unroll
             for (int t = 0; t < 2; ++t)
 #pragma unroll
-                for (int e = 0; e < 16; ++e) most = __builtin_fmaxf(most, p[m][t][e]);
-            most = halves_max(most);
-            const bool sees = !decltype(masked)::value || !(most == kNone);
-            most = __builtin_fmaxf(top[m], sees ? most * by : kNone);
-            const float from = most == kNone ? 0.0f : most;
-            float shrink = __builtin_amdgcn_exp2f(top[m] - from);
-            top[m] = most;
-            total[m] *= shrink;
-            if (sees) {
-                shrink *= unit[m] / scale_v;
-                unit[m] = scale_v;
-            }
-            const float lifted_from = from - 15.0f;
-            float sum = 0.0f;
-#pragma unroll
-            for (int t = 0; t < 2; ++t)
-#pragma unroll
-                for (int e = 0; e < 16; e += 2) {
-                    f32x2 x;
-#pragma unroll
-                    for (int i = 0; i < 2; ++i) {
-                        const float y = __builtin_amdgcn_exp2f(__builtin_fmaf(p[m][t][e + i], by, -lifted_from));
-                        x[i] = decltype(masked)::value && p[m][t][e + i] == kNone ? 0.0f : y;
-                        sum += x[i];
-                    }
-                    const f16x2 h = __builtin_convertvector(x, f16x2);
-                    lifted[m][2 * t + e / 8][e % 8] = h[0];
-                    lifted[m][2 * t + e / 8][e % 8 + 1] = h[1];
+                for (int e = 0; e < 16; ++e) {
+                    const int token = block * kBlock + 32 * t + 8 * (e / 4) + 4 * half + e % 4;
+                    if (!(token >= row.low && token <= row.high)) p[t][e] = kNone;
                 }
-            total[m] += sum * (1.0f / kLift);
-#pragma unroll
-            for (int i = 0; i < D / 32; ++i) acc[m][i] *= shrink;
         }
+        float most = p[0][0];
 #pragma unroll
-        for (int i = 0; i < D / 32; ++i)
+        for (int t = 0; t < 2; ++t)
 #pragma unroll
-            for (int u = 0; u < 4; ++u) {
-                const f16x8 x = *reinterpret_cast<const f16x8 *>(v + (32 * i + column) * S::kValueStride + 16 * u + 8 * half);
+            for (int e = 0; e < 16; ++e) most = __builtin_fmaxf(most, p[t][e]);
+        most = halves_max(most);
+        const bool sees = !decltype(masked)::value || !(most == kNone);
+        most = __builtin_fmaxf(top, sees ? most * by : kNone);
+        const float from = most == kNone ? 0.0f : most;
+        float shrink = __builtin_amdgcn_exp2f(top - from);
+        top = most;
+        total *= shrink;
+        if (sees) {
+            shrink *= unit / scale_v;
+            unit = scale_v;
+        }
+        const float lifted_from = 15.0f - from;
+        float sum = 0.0f;
 #pragma unroll
-                for (int m = 0; m < kTiles; ++m) acc[m][i] = __builtin_amdgcn_mfma_f32_32x32x16_f16(x, lifted[m][u], acc[m][i], 0, 0, 0);
+        for (int t = 0; t < 2; ++t)
+#pragma unroll
+            for (int e = 0; e < 16; e += 2) {
+                f32x2 x;
+#pragma unroll
+                for (int i = 0; i < 2; ++i) {
+                    const float y = __builtin_amdgcn_exp2f(__builtin_fmaf(p[t][e + i], by, lifted_from));
+                    x[i] = decltype(masked)::value && p[t][e + i] == kNone ? 0.0f : y;
+                    sum += x[i];
+                }
+                const f16x2 h = __builtin_convertvector(x, f16x2);
+                lifted[2 * t + e / 8][e % 8] = h[0];
+                lifted[2 * t + e / 8][e % 8 + 1] = h[1];
             }
+        total += sum * (1.0f / kLift);
+#pragma unroll
+        for (int i = 0; i < D / 32; ++i) acc[i] *= shrink;
     };
 
-    if (begin < end) {
-        Staged<D> staged;
-        Page now = page_of(begin), next = now;
-        staged.fetch(now.codes);
-        staged.put_down(keys[0], values[0]);
-        if (begin + 1 < end) {
-            next = page_of(begin + 1);
-            staged.fetch(next.codes);
+    if (n > 0) {
+        const int later = wave >= 4 ? 1 : 0;
+        StagedKeys<D> next_keys;
+        StagedValues<D> next_values;
+        look_up(0);
+        next_keys.fetch(codes_of(0));
+        next_keys.put_down(keys[0]);
+        next_keys.fetch(codes_of(1));
+        next_values.fetch(codes_of(0));
+        auto stage = [&](int b) {                             // K(b + 1), V(b)
+            next_keys.put_down(keys[(b + 1) & 1]);
+            next_values.put_down(values[b & 1]);
+            next_keys.fetch(codes_of(b + 2));
+            next_values.fetch(codes_of(b + 1));
+        };
+        if (later) stage(0);
+        meet();
+        if (later) meet();
+        for (int b = 0; b < n; ++b) {
+            __builtin_amdgcn_s_setprio(1);
+            if (b > 0) products(values[(b - 1) & 1], keys[b & 1], std::false_type(), std::false_type());
+            else products(values[0], keys[0], std::true_type(), std::false_type());
+            __builtin_amdgcn_s_setprio(0);
+            meet();
+            if (b + 3 - base >= 64) look_up(b);
+            const float scale_k = scale_of(b, 0), scale_v = scale_of(b, 1);
+            const int block = begin + b;
+            if (block * kBlock >= full_low && block * kBlock + kBlock - 1 <= full_high) probabilities(block, scale_k, scale_v, std::false_type());
+            else probabilities(block, scale_k, scale_v, std::true_type());
+            stage(b + later);
+            if (!later || b + 1 < n) meet();
         }
-        for (int block = begin; block < end; ++block) {
-            const int b = (block - begin) & 1;
-            __syncthreads();                                  // block's numbers are in place, and the other buffer is free
-            if (block + 1 < end) staged.put_down(keys[b ^ 1], values[b ^ 1]);
-            Page after = next;
-            if (block + 2 < end) {
-                after = page_of(block + 2);
-                staged.fetch(after.codes);
-            }
-            if (block * kBlock >= full_low && block * kBlock + kBlock - 1 <= full_high) attend(block, now.scale_k, now.scale_v, keys[b], values[b], std::false_type());
-            else attend(block, now.scale_k, now.scale_v, keys[b], values[b], std::true_type());
-            now = next;
-            next = after;
-        }
+        products(values[(n - 1) & 1], keys[0], std::false_type(), std::true_type());
     }
 
+    Meeting sum;
+    sum.top = top;
+    const auto both = __builtin_amdgcn_permlane32_swap(as_u32(total), as_u32(total), false, false);
+    sum.total = as_float(both[0]) + as_float(both[1]);
+    if (r >= rows) return;
+    uint16_t *out = a.out.data + s * a.out.sequence + row.i * a.out.row + row.head * a.out.head + 4 * half;
+    const float by = unit * (1.0f / kLift) * sum.inverse();
 #pragma unroll
-    for (int m = 0; m < kTiles; ++m) {
-        const int r = r0 + (wave * kTiles + m) * 32 + column;
-        Meeting sum;
-        sum.top = top[m];
-        const auto both = __builtin_amdgcn_permlane32_swap(as_u32(total[m]), as_u32(total[m]), false, false);
-        sum.total = as_float(both[0]) + as_float(both[1]);
-        if (r >= rows) continue;
-        uint16_t *out = a.out.data + s * a.out.sequence + row[m].i * a.out.row + row[m].head * a.out.head + 4 * half;
-        const float by = unit[m] * (1.0f / kLift) * sum.inverse();
+    for (int i = 0; i < D / 32; ++i)
 #pragma unroll
-        for (int i = 0; i < D / 32; ++i)
+        for (int e = 0; e < 16; e += 4) {
+            uint16_t v[4];
 #pragma unroll
-            for (int e = 0; e < 16; e += 4) {
-                uint16_t v[4];
-#pragma unroll
-                for (int x = 0; x < 4; ++x) v[x] = narrow<BF16>(acc[m][i][e + x] * by);
-                *reinterpret_cast<u32x2 *>(out + 32 * i + 2 * e) = u32x2{v[0] | (uint32_t)v[1] << 16, v[2] | (uint32_t)v[3] << 16};
-            }
-        if (a.lse && half == 0) a.lse[((size_t)s * a.rows + row[m].i) * a.q_heads + row[m].head] = sum.lse();
-    }
+            for (int x = 0; x < 4; ++x) v[x] = narrow<BF16>(acc[i][e + x] * by);
+            *reinterpret_cast<u32x2 *>(out + 32 * i + 2 * e) = u32x2{v[0] | (uint32_t)v[1] << 16, v[2] | (uint32_t)v[3] << 16};
+        }
+    if (a.lse && half == 0) a.lse[((size_t)s * a.rows + row.i) * a.q_heads + row.head] = sum.lse();
 }
 
 }  // namespace
@@ -268,7 +296,7 @@ void launch_prompt(const spqt_kv_cache &cache, const Call &a, hipStream_t stream
     dispatch(cache, [&](auto dim, auto bf16) {
         constexpr int D = decltype(dim)::value;
         const int tiles = (a.rows * a.group + Shape<D>::kRows - 1) / Shape<D>::kRows;
-        hipLaunchKernelGGL((spqt_kv_prompt_kernel<D, decltype(bf16)::value>), dim3((unsigned)tiles * cache.kv_heads, 1, cache.sequences), dim3(kThreads), 0, stream,
+        hipLaunchKernelGGL((spqt_kv_prompt_kernel<D, decltype(bf16)::value>), dim3((unsigned)tiles * cache.kv_heads, 1, cache.sequences), dim3(Shape<D>::kThreads), 0, stream,
                            view(cache), a, tiles);
     });
 }
