@@ -87,7 +87,7 @@ int spqt_kv_workspace_bytes(int sequences, int rows, int q_heads, int kv_heads, 
  *   weights = decay * weights + sum over the call's rows and the heads that read its kv head of its probability
  * (decay 0 does not read them).
  * workspace: workspace_bytes >= spqt_kv_workspace_bytes, 256-byte aligned, prepared once with spqt_workspace_init;
- * every call leaves it as it found it, so calls on one stream may share one. */
+ * every call leaves what the next one relies on, so calls on one stream may share one, whatever their shapes. */
 int spqt_kv_attention(const spqt_kv_cache *cache, const spqt_kv_rows *q, const spqt_kv_rows *out, float *lse, int rows, const int32_t *counts,
                       int q_heads, float scale, int window, float decay, void *workspace, size_t workspace_bytes, void *stream);
 

@@ -60,9 +60,9 @@ __device__ __forceinline__ f32x4 scores_of(const u32x4 (&k)[D / 64], const f16x8
     return s;
 }
 
-// Where the sums of rows meet: counters of what has come, one for every 16 rows of a kv head and sequence, and two places for each workgroup.
+// Where the sums of rows meet: two places for each workgroup, and a counter of what has come for the one unit that begins in it and goes on in others.
 struct Space {
-    uint32_t *arrived;
+    uint32_t *arrived;   // [kShares], all 0 between calls
     float *stats;        // [2 * kShares][16][2]: the rows' maxima and sums
     float *sums;         // [2 * kShares][16][D]
 };
@@ -434,7 +434,7 @@ __global__ __launch_bounds__(step_threads(D)) void spqt_kv_step_kernel(Cache c, 
     // A device-scope store has reached every XCD when it is acknowledged; the counters are raised after all threads' stores are.
     asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
     __syncthreads();
-    auto counter_of = [&](const Place &u) { return space.arrived + (size_t)u.s * units_each + u.unit; };
+    auto counter_of = [&](const Place &u) { return space.arrived + share_of(u.start); };
     if (threadIdx.x == 0) {
         if (first_meets) order[0] = __hip_atomic_fetch_add(counter_of(group_first), 1u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
         if (last_meets) order[1] = __hip_atomic_fetch_add(counter_of(group_last), 1u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
@@ -527,8 +527,6 @@ __global__ __launch_bounds__(kThreads) void spqt_kv_weigh_kernel(Cache c, Call a
         }
 }
 
-size_t counter_bytes(int64_t units) { return ((size_t)units * 4 + 255) / 256 * 256; }
-
 }  // namespace
 
 extern "C" int spqt_kv_workspace_bytes(int sequences, int rows, int q_heads, int kv_heads, int head_dim, int max_blocks, size_t *out_bytes) {
@@ -536,9 +534,12 @@ extern "C" int spqt_kv_workspace_bytes(int sequences, int rows, int q_heads, int
     if (sequences < 1 || sequences > 65535 || rows < 1 || rows > kMaxRows || kv_heads < 1 || kv_heads > 16384 || q_heads < kv_heads || q_heads % kv_heads != 0 ||
         head_dim < 64 || head_dim > SPQT_KV_MAX_DIM || head_dim % 64 != 0 || max_blocks < 1 || max_blocks > 1 << 24)
         return SPQT_ESHAPE;
-    const int64_t tiles = ((int64_t)rows * (q_heads / kv_heads) + 15) / 16, units = (int64_t)sequences * kv_heads * tiles;
-    if (units * max_blocks > 0x7FFFFFFF) return SPQT_ESHAPE;
-    *out_bytes = kWorkspaceHead + counter_bytes(units) + 2 * kShares * 16 * (size_t)(head_dim + 2) * 4;
+    const int group = q_heads / kv_heads;
+    if ((int64_t)rows * group > 1 << 28) return SPQT_ESHAPE;
+    // the step kernel's places and, where a call may be of that kind, the prompt kernel's, one or the other
+    size_t bytes = 2 * kShares * 16 * (size_t)(head_dim + 2) * 4;
+    if (is_prompt(rows, group) && prompt_bytes(head_dim) > bytes) bytes = prompt_bytes(head_dim);
+    *out_bytes = kWorkspaceHead + kShares * 4 + bytes;
     return SPQT_OK;
 }
 
@@ -555,18 +556,17 @@ extern "C" int spqt_kv_attention(const spqt_kv_cache *cache, const spqt_kv_rows 
     if ((uintptr_t)lse % 4 != 0 || (uintptr_t)counts % 4 != 0 || (uintptr_t)workspace % 256 != 0) return SPQT_EALIGN;
     if (workspace_bytes < need) return SPQT_ESIZE;
     const Call a = {view(*q), view(*out), lse, counts, rows, q_heads, q_heads / cache->kv_heads, window, scale, decay};
-    if ((int64_t)rows * a.group > 1 << 28) return SPQT_ESHAPE;
     const int tiles = (rows * a.group + 15) / 16;
-    const int64_t units = (int64_t)cache->sequences * cache->kv_heads * tiles;
-    char *at = (char *)workspace + kWorkspaceHead;
+    const bool prompt = is_prompt(rows, a.group);
+    if (!prompt && (int64_t)cache->sequences * cache->kv_heads * tiles * cache->max_blocks > 0x7FFFFFFF) return SPQT_ESHAPE;
     Space space;
-    space.arrived = (uint32_t *)at;
-    space.stats = (float *)(at + counter_bytes(units));
+    space.arrived = (uint32_t *)((char *)workspace + kWorkspaceHead);
+    space.stats = (float *)(space.arrived + kShares);
     space.sums = space.stats + 2 * kShares * 32;
     dispatch(*cache, [&](auto dim, auto bf16) {
         constexpr int D = decltype(dim)::value;
         constexpr bool B = decltype(bf16)::value;
-        if (is_prompt(a, D)) launch_prompt(*cache, a, (hipStream_t)stream);
+        if (prompt) launch_prompt(*cache, a, space.stats, (hipStream_t)stream);
         else hipLaunchKernelGGL((spqt_kv_step_kernel<D, B>), dim3(kShares), dim3(step_threads(D)), 0, (hipStream_t)stream, view(*cache), a, space, cache->sequences, tiles);
         if (cache->weights)
             hipLaunchKernelGGL((spqt_kv_weigh_kernel<D, B>), dim3((cache->max_blocks + kWaves - 1) / kWaves, cache->kv_heads, cache->sequences), dim3(kThreads), 0,

@@ -82,9 +82,10 @@ __device__ __forceinline__ float queries_f16(const u32x4 (&w)[N], f16x8 (&q)[N],
     return down;
 }
 
-// Many rows (kv_prompt.hip); true where it is for this call.
-bool is_prompt(const Call &a, int head_dim);
-void launch_prompt(const spqt_kv_cache &cache, const Call &a, hipStream_t stream);
+// Many rows (kv_prompt.hip): whether a call is of that kind, what such calls need of the workspace at most, and the call.
+bool is_prompt(int rows, int group);
+size_t prompt_bytes(int dim);
+void launch_prompt(const spqt_kv_cache &cache, const Call &a, void *space, hipStream_t stream);
 
 }  // namespace kv
 }  // namespace spqt

@@ -78,6 +78,13 @@ __device__ __forceinline__ float halves_max(float v) {
     return __builtin_fmaxf(as_float(r[0]), as_float(r[1]));
 }
 
+// Where the tokens are divided into parts: what each of them makes of a row, in units of 2^(its maximum).
+struct Parts {
+    int n;
+    float *sums;         // [sequence][kv head][256 (128) rows][part][row][D]
+    float *stats;        // the same of [2]: a row's maximum and sum
+};
+
 // Waits for the workgroup's shared memory, not for what is on its way from global memory.
 __device__ __forceinline__ void meet() {
     __builtin_amdgcn_fence(__ATOMIC_RELEASE, "workgroup", "local");
@@ -92,7 +99,7 @@ __device__ __forceinline__ void meet() {
 //   first four  O += V P(b-1), S = K(b) Q       P(b), K(b+1), V(b)
 //   others      P(b-1), K(b+1), V(b)            O += V P(b-1), S = K(b) Q
 template <int D, bool BF16>
-__global__ __launch_bounds__(Shape<D>::kThreads) void spqt_kv_prompt_kernel(Cache c, Call a, int tiles) {
+__global__ __launch_bounds__(Shape<D>::kThreads) void spqt_kv_prompt_kernel(Cache c, Call a, int tiles, Parts parts) {
     typedef Shape<D> S;
     __shared__ __attribute__((aligned(16))) _Float16 keys[2][kBlock * S::kKeyStride];
     __shared__ __attribute__((aligned(16))) _Float16 values[2][D * S::kValueStride];
@@ -107,7 +114,10 @@ __global__ __launch_bounds__(Shape<D>::kThreads) void spqt_kv_prompt_kernel(Cach
     const int last_live = r0 + S::kRows < count * a.group ? r0 + S::kRows - 1 : count * a.group - 1;
     const Row last = row_of(a, last_live < 0 ? 0 : last_live, head, length, count);
     const bool any = last_live >= r0 && last.high >= 0;
-    const int begin = any ? block_of(first.high >= 0 ? first.low : 0) : 0, n = any ? block_of(last.high) + 1 - begin : 0;
+    const int whole_begin = any ? block_of(first.high >= 0 ? first.low : 0) : 0, whole = any ? block_of(last.high) + 1 - whole_begin : 0;
+    // this workgroup's part of them
+    const int from_block = (int)((int64_t)whole * blockIdx.y / parts.n), begin = whole_begin + from_block;
+    const int n = (int)((int64_t)whole * (blockIdx.y + 1) / parts.n) - from_block;
 
     const int r = r0 + wave * 32 + column;
     Row row = row_of(a, r, head, length, count);
@@ -270,6 +280,17 @@ __global__ __launch_bounds__(Shape<D>::kThreads) void spqt_kv_prompt_kernel(Cach
     sum.top = top;
     const auto both = __builtin_amdgcn_permlane32_swap(as_u32(total), as_u32(total), false, false);
     sum.total = as_float(both[0]) + as_float(both[1]);
+    if (parts.n > 1) {
+        const size_t slot = ((((size_t)s * c.kv_heads + head) * tiles + tile) * parts.n + blockIdx.y) * S::kRows + wave * 32 + column;
+        const float by = unit * (1.0f / kLift);
+#pragma unroll
+        for (int i = 0; i < D / 32; ++i)
+#pragma unroll
+            for (int e = 0; e < 16; e += 4)
+                *reinterpret_cast<f32x4 *>(parts.sums + slot * D + 32 * i + 2 * e + 4 * half) = f32x4{acc[i][e], acc[i][e + 1], acc[i][e + 2], acc[i][e + 3]} * by;
+        if (half == 0) *reinterpret_cast<f32x2 *>(parts.stats + slot * 2) = f32x2{sum.top, sum.total};
+        return;
+    }
     if (r >= rows) return;
     uint16_t *out = a.out.data + s * a.out.sequence + row.i * a.out.row + row.head * a.out.head + 4 * half;
     const float by = unit * (1.0f / kLift) * sum.inverse();
@@ -285,19 +306,68 @@ __global__ __launch_bounds__(Shape<D>::kThreads) void spqt_kv_prompt_kernel(Cach
     if (a.lse && half == 0) a.lse[((size_t)s * a.rows + row.i) * a.q_heads + row.head] = sum.lse();
 }
 
+// The parts' sums of a row to its output, eight rows a workgroup.
+template <int D, bool BF16>
+__global__ __launch_bounds__(256) void spqt_kv_parts_kernel(Call a, int kv_heads, int tiles, Parts parts) {
+    constexpr int kEach = D / 32;
+    const int s = blockIdx.z, head = blockIdx.y, r = blockIdx.x * 8 + threadIdx.x / 32, d = threadIdx.x % 32 * kEach;
+    if (r >= a.rows * a.group) return;
+    const size_t slot = (((size_t)s * kv_heads + head) * tiles + r / Shape<D>::kRows) * parts.n * Shape<D>::kRows + r % Shape<D>::kRows;
+    Meeting m;
+    float x[kEach];
+#pragma unroll
+    for (int i = 0; i < kEach; ++i) x[i] = 0.0f;
+#pragma unroll 4
+    for (int part = 0; part < parts.n; ++part) {
+        const size_t at = slot + (size_t)part * Shape<D>::kRows;
+        const f32x2 stat = *reinterpret_cast<const f32x2 *>(parts.stats + at * 2);
+        float mine, others;
+        m.add(stat.x, stat.y, mine, others);
+#pragma unroll
+        for (int i = 0; i < kEach; ++i) x[i] = x[i] * mine + parts.sums[at * D + d + i] * others;
+    }
+    const int i = r / a.group, q_head = head * a.group + r % a.group;
+    uint16_t *out = a.out.data + s * a.out.sequence + i * a.out.row + q_head * a.out.head + d;
+    const float by = m.inverse();
+#pragma unroll
+    for (int e = 0; e < kEach; e += 2) *reinterpret_cast<uint32_t *>(out + e) = narrow<BF16>(x[e] * by) | (uint32_t)narrow<BF16>(x[e + 1] * by) << 16;
+    if (a.lse && threadIdx.x % 32 == 0) a.lse[((size_t)s * a.rows + i) * a.q_heads + q_head] = m.lse();
+}
+
+constexpr int kParted = 256;                              // workgroups of a launch whose tokens are divided, at most
+// Parts that the tokens are divided into, where the rows alone would not fill the chip: as many as leave one workgroup per CU, of at least eight
+// blocks each for a sequence that fills its table.
+int parts_of(int64_t units, int max_blocks) {
+    int64_t n = kParted / units;
+    if (n > max_blocks / 8) n = max_blocks / 8;
+    return n < 1 ? 1 : (n > 64 ? 64 : (int)n);
+}
+int rows_of(int dim) { return dim > 128 ? Shape<256>::kRows : Shape<128>::kRows; }
+
 }  // namespace
 
 namespace spqt {
 namespace kv {
 
-bool is_prompt(const Call &a, int) { return a.rows * a.group > 64; }
+bool is_prompt(int rows, int group) { return (int64_t)rows * group > 64; }
 
-void launch_prompt(const spqt_kv_cache &cache, const Call &a, hipStream_t stream) {
+size_t prompt_bytes(int dim) { return (size_t)kParted * rows_of(dim) * (dim + 2) * 4; }
+
+void launch_prompt(const spqt_kv_cache &cache, const Call &a, void *space, hipStream_t stream) {
     dispatch(cache, [&](auto dim, auto bf16) {
         constexpr int D = decltype(dim)::value;
+        constexpr bool B = decltype(bf16)::value;
         const int tiles = (a.rows * a.group + Shape<D>::kRows - 1) / Shape<D>::kRows;
-        hipLaunchKernelGGL((spqt_kv_prompt_kernel<D, decltype(bf16)::value>), dim3((unsigned)tiles * cache.kv_heads, 1, cache.sequences), dim3(Shape<D>::kThreads), 0, stream,
-                           view(cache), a, tiles);
+        const int64_t units = (int64_t)tiles * cache.kv_heads * cache.sequences;
+        Parts parts;
+        parts.n = parts_of(units, cache.max_blocks);
+        parts.sums = (float *)space;
+        parts.stats = parts.sums + (size_t)units * parts.n * Shape<D>::kRows * D;
+        hipLaunchKernelGGL((spqt_kv_prompt_kernel<D, B>), dim3((unsigned)tiles * cache.kv_heads, parts.n, cache.sequences), dim3(Shape<D>::kThreads), 0, stream,
+                           view(cache), a, tiles, parts);
+        if (parts.n > 1)
+            hipLaunchKernelGGL((spqt_kv_parts_kernel<D, B>), dim3((a.rows * a.group + 7) / 8, cache.kv_heads, cache.sequences), dim3(256), 0, stream, a, cache.kv_heads,
+                               tiles, parts);
     });
 }
 

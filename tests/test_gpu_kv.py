@@ -307,6 +307,10 @@ CASES = [
     (2, 1, 192, "float16", [513, 0, 190], [200, 0, 190], 200, 0),
     (3, 3, 128, "bfloat16", [5, 700], [5, 1], 30, 1),
     (8, 2, 64, "float16", [40], None, 60, 0),          # rows before the first token see nothing
+    (8, 1, 128, "float16", [2100], None, 40, 0),       # many rows, tokens in parts
+    (4, 2, 64, "bfloat16", [1500, 30, 0, 800], [50, 30, 0, 1], 50, 300),
+    (6, 1, 192, "bfloat16", [1100, 1030], [33, 20], 33, 0),
+    (4, 1, 256, "float16", [1300], None, 70, 0),
 ]
 
 
@@ -572,6 +576,19 @@ def test_another_stream_and_a_shared_workspace(gpu):
             side.synchronize()
             for x, y in zip(want, got):
                 assert x[0].equal(y[0]) and x[1].equal(y[1])
+
+
+def test_one_workspace_for_calls_of_all_shapes(gpu):
+    """Counters lie where every shape looks for them, and partial sums of one call are not in the way of the next."""
+    torch, spqt = gpu
+    cases = [CASES[i] for i in (7, 18, 3, 19, 8, 21, 9, 11)]
+    made = [case_cache(gpu, case, 82) for case in cases]
+    ws = max((spqt.new_kv_workspace(4, 4096, 64, 1, dim, 64) for dim in (64, 128, 192, 256)), key=lambda w: w.numel())
+    for _ in range(2):
+        for case, (c, q) in zip(cases, made):
+            want = attend(gpu, c, q, case[5], case[7])
+            got = attend(gpu, c, q, case[5], case[7], workspace=ws)
+            assert want[0].equal(got[0]) and want[1].equal(got[1])
 
 
 def test_refusals(gpu):
