@@ -15,10 +15,12 @@
 #include <c10/hip/HIPStream.h>
 #include <torch/csrc/autograd/python_variable.h>
 
+#include <cmath>
 #include <cstdint>
 
 #include "spqt.h"
 #include "spqt_colblock.h"
+#include "spqt_kv.h"
 
 namespace {
 
@@ -248,9 +250,116 @@ PyObject *cb_gemv_fused(PyObject *, PyObject *const *a, Py_ssize_t n) {
     });
 }
 
+// The key/value cache (kv.py). A cache's tensors: on one GPU, dense, of the shapes that the codes and the table ask for.
+struct KvTensors {
+    spqt_kv_cache c;
+    c10::Device device;
+};
+const at::Tensor &kv_tensor(PyObject *o, at::ScalarType type, c10::Device device, c10::IntArrayRef shape) {
+    const at::Tensor &t = tensor(o, type);
+    if (t.device() != device || t.sizes() != shape) throw NotPlain();
+    return t;
+}
+KvTensors kv_cache(PyObject *codes, PyObject *scales, PyObject *table, PyObject *lengths, PyObject *tail, PyObject *weights, at::ScalarType type) {
+    const at::Tensor &k = tensor(codes, at::kByte), &b = tensor(table, at::kInt);
+    if (type != at::kHalf && type != at::kBFloat16) throw NotPlain();
+    if (k.dim() != 5 || k.size(2) != 2 || k.size(3) != SPQT_KV_BLOCK || b.dim() != 2 || b.device() != k.device()) throw NotPlain();
+    const int64_t pages = k.size(0), heads = k.size(1), dim = k.size(4), sequences = b.size(0), blocks = b.size(1);
+    if (heads > 1 << 20 || dim > 1 << 20 || sequences > 1 << 20 || blocks > 1 << 30) throw NotPlain();
+    KvTensors r = {{}, k.device()};
+    r.c.codes = k.data_ptr();
+    r.c.scales = (float *)kv_tensor(scales, at::kFloat, r.device, {pages, heads, 2}).data_ptr();
+    r.c.tail = tail == Py_None ? nullptr : kv_tensor(tail, type, r.device, {sequences, heads, 2, SPQT_KV_BLOCK, dim}).data_ptr();
+    r.c.weights = weights == Py_None ? nullptr : (float *)kv_tensor(weights, at::kFloat, r.device, {pages, heads, SPQT_KV_BLOCK}).data_ptr();
+    r.c.table = (const int32_t *)b.data_ptr();
+    r.c.lengths = (const int32_t *)kv_tensor(lengths, at::kInt, r.device, {sequences}).data_ptr();
+    r.c.pages = pages;
+    r.c.sequences = (int)sequences;
+    r.c.max_blocks = (int)blocks;
+    r.c.kv_heads = (int)heads;
+    r.c.head_dim = (int)dim;
+    r.c.type = type == at::kBFloat16 ? SPQT_KV_BF16 : SPQT_KV_FP16;
+    return r;
+}
+// A 16-bit tensor whose last dimension is dense; heads 0: any number of them.
+struct KvRows {
+    spqt_kv_rows r;
+    int64_t rows, heads;
+};
+at::ScalarType kv_type(PyObject *o) {
+    if (!THPVariable_CheckExact(o) || !THPVariable_Unpack(o).defined()) throw NotPlain();
+    return THPVariable_Unpack(o).scalar_type();
+}
+KvRows kv_rows(PyObject *o, at::ScalarType type, const KvTensors &k, int64_t heads) {
+    if (!THPVariable_CheckExact(o)) throw NotPlain();
+    const at::Tensor &t = THPVariable_Unpack(o);
+    const c10::TensorImpl *impl = t.unsafeGetTensorImpl();
+    if (!t.defined() || impl->is_python_dispatch() || !impl->has_storage() || t.layout() != at::kStrided || !t.is_cuda() || t.scalar_type() != type ||
+        t.device() != k.device || t.dim() != 4)
+        throw NotPlain();
+    if (t.size(0) != k.c.sequences || t.size(3) != k.c.head_dim || t.stride(3) != 1 || (heads && t.size(2) != heads)) throw NotPlain();
+    if (t.size(1) > 1 << 30 || t.size(2) > 1 << 30) throw NotPlain();
+    auto stride = [&](int d) { return t.size(d) > 1 ? t.stride(d) : 0; };
+    return {{t.data_ptr(), stride(0), stride(1), stride(2)}, t.size(1), t.size(2)};
+}
+const int32_t *kv_counts(PyObject *o, const KvTensors &k) {
+    return o == Py_None ? nullptr : (const int32_t *)kv_tensor(o, at::kInt, k.device, {k.c.sequences}).data_ptr();
+}
+// kv_append(function, codes, scales, tail, table, lengths, k, v, counts, weights, stream)
+PyObject *kv_append(PyObject *, PyObject *const *a, Py_ssize_t n) {
+    return guarded(n, 11, [&]() {
+        const at::ScalarType type = kv_type(a[6]);
+        if (a[3] == Py_None) throw NotPlain();
+        const KvTensors c = kv_cache(a[1], a[2], a[4], a[5], a[3], a[9], type);
+        const KvRows k = kv_rows(a[6], type, c, c.c.kv_heads), v = kv_rows(a[7], type, c, c.c.kv_heads);
+        if (k.rows != v.rows) throw NotPlain();
+        return call(function<decltype(&spqt_kv_append)>(a[0]), &c.c, &k.r, &v.r, (int)k.rows, kv_counts(a[8], c), current_stream(a[10]));
+    });
+}
+// kv_read(function, codes, scales, table, lengths, k_out, v_out, counts, stream)
+PyObject *kv_read(PyObject *, PyObject *const *a, Py_ssize_t n) {
+    return guarded(n, 9, [&]() {
+        const at::ScalarType type = kv_type(a[5]);
+        const KvTensors c = kv_cache(a[1], a[2], a[3], a[4], Py_None, Py_None, type);
+        const KvRows k = kv_rows(a[5], type, c, c.c.kv_heads), v = kv_rows(a[6], type, c, c.c.kv_heads);
+        if (k.rows != v.rows) throw NotPlain();
+        return call(function<decltype(&spqt_kv_read)>(a[0]), &c.c, &k.r, &v.r, (int)k.rows, kv_counts(a[7], c), current_stream(a[8]));
+    });
+}
+// kv_attention(function, codes, scales, table, lengths, q, out, workspace, scale, counts, window, lse, weights, decay, stream)
+PyObject *kv_attention(PyObject *, PyObject *const *a, Py_ssize_t n) {
+    return guarded(n, 15, [&]() {
+        const at::ScalarType type = kv_type(a[5]);
+        const KvTensors c = kv_cache(a[1], a[2], a[3], a[4], Py_None, a[12], type);
+        const KvRows q = kv_rows(a[5], type, c, 0), out = kv_rows(a[6], type, c, q.heads);
+        if (q.rows != out.rows || a[7] == Py_None) throw NotPlain();
+        float *lse = a[11] == Py_None ? nullptr : (float *)kv_tensor(a[11], at::kFloat, c.device, {c.c.sequences, q.rows, q.heads}).data_ptr();
+        const at::Tensor &space = tensor(a[7], at::kByte);
+        if (space.device() != c.device || space.dim() != 1) throw NotPlain();
+        const float scale = a[8] == Py_None ? (float)std::pow((double)c.c.head_dim, -0.5) : threshold(a[8]);
+        return call(function<decltype(&spqt_kv_attention)>(a[0]), &c.c, &q.r, &out.r, lse, (int)q.rows, kv_counts(a[9], c), (int)q.heads, scale,
+                    small(a[10]), threshold(a[13]), space.data_ptr(), (size_t)space.numel(), current_stream(a[14]));
+    });
+}
+// kv_evict(function, codes, scales, tail, weights, table, lengths, keep, recent, new_table, new_lengths, kept, stream)
+PyObject *kv_evict(PyObject *, PyObject *const *a, Py_ssize_t n) {
+    return guarded(n, 13, [&]() {
+        if (a[3] == Py_None || a[4] == Py_None) throw NotPlain();
+        const KvTensors c = kv_cache(a[1], a[2], a[5], a[6], a[3], a[4], kv_type(a[3]));
+        const int keep = small(a[7]), recent = small(a[8]);
+        const at::Tensor &table = tensor(a[9], at::kInt);
+        if (table.device() != c.device || table.dim() != 2 || table.size(0) != c.c.sequences || table.size(1) > 1 << 30) throw NotPlain();
+        int32_t *lengths = (int32_t *)kv_tensor(a[10], at::kInt, c.device, {c.c.sequences}).data_ptr();
+        int32_t *kept = (int32_t *)kv_tensor(a[11], at::kInt, c.device, {c.c.sequences, c.c.kv_heads, keep}).data_ptr();
+        return call(function<decltype(&spqt_kv_evict)>(a[0]), &c.c, keep, recent, (const int32_t *)table.data_ptr(), (int)table.size(1), lengths, kept,
+                    current_stream(a[12]));
+    });
+}
+
 #define SPQT_METHOD(name) {#name, (PyCFunction)(void (*)(void))name, METH_FASTCALL, nullptr}
 PyMethodDef methods[] = {SPQT_METHOD(gather),  SPQT_METHOD(gather_rows), SPQT_METHOD(gemv),         SPQT_METHOD(gemv_fused), SPQT_METHOD(gemv_fused_rows),
-                         SPQT_METHOD(cb_gemv), SPQT_METHOD(cb_gemv_one), SPQT_METHOD(cb_gemv_fused), {nullptr, nullptr, 0, nullptr}};
+                         SPQT_METHOD(cb_gemv), SPQT_METHOD(cb_gemv_one), SPQT_METHOD(cb_gemv_fused),
+                         SPQT_METHOD(kv_append), SPQT_METHOD(kv_read), SPQT_METHOD(kv_attention), SPQT_METHOD(kv_evict), {nullptr, nullptr, 0, nullptr}};
 PyModuleDef module = {PyModuleDef_HEAD_INIT, "_fastcall", "Device calls of binding.py without the interpreter.", -1, methods, nullptr, nullptr, nullptr, nullptr};
 
 }  // namespace

@@ -16,10 +16,9 @@ from __future__ import annotations
 import ctypes
 
 from . import binding as _b
-from .binding import SpqtError, _check, lib
+from .binding import KV_EXPORTS, SpqtError, _check, lib  # noqa: F401
 
 KV_BLOCK = 64
-KV_EXPORTS = ["spqt_kv_append", "spqt_kv_read", "spqt_kv_workspace_bytes", "spqt_kv_attention", "spqt_kv_evict"]
 
 
 class KvCacheView(ctypes.Structure):
@@ -95,6 +94,10 @@ def new_kv_cache(pages: int, kv_heads: int, head_dim: int, sequences: int, dtype
 
 def spqt_kv_append(codes, scales, tail, table, lengths, k, v, counts=None, weights=None, stream=None) -> None:
     """Quantizes k and v [sequences, rows, kv_heads, head_dim] into the cache as the last counts[s] of lengths[s] tokens."""
+    if _b._fast is not None:
+        rc = _b._fast.kv_append((_b._lib or lib()).at["spqt_kv_append"], codes, scales, tail, table, lengths, k, v, counts, weights, stream)
+        if rc is not None:
+            return _check(rc)
     dtype = _dtype_of(k, "k")
     cache = _cache(codes, scales, table, lengths, dtype, tail, weights)
     shape = (cache.sequences, None, cache.kv_heads, cache.head_dim)
@@ -105,6 +108,10 @@ def spqt_kv_append(codes, scales, tail, table, lengths, k, v, counts=None, weigh
 
 def spqt_kv_read(codes, scales, table, lengths, k_out, v_out, counts=None, stream=None) -> None:
     """The last counts[s] tokens of every sequence as 16-bit values, into k_out and v_out [sequences, rows, kv_heads, head_dim]; other rows are set to 0."""
+    if _b._fast is not None:
+        rc = _b._fast.kv_read((_b._lib or lib()).at["spqt_kv_read"], codes, scales, table, lengths, k_out, v_out, counts, stream)
+        if rc is not None:
+            return _check(rc)
     dtype = _dtype_of(k_out, "k_out")
     cache = _cache(codes, scales, table, lengths, dtype)
     shape = (cache.sequences, None, cache.kv_heads, cache.head_dim)
@@ -133,6 +140,10 @@ def spqt_kv_attention(codes, scales, table, lengths, q, out, workspace, scale=No
     lengths[s] - counts[s] + i and sees those up to itself, the last `window` of them if window > 0.  scale None: 1 / sqrt(head_dim).
     lse: float32 [sequences, rows, q_heads] or None.  weights (with lse): weights = decay * weights + the probabilities that every
     cached token got in this call."""
+    if _b._fast is not None:
+        rc = _b._fast.kv_attention((_b._lib or lib()).at["spqt_kv_attention"], codes, scales, table, lengths, q, out, workspace, scale, counts, window, lse, weights, decay, stream)
+        if rc is not None:
+            return _check(rc)
     dtype = _dtype_of(q, "q")
     cache = _cache(codes, scales, table, lengths, dtype, None, weights)
     device = codes.device
@@ -149,6 +160,10 @@ def spqt_kv_attention(codes, scales, table, lengths, q, out, workspace, scale=No
 def spqt_kv_evict(codes, scales, tail, weights, table, lengths, keep: int, recent: int, new_table, new_lengths, kept, stream=None) -> None:
     """Cuts every sequence down to `keep` tokens per kv head, the last `recent` ones and the heaviest others, and moves them to the pages
     of new_table int32 [sequences, new_blocks].  new_lengths int32 [sequences] and kept int32 [sequences, kv_heads, keep] are written."""
+    if _b._fast is not None:
+        rc = _b._fast.kv_evict((_b._lib or lib()).at["spqt_kv_evict"], codes, scales, tail, weights, table, lengths, keep, recent, new_table, new_lengths, kept, stream)
+        if rc is not None:
+            return _check(rc)
     torch = _b._torch or _b._load_torch()
     cache = _cache(codes, scales, table, lengths, _dtype_of(tail, "tail"), tail, weights)
     device = codes.device

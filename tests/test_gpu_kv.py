@@ -591,8 +591,42 @@ def test_one_workspace_for_calls_of_all_shapes(gpu):
             assert want[0].equal(got[0]) and want[1].equal(got[1])
 
 
-def test_refusals(gpu):
+def test_through_the_extension_module_and_without_it(gpu, monkeypatch):
+    """The same results bit for bit, also on a stream that torch has made current."""
     torch, spqt = gpu
+    from paper_2511_04477_amd import binding
+    assert binding._fast is not None
+    side = torch.cuda.Stream()
+    results = []
+    for fast, stream in ((True, torch.cuda.current_stream()), (False, torch.cuda.current_stream()), (True, side), (False, side)):
+        with monkeypatch.context() as m:
+            if not fast:
+                m.setattr(binding, "_fast", None)
+            stream.wait_stream(torch.cuda.current_stream())
+            with torch.cuda.stream(stream):
+                c = Cache(gpu, 2, 2, 64, torch.bfloat16, 8, 90)
+                c.codes.fill_(128)                     # the pool's bytes that no token writes
+                c.append(200, [200, 90])
+                q = torch.randn((2, 3, 4, 64), generator=c.gen).bfloat16().cuda()
+                out, lse = attend(gpu, c, q, None, window=150, weigh=True, decay=0.5)
+                new_lengths = torch.zeros(2, dtype=torch.int32, device="cuda")
+                kept = torch.zeros((2, 2, 100), dtype=torch.int32, device="cuda")
+                spqt.spqt_kv_evict(c.codes, c.scales, c.tail, c.weights, c.table[:, :4].contiguous(), c.lengths, 100, 20, c.table[:, 4:].contiguous(), new_lengths, kept)
+                k, v = (torch.zeros((2, 100, 2, 64), dtype=torch.bfloat16, device="cuda") for _ in range(2))
+                spqt.spqt_kv_read(c.codes, c.scales, c.table[:, 4:].contiguous(), new_lengths, k, v, counts=new_lengths)
+                results.append((out, lse, kept, k, v, c.weights))
+            stream.synchronize()
+    for other in results[1:]:
+        for a, b in zip(results[0], other):
+            assert a.equal(b)
+
+
+@pytest.mark.parametrize("fast", [True, False])
+def test_refusals(gpu, fast, monkeypatch):
+    torch, spqt = gpu
+    if not fast:
+        from paper_2511_04477_amd import binding
+        monkeypatch.setattr(binding, "_fast", None)
     c, q = case_cache(gpu, CASES[2], 90)
     ws = spqt.new_kv_workspace(3, 1, 8, 2, 128, 4)
     out = torch.zeros(q.shape, dtype=q.dtype, device="cuda")
