@@ -82,6 +82,58 @@ __device__ __forceinline__ float queries_f16(const u32x4 (&w)[N], f16x8 (&q)[N],
     return down;
 }
 
+
+// 16 rows at a time: S^T = K Q^T, so that a lane of v_mfma_f32_16x16x32_f16 has ONE row of Q and four tokens of each 16.
+
+__device__ __forceinline__ int lanes_max(int v) {            // over the 16 rows
+#pragma unroll
+    for (int step = 1; step < 16; step *= 2) {
+        const int o = __shfl_xor(v, step);
+        v = o > v ? o : v;
+    }
+    return v;
+}
+__device__ __forceinline__ float columns_max(float v) {      // over the four lanes of a row
+    v = __builtin_fmaxf(v, __shfl_xor(v, 16));
+    return __builtin_fmaxf(v, __shfl_xor(v, 32));
+}
+__device__ __forceinline__ float columns_sum(float v) {
+    v += __shfl_xor(v, 16);
+    return v + __shfl_xor(v, 32);
+}
+
+// A row of Q as an operand, 32 elements a step: step j of a lane are elements 64 (j / 2) + 16 (lane / 16) + 8 (j % 2) on, as in load_keys; queries_f16 makes it fp16.
+template <int D>
+__device__ __forceinline__ void load_queries(u32x4 (&w)[D / 32], const uint16_t *row, bool live, int lane) {
+#pragma unroll
+    for (int j = 0; j < D / 32; ++j)
+        w[j] = live ? *reinterpret_cast<const u32x4 *>(row + 64 * (j / 2) + 16 * (lane / 16) + 8 * (j % 2)) : u32x4{0u, 0u, 0u, 0u};
+}
+
+// 16 tokens' keys as an operand.
+template <int D>
+__device__ __forceinline__ void load_keys(u32x4 (&k)[D / 64], const uint8_t *page, int tile, int lane) {
+#pragma unroll
+    for (int j = 0; j < D / 64; ++j) k[j] = *reinterpret_cast<const u32x4 *>(page + (16 * tile + lane % 16) * D + 64 * j + 16 * (lane / 16));
+}
+
+template <int D>
+__device__ __forceinline__ f32x4 scores_of(const u32x4 (&k)[D / 64], const f16x8 (&q)[D / 32]) {
+    f32x4 s = {0.0f, 0.0f, 0.0f, 0.0f};
+#pragma unroll
+    for (int j = 0; j < D / 32; ++j) {
+        const u32x2 half = {k[j / 2][2 * (j % 2)], k[j / 2][2 * (j % 2) + 1]};
+        s = __builtin_amdgcn_mfma_f32_16x16x32_f16(codes_f16(half), q[j], s, 0, 0, 0);
+    }
+    return s;
+}
+
+// A few rows (kv_step.hip): what such calls need of the workspace, zeros first, and the call.
+constexpr size_t kStepCounters = 1024;                    // bytes of counters at the head of the workspace, all 0 between calls
+size_t step_bytes(int dim);                               // and what follows them
+bool step_fits(const spqt_kv_cache &cache, const Call &a);
+void launch_step(const spqt_kv_cache &cache, const Call &a, void *counters, void *space, hipStream_t stream);
+
 // Many rows (kv_prompt.hip): whether a call is of that kind, what such calls need of the workspace at most, and the call.
 bool is_prompt(int rows, int group);
 size_t prompt_bytes(int dim);
