@@ -30,12 +30,12 @@ __global__ __launch_bounds__(kThreads) void spqt_kv_weigh_kernel(Cache c, Call a
         const bool inside = r < count * a.group;
         Row row = row_of(a, r, head, length, count);
         if (!inside) row.high = -1;
-        if (lanes_max(row.high) < block * kBlock) continue;
+        if (rows_max(row.high) < block * kBlock) continue;
         u32x4 raw[D / 32];
         f16x8 q[D / 32];
         load_queries<D>(raw, a.q.data + s * a.q.sequence + row.i * a.q.row + row.head * a.q.head, row.high >= 0, lane);
-        const float back = queries_f16<BF16>(raw, q, 16);
-        const float scale = a.scale * back * kLog2e * scale_k;
+        const float positive = positive_scale(a.scale, raw), back = queries_f16<BF16>(raw, q, 16);
+        const float scale = positive * back * kLog2e * scale_k;
         const float whole = row.high >= 0 ? a.lse[((size_t)s * a.rows + row.i) * a.q_heads + row.head] * kLog2e : 0.0f;
 #pragma unroll
         for (int t = 0; t < 4; ++t) {

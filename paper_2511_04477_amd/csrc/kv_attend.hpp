@@ -50,6 +50,15 @@ struct Meeting {
     __device__ __forceinline__ float lse() const { return total == 0.0f ? kNone : (top == kNone ? 0.0f : top) * kLn2 + __builtin_logf(total); }
 };
 
+// A negative scale is taken as a positive one for the negative queries, so that the largest score is that of the largest product.
+template <int N>
+__device__ __forceinline__ float positive_scale(float scale, u32x4 (&w)[N]) {
+    const uint32_t flip = as_u32(scale) >> 31 ? 0x80008000u : 0u;
+#pragma unroll
+    for (int j = 0; j < N; ++j) w[j] ^= flip;
+    return __builtin_fabsf(scale);
+}
+
 // A lane's part of a row of Q in fp16; `step` is the first distance between the lanes that share the row.  bf16 rows are scaled by a power of two to have
 // their largest element in 2^14 .. 2^15, where fp16 holds them (exactly, down to 2^-30 of the largest); the factor that undoes it is returned.
 template <bool BF16, int N>
@@ -85,21 +94,32 @@ __device__ __forceinline__ float queries_f16(const u32x4 (&w)[N], f16x8 (&q)[N],
 
 // 16 rows at a time: S^T = K Q^T, so that a lane of v_mfma_f32_16x16x32_f16 has ONE row of Q and four tokens of each 16.
 
-__device__ __forceinline__ int lanes_max(int v) {            // over the 16 rows
-#pragma unroll
-    for (int step = 1; step < 16; step *= 2) {
-        const int o = __shfl_xor(v, step);
-        v = o > v ? o : v;
-    }
-    return v;
+// f over the 16 rows; the same for all of them.
+template <class F>
+__device__ __forceinline__ int over_rows(int v, F f) {
+    v = f(v, __builtin_amdgcn_update_dpp(v, v, 0x121, 0xf, 0xf, false));                     // row_ror:1, 2, 4, 8
+    v = f(v, __builtin_amdgcn_update_dpp(v, v, 0x122, 0xf, 0xf, false));
+    v = f(v, __builtin_amdgcn_update_dpp(v, v, 0x124, 0xf, 0xf, false));
+    return f(v, __builtin_amdgcn_update_dpp(v, v, 0x128, 0xf, 0xf, false));
 }
-__device__ __forceinline__ float columns_max(float v) {      // over the four lanes of a row
-    v = __builtin_fmaxf(v, __shfl_xor(v, 16));
-    return __builtin_fmaxf(v, __shfl_xor(v, 32));
+__device__ __forceinline__ int rows_max(int v) {
+    return over_rows(v, [](int x, int y) { return x > y ? x : y; });
+}
+__device__ __forceinline__ int rows_min(int v) {
+    return over_rows(v, [](int x, int y) { return x < y ? x : y; });
+}
+// Over the four lanes of a row.
+__device__ __forceinline__ float columns_max(float v) {
+    auto r = __builtin_amdgcn_permlane16_swap(as_u32(v), as_u32(v), false, false);
+    v = __builtin_fmaxf(as_float(r[0]), as_float(r[1]));
+    r = __builtin_amdgcn_permlane32_swap(as_u32(v), as_u32(v), false, false);
+    return __builtin_fmaxf(as_float(r[0]), as_float(r[1]));
 }
 __device__ __forceinline__ float columns_sum(float v) {
-    v += __shfl_xor(v, 16);
-    return v + __shfl_xor(v, 32);
+    auto r = __builtin_amdgcn_permlane16_swap(as_u32(v), as_u32(v), false, false);
+    v = as_float(r[0]) + as_float(r[1]);
+    r = __builtin_amdgcn_permlane32_swap(as_u32(v), as_u32(v), false, false);
+    return as_float(r[0]) + as_float(r[1]);
 }
 
 // A row of Q as an operand, 32 elements a step: step j of a lane are elements 64 (j / 2) + 16 (lane / 16) + 8 (j % 2) on, as in load_keys; queries_f16 makes it fp16.
@@ -117,14 +137,14 @@ __device__ __forceinline__ void load_keys(u32x4 (&k)[D / 64], const uint8_t *pag
     for (int j = 0; j < D / 64; ++j) k[j] = *reinterpret_cast<const u32x4 *>(page + (16 * tile + lane % 16) * D + 64 * j + 16 * (lane / 16));
 }
 
+// The products of 16 tokens' codes with the queries.  (The stored bytes as fp16's smallest numbers, 2^-24 (code + 128), would save half of the conversion and
+// start the sums at -128 times that of the queries, but a token of small codes in a block of large ones then has the errors of large ones.)
 template <int D>
 __device__ __forceinline__ f32x4 scores_of(const u32x4 (&k)[D / 64], const f16x8 (&q)[D / 32]) {
     f32x4 s = {0.0f, 0.0f, 0.0f, 0.0f};
 #pragma unroll
-    for (int j = 0; j < D / 32; ++j) {
-        const u32x2 half = {k[j / 2][2 * (j % 2)], k[j / 2][2 * (j % 2) + 1]};
-        s = __builtin_amdgcn_mfma_f32_16x16x32_f16(codes_f16(half), q[j], s, 0, 0, 0);
-    }
+    for (int j = 0; j < D / 32; ++j)
+        s = __builtin_amdgcn_mfma_f32_16x16x32_f16(codes_f16(u32x2{k[j / 2][2 * (j % 2)], k[j / 2][2 * (j % 2) + 1]}), q[j], s, 0, 0, 0);
     return s;
 }
 

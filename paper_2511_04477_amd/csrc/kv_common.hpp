@@ -17,6 +17,8 @@ typedef uint32_t u32x2 __attribute__((ext_vector_type(2)));
 typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
 typedef float f32x4 __attribute__((ext_vector_type(4)));
 typedef _Float16 f16x2 __attribute__((ext_vector_type(2)));
+typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
+typedef float f32x2 __attribute__((ext_vector_type(2)));
 typedef _Float16 f16x8 __attribute__((ext_vector_type(8)));
 
 // What a kernel knows of a cache: spqt_kv_cache without what it does not use.
@@ -51,6 +53,13 @@ __device__ __forceinline__ uint16_t narrow(float v) {
     if (!BF16) return __builtin_bit_cast(uint16_t, (_Float16)v);
     const uint32_t u = as_u32(v);
     return v != v ? (uint16_t)0x7FC0 : (uint16_t)((u + 0x7FFFu + ((u >> 16) & 1u)) >> 16);
+}
+
+// Two of them, the first one in the lower half.
+template <bool BF16>
+__device__ __forceinline__ uint32_t narrow2(float a, float b) {
+    if (BF16) return __builtin_bit_cast(uint32_t, __builtin_convertvector(f32x2{a, b}, bf16x2));
+    return __builtin_bit_cast(uint32_t, __builtin_convertvector(f32x2{a, b}, f16x2));
 }
 
 // The scale of a block whose largest |x| has these 16 bits (NaN and infinities order above all numbers, and give NaN).

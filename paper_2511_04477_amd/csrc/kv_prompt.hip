@@ -10,7 +10,6 @@ namespace {
 using namespace spqt;
 using namespace spqt::kv;
 
-typedef float f32x2 __attribute__((ext_vector_type(2)));
 typedef float f32x16 __attribute__((ext_vector_type(16)));
 
 // Eight wavefronts of 32 rows, two on every SIMD; four where sums and queries of longer heads leave no registers for two.
@@ -130,7 +129,8 @@ __global__ __launch_bounds__(Shape<D>::kThreads) void spqt_kv_prompt_kernel(Cach
         u32x4 w[D / 16];
 #pragma unroll
         for (int j = 0; j < D / 16; ++j) w[j] = live ? *reinterpret_cast<const u32x4 *>(from + 16 * j + 8 * half) : u32x4{0u, 0u, 0u, 0u};
-        scale = a.scale * kLog2e * queries_f16<BF16>(w, q, 32);
+        scale = positive_scale(a.scale, w) * kLog2e;
+        scale *= queries_f16<BF16>(w, q, 32);
     }
     int full_low = row.low, full_high = row.high;             // every row of the wavefront sees these tokens
 #pragma unroll
@@ -298,10 +298,8 @@ __global__ __launch_bounds__(Shape<D>::kThreads) void spqt_kv_prompt_kernel(Cach
     for (int i = 0; i < D / 32; ++i)
 #pragma unroll
         for (int e = 0; e < 16; e += 4) {
-            uint16_t v[4];
-#pragma unroll
-            for (int x = 0; x < 4; ++x) v[x] = narrow<BF16>(acc[i][e + x] * by);
-            *reinterpret_cast<u32x2 *>(out + 32 * i + 2 * e) = u32x2{v[0] | (uint32_t)v[1] << 16, v[2] | (uint32_t)v[3] << 16};
+            *reinterpret_cast<u32x2 *>(out + 32 * i + 2 * e) =
+                u32x2{narrow2<BF16>(acc[i][e] * by, acc[i][e + 1] * by), narrow2<BF16>(acc[i][e + 2] * by, acc[i][e + 3] * by)};
         }
     if (a.lse && half == 0) a.lse[((size_t)s * a.rows + row.i) * a.q_heads + row.head] = sum.lse();
 }
@@ -330,7 +328,7 @@ __global__ __launch_bounds__(256) void spqt_kv_parts_kernel(Call a, int kv_heads
     uint16_t *out = a.out.data + s * a.out.sequence + i * a.out.row + q_head * a.out.head + d;
     const float by = m.inverse();
 #pragma unroll
-    for (int e = 0; e < kEach; e += 2) *reinterpret_cast<uint32_t *>(out + e) = narrow<BF16>(x[e] * by) | (uint32_t)narrow<BF16>(x[e + 1] * by) << 16;
+    for (int e = 0; e < kEach; e += 2) *reinterpret_cast<uint32_t *>(out + e) = narrow2<BF16>(x[e] * by, x[e + 1] * by);
     if (a.lse && threadIdx.x % 32 == 0) a.lse[((size_t)s * a.rows + i) * a.q_heads + q_head] = m.lse();
 }
 

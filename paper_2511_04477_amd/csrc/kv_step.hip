@@ -57,36 +57,56 @@ template <int D, bool BF16>
 struct Wave {
     f16x8 q[D / 32];
     Row row;
-    float scale, top, total, unit;       // the row's running maximum, this lane's part of its sum, the scale that acc is in
+    float scale, top, total, unit; // the row's running maximum, this lane's part of its sum, the scale that acc is in
+    int full_low, full_high;             // every row sees the tokens from full_low to full_high
     f32x4 acc[D / 16];
     u32x4 k[4][D / 64], v[D / 16];
 
-    __device__ __forceinline__ void fetch_keys(const uint8_t *page, int lane) {
-#pragma unroll
-        for (int t = 0; t < 4; ++t) load_keys<D>(k[t], page, t, lane);
-    }
-    __device__ __forceinline__ void fetch_values(const uint8_t *page, int lane) {
-#pragma unroll
-        for (int i = 0; i < D / 16; ++i) v[i] = *reinterpret_cast<const u32x4 *>(page + (16 * i + (lane & 15)) * kBlock + 16 * (lane >> 4));
-    }
-    // One block, whose codes have been fetched.  `refill_keys` and `refill_values` request the next one's, each as soon as the registers are free.
-    template <class K, class V>
-    __device__ __forceinline__ void block(int number, float scale_k, float scale_v, int lane, K refill_keys, V refill_values) {
-        f32x4 p[4];
-#pragma unroll
-        for (int t = 0; t < 4; ++t) p[t] = scores_of<D>(k[t], q);
-        refill_keys();
-        float most = top;
-        const float by = scale * scale_k;
+    // The codes of a page; `on` 0: sixteen bytes of it over and over, for the last block's successor.
+    __device__ __forceinline__ void fetch_keys(const uint8_t *page, uint32_t on, int lane) {
+        const uint32_t at = (uint32_t)((lane & 15) * D + 16 * (lane >> 4)) & on, step = (uint32_t)D & on;
 #pragma unroll
         for (int t = 0; t < 4; ++t)
 #pragma unroll
-            for (int e = 0; e < 4; ++e) {
-                const int token = number * kBlock + 16 * t + 4 * (lane >> 4) + e;
-                p[t][e] = token >= row.low && token <= row.high ? p[t][e] * by : kNone;
-                most = __builtin_fmaxf(most, p[t][e]);
-            }
+            for (int j = 0; j < D / 64; ++j) k[t][j] = *reinterpret_cast<const u32x4 *>(page + (at + 16 * t * step) + (on ? 64 * j : 0));
+    }
+    __device__ __forceinline__ void fetch_values(const uint8_t *page, uint32_t on, int lane) {
+        const uint32_t at = (uint32_t)((lane & 15) * kBlock + 16 * (lane >> 4)) & on;
+#pragma unroll
+        for (int i = 0; i < D / 16; ++i) v[i] = *reinterpret_cast<const u32x4 *>(page + at + 16 * i * kBlock);
+    }
+    // One block, whose codes have been fetched; the next one's are requested as soon as the registers are free.
+    __device__ __forceinline__ void block(int number, float scale_k, float scale_v, const uint8_t *next, uint32_t on, int lane) {
+        f32x4 p[4];
+#pragma unroll
+        for (int t = 0; t < 4; ++t) p[t] = scores_of<D>(k[t], q);
+        fetch_keys(next, on, lane);
+        if (number * kBlock < full_low || number * kBlock + kBlock - 1 > full_high) {
+            asm volatile("");                                // a branch: few blocks are masked
+            const uint32_t from = (uint32_t)(number * kBlock + 4 * (lane >> 4) - row.low), seen = (uint32_t)(row.high - row.low);
+#pragma unroll
+            for (int t = 0; t < 4; ++t)
+#pragma unroll
+                for (int e = 0; e < 4; ++e)
+                    if (row.high < row.low || from + (uint32_t)(16 * t + e) > seen) p[t][e] = kNone;
+        }
+        float most = __builtin_fmaxf(p[0][0], p[0][1]);
+#pragma unroll
+        for (int t = 0; t < 4; ++t)
+#pragma unroll
+            for (int e = 0; e < 4; ++e) most = __builtin_fmaxf(most, p[t][e]);
         most = columns_max(most);
+        float by = scale * scale_k + 0x1p-126f;               // not 0: -inf times it is -inf
+        if (scale_k != scale_k) {                            // a NaN for what is seen, none for the rest
+            asm volatile("");
+#pragma unroll
+            for (int t = 0; t < 4; ++t)
+#pragma unroll
+                for (int e = 0; e < 4; ++e) p[t][e] = p[t][e] == kNone ? kNone : scale_k;
+            most = kNone;
+            by = 1.0f;
+        }
+        most = __builtin_fmaxf(top, most == kNone ? kNone : most * by);
         const float from = most == kNone ? 0.0f : most;      // nothing seen yet: 2^(-inf - 0)
         float shrink = __builtin_amdgcn_exp2f(top - from);
         total *= shrink;
@@ -97,21 +117,40 @@ struct Wave {
         }
         const float ratio = scale_v / unit * kLift;
         f16x8 lifted[2], rest[2];                            // a probability in units of `unit`
+        float sum = 0.0f;
 #pragma unroll
         for (int t = 0; t < 4; ++t)
 #pragma unroll
-            for (int e = 0; e < 4; ++e) {
-                const bool seen = !(p[t][e] == kNone);       // a NaN is one
-                const float x = __builtin_amdgcn_exp2f(p[t][e] - from);
-                total += x;
-                const float y = seen ? x * ratio : 0.0f;
-                const _Float16 h = (_Float16)y;
-                lifted[t / 2][4 * (t % 2) + e] = h;
-                rest[t / 2][4 * (t % 2) + e] = (_Float16)(y - (float)h);
+            for (int e = 0; e < 4; e += 2) {
+                f32x2 y;
+#pragma unroll
+                for (int i = 0; i < 2; ++i) {
+                    const float x = __builtin_amdgcn_exp2f(__builtin_fmaf(p[t][e + i], by, -from));
+                    sum += x;
+                    y[i] = x * ratio;
+                }
+                const f16x2 h = __builtin_convertvector(y, f16x2);
+                const f16x2 l = __builtin_convertvector(f32x2{y[0] - (float)h[0], y[1] - (float)h[1]}, f16x2);
+#pragma unroll
+                for (int i = 0; i < 2; ++i) {
+                    lifted[t / 2][4 * (t % 2) + e + i] = h[i];
+                    rest[t / 2][4 * (t % 2) + e + i] = l[i];
+                }
             }
+        total += sum;
+        if (scale_v != scale_v) {                            // only what is masked is none the less 0
+            asm volatile("");
+#pragma unroll
+            for (int t = 0; t < 4; ++t)
+#pragma unroll
+                for (int e = 0; e < 4; ++e)
+                    if (p[t][e] == kNone) lifted[t / 2][4 * (t % 2) + e] = rest[t / 2][4 * (t % 2) + e] = (_Float16)0.0f;
+        }
+        if (__ballot(shrink != 1.0f))
+#pragma unroll
+            for (int i = 0; i < D / 16; ++i) acc[i] *= shrink;
 #pragma unroll
         for (int i = 0; i < D / 16; ++i) {
-            acc[i] *= shrink;
 #pragma unroll
             for (int u = 0; u < 2; ++u) {
                 const f16x8 codes = codes_f16(u32x2{v[i][2 * u], v[i][2 * u + 1]});
@@ -119,7 +158,7 @@ struct Wave {
                 acc[i] = __builtin_amdgcn_mfma_f32_16x16x32_f16(codes, rest[u], acc[i], 0, 0, 0);
             }
         }
-        refill_values();
+        fetch_values(next + kBlock * D, on, lane);
     }
     // Blocks first .. first + n - 1 of the sequence.  Pages and scales of 64 of them are looked up at once, one per lane; the loads of the first ones go out
     // one chain after the other, the queries' among them.
@@ -134,7 +173,10 @@ struct Wave {
             if (done == 0) {
                 const int r = tile * 16 + (lane & 15);
                 row = row_of(a, r, head, span.length, span.count);
-                if (r >= a.rows * a.group) row.high = -1;
+                const bool inside = r < a.rows * a.group;
+                full_low = rows_max(inside ? row.low : 0);
+                full_high = rows_min(inside ? row.high : 0x7FFFFFFF);
+                if (!inside) row.high = -1;
                 load_queries<D>(raw, a.q.data + s * a.q.sequence + row.i * a.q.row + row.head * a.q.head, row.high >= 0, lane);
             }
             const bool there = mine && page < c.pages;
@@ -147,21 +189,20 @@ struct Wave {
             auto codes_of = [&](int i) { return c.codes + codes_at(c, lane_of(page, i), head, 0); };
             auto scale_of = [&](int i, int which) { return as_float(lane_of(as_u32(scales[which]), i)); };
             const uint8_t *now = codes_of(0);
-            fetch_keys(now, lane);
-            fetch_values(now + kBlock * D, lane);
+            fetch_keys(now, ~0u, lane);
+            fetch_values(now + kBlock * D, ~0u, lane);
             if (done == 0) {
-                scale = a.scale * kLog2e * queries_f16<BF16>(raw, q, 16);
+                scale = positive_scale(a.scale, raw) * kLog2e;
+                scale *= queries_f16<BF16>(raw, q, 16);
                 top = kNone;
                 total = 0.0f;
                 unit = 0x1p-120f;
 #pragma unroll
                 for (int i = 0; i < D / 16; ++i) acc[i] = {0.0f, 0.0f, 0.0f, 0.0f};
             }
-            for (int i = 0; i + 1 < here; ++i) {
-                const uint8_t *next = codes_of(i + 1);
-                block(b0 + i, scale_of(i, 0), scale_of(i, 1), lane, [&]() { fetch_keys(next, lane); }, [&]() { fetch_values(next + kBlock * D, lane); });
-            }
-            block(b0 + here - 1, scale_of(here - 1, 0), scale_of(here - 1, 1), lane, []() {}, []() {});
+#pragma unroll 1
+            for (int i = 0; i < here; ++i)
+                block(b0 + i, scale_of(i, 0), scale_of(i, 1), codes_of(i + 1 < here ? i + 1 : i), i + 1 < here ? ~0u : 0u, lane);
         }
     }
 };
@@ -304,10 +345,7 @@ __global__ __launch_bounds__(step_threads(D)) void spqt_kv_step_kernel(Cache c, 
         by *= m.inverse();
 #pragma unroll
         for (int d = 0; d < D / 16; ++d) {
-            uint16_t v[4];
-#pragma unroll
-            for (int e = 0; e < 4; ++e) v[e] = narrow<BF16>(x[d][e] * by);
-            *reinterpret_cast<u32x2 *>(out + 16 * d) = u32x2{v[0] | (uint32_t)v[1] << 16, v[2] | (uint32_t)v[3] << 16};
+            *reinterpret_cast<u32x2 *>(out + 16 * d) = u32x2{narrow2<BF16>(x[d][0] * by, x[d][1] * by), narrow2<BF16>(x[d][2] * by, x[d][3] * by)};
         }
         if (a.lse && quarter == 0) a.lse[((size_t)p.s * a.rows + i) * a.q_heads + head] = m.lse();
     };
@@ -327,7 +365,7 @@ __global__ __launch_bounds__(step_threads(D)) void spqt_kv_step_kernel(Cache c, 
         uint16_t *out = a.out.data + p.s * a.out.sequence + i * a.out.row + head * a.out.head + my_d;
         const float by = m.inverse();
 #pragma unroll
-        for (int d = 0; d < kPart; d += 2) *reinterpret_cast<uint32_t *>(out + d) = narrow<BF16>(x[d] * by) | (uint32_t)narrow<BF16>(x[d + 1] * by) << 16;
+        for (int d = 0; d < kPart; d += 2) *reinterpret_cast<uint32_t *>(out + d) = narrow2<BF16>(x[d] * by, x[d + 1] * by);
         if (a.lse && threadIdx.x % kRowThreads == 0) a.lse[((size_t)p.s * a.rows + i) * a.q_heads + head] = m.lse();
     };
     auto live_rows = [&](const Place &p) {

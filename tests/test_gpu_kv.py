@@ -415,6 +415,18 @@ def test_queries_of_any_size(gpu, size):
     compare(gpu, c, q * 0, None, 0, out, lse, scale=scale)
 
 
+@pytest.mark.parametrize("rows", [1, 40])
+@pytest.mark.parametrize("scale", [0.0, -0.3])
+def test_scales_that_are_not_positive(gpu, rows, scale):
+    torch, _ = gpu
+    c = Cache(gpu, 1, 2, 128, torch.float16, 3, 44)
+    c.append(150)
+    c.weights.zero_()
+    q = torch.randn((1, rows, 4, 128), generator=c.gen).half().cuda()
+    out, lse = attend(gpu, c, q, None, window=100, scale=scale, weigh=True)
+    compare(gpu, c, q if scale >= 0 else -q, None, 100, out, lse, scale=abs(scale), weights=c.weights, before=torch.zeros(c.weights.shape))
+
+
 def test_attention_over_pages_beyond_four_gigabytes(gpu):
     torch, spqt = gpu
     pages = 36_000                                     # 8 heads, 128: 128 KB a page, 4.7 GB
