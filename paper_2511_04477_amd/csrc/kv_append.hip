@@ -32,7 +32,7 @@ __global__ __launch_bounds__(kTileThreads) void spqt_kv_append_kernel(Cache c, R
         for (int p = from * (D / 8) + (int)threadIdx.x; p < to * (D / 8); p += kTileThreads) {
             const int t = p / (D / 8), d = p % (D / 8) * 8;
             const u32x4 x = *reinterpret_cast<const u32x4 *>(in + (base + t - row0) * r.row + d);
-            *reinterpret_cast<u32x4 *>(&tile.v[t][d]) = x;
+            tile.put(t, d, x);
             pair = larger_pair(larger_pair(pair, x.x), larger_pair(x.y, larger_pair(x.z, x.w)));
             if (block == last && to < kBlock) *reinterpret_cast<u32x4 *>(tail + p * 8) = x;
         }
@@ -44,7 +44,7 @@ __global__ __launch_bounds__(kTileThreads) void spqt_kv_append_kernel(Cache c, R
             const bool grown = from > 0 && !(scale == held);
             if (grown)
                 for (int p = (int)threadIdx.x; p < from * (D / 8); p += kTileThreads)
-                    *reinterpret_cast<u32x4 *>(&tile.v[p / (D / 8)][p % (D / 8) * 8]) = *reinterpret_cast<const u32x4 *>(tail + p * 8);
+                    tile.put(p / (D / 8), p % (D / 8) * 8, *reinterpret_cast<const u32x4 *>(tail + p * 8));
             __syncthreads();                       // the tile is whole, and everyone has the old scale
             store_tile<D, BF16>(c, tile, page, head, which, grown ? 0 : from, to, scale);
             if (threadIdx.x == 0) *scales = scale;
@@ -56,10 +56,12 @@ __global__ __launch_bounds__(kTileThreads) void spqt_kv_append_kernel(Cache c, R
     }
 }
 
-// One workgroup per block that the call reads from, head and side.  The codes of a block go through shared memory as they are.
+// One workgroup per block that the call reads from, head and side.  Keys go straight through; values go through shared memory as they are, and come out
+// four tokens of eight elements at a time.
 template <int D, bool BF16>
 __global__ __launch_bounds__(kTileThreads) void spqt_kv_read_kernel(Cache c, Rows keys, Rows values, int rows, const int32_t *counts) {
-    __shared__ uint8_t codes[kBlock * D];
+    constexpr int kLine = kBlock / 4 + 1;                 // words of an element's tokens, and one
+    __shared__ uint32_t codes[D * kLine];
     const int s = blockIdx.z, head = blockIdx.y >> 1, which = blockIdx.y & 1;
     const int length = length_of(c, s), count = count_of(counts, s, rows), row0 = length - count;
     const int block = block_of(row0) + (int)blockIdx.x, base = block * kBlock;
@@ -71,22 +73,40 @@ __global__ __launch_bounds__(kTileThreads) void spqt_kv_read_kernel(Cache c, Row
     const bool there = page < c.pages;
     if (!there) page = 0;
     const float scale = there ? c.scales[scale_at(c, page, head, which)] : __builtin_nanf("");
-    if (any) {
-        const uint8_t *in = c.codes + codes_at(c, page, head, which);
-        for (int p = (int)threadIdx.x * 16; p < kBlock * D; p += kTileThreads * 16) *reinterpret_cast<u32x4 *>(codes + p) = *reinterpret_cast<const u32x4 *>(in + p);
-    }
-    __syncthreads();
-    for (int p = (int)threadIdx.x; p < kBlock * (D / 8); p += kTileThreads) {
-        const int t = p / (D / 8), d = p % (D / 8) * 8, i = base + t - row0;
-        if (i < 0 || i >= rows) continue;
+    const uint8_t *in = c.codes + codes_at(c, page, head, which);
+    auto write = [&](int t, int d, u32x2 bytes) {
+        const int i = base + t - row0;
+        if (i < 0 || i >= rows) return;
         u32x4 x = {0u, 0u, 0u, 0u};
         if (i < count && base + t >= 0)
 #pragma unroll
-            for (int j = 0; j < 8; ++j) {
-                const uint32_t byte = codes[which ? (d + j) * kBlock + place_of(t) : t * D + d + j];
-                x[j / 2] |= (uint32_t)value_of<BF16>(byte, scale) << (16 * (j % 2));
-            }
+            for (int j = 0; j < 4; ++j)
+                x[j] = values_of<BF16>(bytes[j / 2] >> (16 * (j % 2)) & 255, bytes[j / 2] >> (16 * (j % 2) + 8) & 255, scale);
         *reinterpret_cast<u32x4 *>(out + i * r.row + d) = x;
+    };
+    if (which == 0) {
+        for (int p = (int)threadIdx.x; p < kBlock * (D / 8); p += kTileThreads)
+            write(p / (D / 8), p % (D / 8) * 8, *reinterpret_cast<const u32x2 *>(in + p * 8));
+        return;
+    }
+    for (int p = (int)threadIdx.x; p < D * 4; p += kTileThreads) {
+        const u32x4 x = *reinterpret_cast<const u32x4 *>(in + p * 16);
+#pragma unroll
+        for (int i = 0; i < 4; ++i) codes[p / 4 * kLine + p % 4 * 4 + i] = x[i];
+    }
+    __syncthreads();
+    for (int p = (int)threadIdx.x; p < 16 * (D / 8); p += kTileThreads) {
+        const int word = p / (D / 8), d = p % (D / 8) * 8, t = word % 4 * 16 + word / 4 * 4;
+        uint32_t x[8];
+#pragma unroll
+        for (int j = 0; j < 8; ++j) x[j] = codes[(d + j) * kLine + word];
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            u32x2 bytes = {0u, 0u};
+#pragma unroll
+            for (int j = 0; j < 8; ++j) bytes[j / 4] |= (x[j] >> (8 * i) & 255u) << (8 * (j % 4));
+            write(t + i, d, bytes);
+        }
     }
 }
 

@@ -52,9 +52,7 @@ __global__ __launch_bounds__(kThreads) void spqt_kv_weigh_kernel(Cache c, Call a
     for (int t = 0; t < 4; ++t)
 #pragma unroll
         for (int e = 0; e < 4; ++e) {
-            float x = sum[t][e];
-#pragma unroll
-            for (int step = 1; step < 16; step *= 2) x += __shfl_xor(x, step);
+            const float x = rows_sum(sum[t][e]);
             const int at = 16 * t + 4 * quarter + e;
             if (column == 0 && block * kBlock + at < length) weights[at] = a.decay == 0.0f ? x : __builtin_fmaf(a.decay, weights[at], x);
         }

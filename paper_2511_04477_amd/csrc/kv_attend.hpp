@@ -108,6 +108,9 @@ __device__ __forceinline__ int rows_max(int v) {
 __device__ __forceinline__ int rows_min(int v) {
     return over_rows(v, [](int x, int y) { return x < y ? x : y; });
 }
+__device__ __forceinline__ float rows_sum(float v) {
+    return as_float((uint32_t)over_rows((int)as_u32(v), [](int x, int y) { return (int)as_u32(as_float((uint32_t)x) + as_float((uint32_t)y)); }));
+}
 // Over the four lanes of a row.
 __device__ __forceinline__ float columns_max(float v) {
     auto r = __builtin_amdgcn_permlane16_swap(as_u32(v), as_u32(v), false, false);

@@ -47,15 +47,7 @@ template <bool BF16>
 __device__ __forceinline__ float widen(uint16_t x) {
     return BF16 ? as_float((uint32_t)x << 16) : (float)__builtin_bit_cast(_Float16, x);
 }
-// To nearest even; a NaN stays one.
-template <bool BF16>
-__device__ __forceinline__ uint16_t narrow(float v) {
-    if (!BF16) return __builtin_bit_cast(uint16_t, (_Float16)v);
-    const uint32_t u = as_u32(v);
-    return v != v ? (uint16_t)0x7FC0 : (uint16_t)((u + 0x7FFFu + ((u >> 16) & 1u)) >> 16);
-}
-
-// Two of them, the first one in the lower half.
+// Two numbers to nearest even, the first one in the lower half.
 template <bool BF16>
 __device__ __forceinline__ uint32_t narrow2(float a, float b) {
     if (BF16) return __builtin_bit_cast(uint32_t, __builtin_convertvector(f32x2{a, b}, bf16x2));
@@ -80,12 +72,15 @@ __device__ __forceinline__ uint32_t code_of(float x, float inverse) {
     return (uint32_t)(int)__builtin_fminf(__builtin_fmaxf(__builtin_rintf(x * inverse) + 128.0f, 1.0f), 255.0f);
 }
 
-// A cached value as a reader gets it.
+// Two cached values as a reader gets them.
 template <bool BF16>
-__device__ __forceinline__ uint16_t value_of(uint32_t byte, float scale) {
+__device__ __forceinline__ uint32_t values_of(uint32_t first, uint32_t second, float scale) {
     const float largest = BF16 ? as_float(0x7F7F0000u) : 65504.0f;
-    const float v = (float)((int)byte - 128) * scale;
-    return narrow<BF16>(v != v ? v : __builtin_fmaxf(-largest, __builtin_fminf(v, largest)));
+    auto value = [&](uint32_t byte) {
+        const float v = (float)((int)byte - 128) * scale;
+        return v != v ? v : __builtin_fmaxf(-largest, __builtin_fminf(v, largest));
+    };
+    return narrow2<BF16>(value(first), value(second));
 }
 
 __device__ __forceinline__ int clamped(int v, int low, int high) { return v < low ? low : (v > high ? high : v); }

@@ -9,10 +9,17 @@ namespace kv {
 
 constexpr int kTileThreads = 256;
 
+// The 16 fours of tokens that a wavefront takes at once are in 8 banks of 8, two in each, with four numbers behind every token.
 template <int D>
 struct Tile {
-    uint16_t v[kBlock][D + 8];
+    uint16_t v[kBlock][D + 4];
     uint32_t largest[kTileThreads / 64];
+
+    __device__ __forceinline__ void put(int t, int d, u32x4 x) {
+        u32x2 *to = reinterpret_cast<u32x2 *>(&v[t][d]);
+        to[0] = u32x2{x.x, x.y};
+        to[1] = u32x2{x.z, x.w};
+    }
 };
 
 // The larger magnitudes of two pairs of 16-bit numbers, as bits (both types order as their magnitude bits do).
@@ -37,6 +44,13 @@ __device__ __forceinline__ uint32_t largest_of(Tile<D> &tile, uint32_t pair) {
     return m;
 }
 
+// The lower or upper one of two numbers.
+template <bool BF16>
+__device__ __forceinline__ float half_of(uint32_t pair, int upper) {
+    if (BF16) return as_float(upper ? pair & 0xFFFF0000u : pair << 16);
+    return widen<false>((uint16_t)(upper ? pair >> 16 : pair & 0xFFFFu));
+}
+
 // Quantizes tokens from .. to - 1 of the tile into the page.
 template <int D, bool BF16>
 __device__ __forceinline__ void store_tile(const Cache &c, const Tile<D> &tile, uint32_t page, int head, int which, int from, int to, float scale) {
@@ -44,26 +58,35 @@ __device__ __forceinline__ void store_tile(const Cache &c, const Tile<D> &tile, 
     uint8_t *out = c.codes + codes_at(c, page, head, which);
     if (which == 0) {
         for (int p = from * (D / 8) + (int)threadIdx.x; p < to * (D / 8); p += kTileThreads) {
-            const uint16_t *x = &tile.v[p / (D / 8)][p % (D / 8) * 8];
+            const u32x2 *x = reinterpret_cast<const u32x2 *>(&tile.v[p / (D / 8)][p % (D / 8) * 8]);
             u32x2 w = {0u, 0u};
 #pragma unroll
-            for (int i = 0; i < 8; ++i) w[i / 4] |= code_of(widen<BF16>(x[i]), inverse) << (8 * (i % 4));
+            for (int i = 0; i < 8; ++i) w[i / 4] |= code_of(half_of<BF16>(x[i / 4][i / 2 % 2], i % 2), inverse) << (8 * (i % 4));
             *reinterpret_cast<u32x2 *>(out + p * 8) = w;
         }
         return;
     }
-    for (int p = (int)threadIdx.x; p < D * 16; p += kTileThreads) {
-        const int d = p / 16, word = p % 16, t = word % 4 * 16 + word / 4 * 4;      // place 4 * word holds tokens t .. t + 3
+    // four tokens of two elements at a time
+    for (int p = (int)threadIdx.x; p < D * 8; p += kTileThreads) {
+        const int d = p / 16 * 2, word = p % 16, t = word % 4 * 16 + word / 4 * 4;  // place 4 * word holds tokens t .. t + 3
         if (t + 4 <= from || t >= to) continue;
-        uint32_t w = 0;
+        uint32_t w[2] = {0u, 0u};
 #pragma unroll
-        for (int i = 0; i < 4; ++i) w |= code_of(widen<BF16>(tile.v[t + i][d]), inverse) << (8 * i);
-        if (t >= from && t + 4 <= to) {
-            *reinterpret_cast<uint32_t *>(out + p * 4) = w;
-        } else {
+        for (int i = 0; i < 4; ++i) {
+            const uint32_t x = *reinterpret_cast<const uint32_t *>(&tile.v[t + i][d]);
 #pragma unroll
-            for (int i = 0; i < 4; ++i)
-                if (t + i >= from && t + i < to) out[p * 4 + i] = (uint8_t)(w >> (8 * i));
+            for (int e = 0; e < 2; ++e) w[e] |= code_of(half_of<BF16>(x, e), inverse) << (8 * i);
+        }
+#pragma unroll
+        for (int e = 0; e < 2; ++e) {
+            uint8_t *at = out + (d + e) * kBlock + word * 4;
+            if (t >= from && t + 4 <= to) {
+                *reinterpret_cast<uint32_t *>(at) = w[e];
+            } else {
+#pragma unroll
+                for (int i = 0; i < 4; ++i)
+                    if (t + i >= from && t + i < to) at[i] = (uint8_t)(w[e] >> (8 * i));
+            }
         }
     }
 }
