@@ -47,15 +47,18 @@ __global__ __launch_bounds__(kThreads) void spqt_kv_weigh_kernel(Cache c, Call a
             }
         }
     }
-    float *weights = c.weights + weight_at(c, page, head);
+    // lane `column` of a token's 16 takes the column-th of its quarter's tokens
+    float mine = 0.0f;
 #pragma unroll
     for (int t = 0; t < 4; ++t)
 #pragma unroll
         for (int e = 0; e < 4; ++e) {
             const float x = rows_sum(sum[t][e]);
-            const int at = 16 * t + 4 * quarter + e;
-            if (column == 0 && block * kBlock + at < length) weights[at] = a.decay == 0.0f ? x : __builtin_fmaf(a.decay, weights[at], x);
+            mine = column == 4 * t + e ? x : mine;
         }
+    const int at = 16 * (column / 4) + 4 * quarter + column % 4;
+    float *weight = c.weights + weight_at(c, page, head) + at;
+    if (block * kBlock + at < length) *weight = a.decay == 0.0f ? mine : __builtin_fmaf(a.decay, *weight, mine);
 }
 
 }  // namespace

@@ -66,10 +66,13 @@ __device__ __forceinline__ float scale_of(uint32_t largest) {
     return as_float(odd);
 }
 
-// The stored byte of x, given 1 / scale.  x * inverse is x / scale to 2^-23 of itself, and x / scale is at least 2^-20 of itself away
-// from the middle between two integers, so it rounds as the quotient does.  NaN (a block with a NaN or an infinity) is stored as 1 - 128.
-__device__ __forceinline__ uint32_t code_of(float x, float inverse) {
-    return (uint32_t)(int)__builtin_fminf(__builtin_fmaxf(__builtin_rintf(x * inverse) + 128.0f, 1.0f), 255.0f);
+// The stored byte of x in the lowest bits of a number, given 1 / scale: adding 1.5 2^23 rounds to the nearest integer.  x * inverse is x / scale to 2^-24 of
+// itself, and x / scale is at least 2^-20 of itself away from the middle between two integers, so it rounds as the quotient does.
+__device__ __forceinline__ uint32_t coded(float x, float inverse) { return as_u32(__builtin_fmaf(x, inverse, 12582912.0f + 128.0f)); }
+// Four of them; what is no number, in a block whose scale is none, is stored as 0.
+__device__ __forceinline__ uint32_t bytes_of(uint32_t a, uint32_t b, uint32_t c, uint32_t d, float inverse) {
+    const uint32_t low = __builtin_amdgcn_perm(b, a, 0x0C0C0400u), high = __builtin_amdgcn_perm(d, c, 0x04000C0Cu);
+    return inverse != inverse ? 0x80808080u : low | high;
 }
 
 // Two cached values as a reader gets them.

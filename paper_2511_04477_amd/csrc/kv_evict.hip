@@ -40,16 +40,7 @@ __global__ __launch_bounds__(kSelectThreads) void spqt_kv_select_kernel(Cache c,
     }
 
     const int32_t *table = c.table + (size_t)s * c.max_blocks;
-    const bool nearby = older <= kNearby;
-    auto look_up = [&](int t) {
-        const uint32_t page = (uint32_t)table[t / kBlock];
-        return page < c.pages ? rank_of(c.weights[weight_at(c, page, head) + t % kBlock]) : ~0u;
-    };
-    auto rank_at = [&](int t) { return nearby ? ranks[t] : look_up(t); };
-    if (nearby)
-#pragma unroll 4
-        for (int t = tid; t < older; t += kSelectThreads) ranks[t] = look_up(t);
-
+    auto choose = [&](auto rank_at) {
     // least: the rank of the lightest one picked; rest: how many of that rank are picked
     uint32_t least = 0;
     int rest = pick;
@@ -128,6 +119,29 @@ __global__ __launch_bounds__(kSelectThreads) void spqt_kv_select_kernel(Cache c,
         if (rank > least || tie) out[place++] = t;
     }
     for (int i = tid; i < late; i += kSelectThreads) out[pick + i] = older + i;
+    };
+    if (older <= kNearby) {
+        // a block per wavefront at a time, whose pages are looked up at once
+        const int blocks = (older + kBlock - 1) / kBlock;
+        for (int b0 = wave; b0 < blocks; b0 += 64 * kSelectWaves) {
+            const int mine = b0 + lane * kSelectWaves;
+            const uint32_t page = mine < blocks ? (uint32_t)table[mine] : 0u;
+#pragma unroll 8
+            for (int i = 0; i < 64; ++i) {
+                const int b = b0 + i * kSelectWaves;
+                if (b >= blocks) break;
+                const uint32_t here = (uint32_t)__builtin_amdgcn_readlane((int)page, i);
+                ranks[b * kBlock + lane] = here < c.pages ? rank_of(c.weights[weight_at(c, here, head) + lane]) : ~0u;
+            }
+        }
+        __syncthreads();
+        choose([&](int t) { return ranks[t]; });
+    } else {
+        choose([&](int t) {
+            const uint32_t page = (uint32_t)table[t / kBlock];
+            return page < c.pages ? rank_of(c.weights[weight_at(c, page, head) + t % kBlock]) : ~0u;
+        });
+    }
 }
 
 // One workgroup per new page, head and side.
@@ -206,7 +220,7 @@ extern "C" int spqt_kv_evict(const spqt_kv_cache *cache, int keep, int recent, c
     if ((uintptr_t)new_table % 4 != 0 || (uintptr_t)new_lengths % 4 != 0 || (uintptr_t)kept % 4 != 0) return SPQT_EALIGN;
     // as many ranks in shared memory as the sequences' tables have room for
     const int64_t room = (int64_t)cache->max_blocks * kBlock;
-    const size_t bytes = room <= kNearby ? (size_t)room * 4 : (size_t)kNearby * 4;
+    const size_t bytes = (size_t)(room < kNearby ? room : kNearby) * 4;
     hipLaunchKernelGGL(spqt_kv_select_kernel, dim3(cache->kv_heads, cache->sequences), dim3(kSelectThreads), bytes, (hipStream_t)stream, view(*cache), keep, recent,
                        new_lengths, kept);
     const int most = cache->max_blocks < (keep + kBlock - 1) / kBlock ? cache->max_blocks : (keep + kBlock - 1) / kBlock;

@@ -24,8 +24,8 @@ struct Tile {
 
 // The larger magnitudes of two pairs of 16-bit numbers, as bits (both types order as their magnitude bits do).
 __device__ __forceinline__ uint32_t larger_pair(uint32_t a, uint32_t b) {
-    const uint32_t al = a & 0x7FFFu, ah = a & 0x7FFF0000u, bl = b & 0x7FFFu, bh = b & 0x7FFF0000u;
-    return (al > bl ? al : bl) | (ah > bh ? ah : bh);
+    typedef uint16_t u16x2 __attribute__((ext_vector_type(2)));
+    return __builtin_bit_cast(uint32_t, __builtin_elementwise_max(__builtin_bit_cast(u16x2, a & 0x7FFF7FFFu), __builtin_bit_cast(u16x2, b & 0x7FFF7FFFu)));
 }
 // The largest magnitude (16 bits) of all threads' pairs.
 template <int D>
@@ -59,10 +59,10 @@ __device__ __forceinline__ void store_tile(const Cache &c, const Tile<D> &tile, 
     if (which == 0) {
         for (int p = from * (D / 8) + (int)threadIdx.x; p < to * (D / 8); p += kTileThreads) {
             const u32x2 *x = reinterpret_cast<const u32x2 *>(&tile.v[p / (D / 8)][p % (D / 8) * 8]);
-            u32x2 w = {0u, 0u};
+            uint32_t c[8];
 #pragma unroll
-            for (int i = 0; i < 8; ++i) w[i / 4] |= code_of(half_of<BF16>(x[i / 4][i / 2 % 2], i % 2), inverse) << (8 * (i % 4));
-            *reinterpret_cast<u32x2 *>(out + p * 8) = w;
+            for (int i = 0; i < 8; ++i) c[i] = coded(half_of<BF16>(x[i / 4][i / 2 % 2], i % 2), inverse);
+            *reinterpret_cast<u32x2 *>(out + p * 8) = u32x2{bytes_of(c[0], c[1], c[2], c[3], inverse), bytes_of(c[4], c[5], c[6], c[7], inverse)};
         }
         return;
     }
@@ -70,13 +70,13 @@ __device__ __forceinline__ void store_tile(const Cache &c, const Tile<D> &tile, 
     for (int p = (int)threadIdx.x; p < D * 8; p += kTileThreads) {
         const int d = p / 16 * 2, word = p % 16, t = word % 4 * 16 + word / 4 * 4;  // place 4 * word holds tokens t .. t + 3
         if (t + 4 <= from || t >= to) continue;
-        uint32_t w[2] = {0u, 0u};
+        uint32_t x[4], w[2];
 #pragma unroll
-        for (int i = 0; i < 4; ++i) {
-            const uint32_t x = *reinterpret_cast<const uint32_t *>(&tile.v[t + i][d]);
+        for (int i = 0; i < 4; ++i) x[i] = *reinterpret_cast<const uint32_t *>(&tile.v[t + i][d]);
 #pragma unroll
-            for (int e = 0; e < 2; ++e) w[e] |= code_of(half_of<BF16>(x, e), inverse) << (8 * i);
-        }
+        for (int e = 0; e < 2; ++e)
+            w[e] = bytes_of(coded(half_of<BF16>(x[0], e), inverse), coded(half_of<BF16>(x[1], e), inverse), coded(half_of<BF16>(x[2], e), inverse),
+                            coded(half_of<BF16>(x[3], e), inverse), inverse);
 #pragma unroll
         for (int e = 0; e < 2; ++e) {
             uint8_t *at = out + (d + e) * kBlock + word * 4;
