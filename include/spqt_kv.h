@@ -49,7 +49,7 @@ typedef struct {
     void *codes;            /* 16-byte aligned */
     float *scales;          /* 8-byte aligned */
     void *tail;             /* append and evict; 16-byte aligned */
-    float *weights;         /* optional except for spqt_kv_evict */
+    float *weights;         /* optional except for spqt_kv_evict; 16-byte aligned */
     const int32_t *table;
     const int32_t *lengths;
     int64_t pages;          /* 1 .. 2^31 - 1 */

@@ -29,12 +29,19 @@ __global__ __launch_bounds__(kTileThreads) void spqt_kv_append_kernel(Cache c, R
         const uint32_t page = (uint32_t)table[block];
         const bool there = page < c.pages;
         uint32_t pair = 0;
-        for (int p = from * (D / 8) + (int)threadIdx.x; p < to * (D / 8); p += kTileThreads) {
-            const int t = p / (D / 8), d = p % (D / 8) * 8;
-            const u32x4 x = *reinterpret_cast<const u32x4 *>(in + (base + t - row0) * r.row + d);
-            tile.put(t, d, x);
-            pair = larger_pair(larger_pair(pair, x.x), larger_pair(x.y, larger_pair(x.z, x.w)));
-            if (block == last && to < kBlock) *reinterpret_cast<u32x4 *>(tail + p * 8) = x;
+        u32x4 x[D / 32];
+#pragma unroll
+        for (int n = 0; n < D / 32; ++n) {
+            const int p = (int)threadIdx.x + n * kTileThreads, t = p / (D / 8);
+            if (t >= from && t < to) x[n] = *reinterpret_cast<const u32x4 *>(in + (base + t - row0) * r.row + p % (D / 8) * 8);
+        }
+#pragma unroll
+        for (int n = 0; n < D / 32; ++n) {
+            const int p = (int)threadIdx.x + n * kTileThreads, t = p / (D / 8);
+            if (t < from || t >= to) continue;
+            tile.put(t, p % (D / 8) * 8, x[n]);
+            pair = larger_pair(larger_pair(pair, x[n].x), larger_pair(x[n].y, larger_pair(x[n].z, x[n].w)));
+            if (block == last && to < kBlock) *reinterpret_cast<u32x4 *>(tail + p * 8) = x[n];
         }
         const float fresh = scale_of<BF16>(largest_of(tile, pair));
         if (there) {
@@ -85,6 +92,7 @@ __global__ __launch_bounds__(kTileThreads) void spqt_kv_read_kernel(Cache c, Row
         *reinterpret_cast<u32x4 *>(out + i * r.row + d) = x;
     };
     if (which == 0) {
+#pragma unroll
         for (int p = (int)threadIdx.x; p < kBlock * (D / 8); p += kTileThreads)
             write(p / (D / 8), p % (D / 8) * 8, *reinterpret_cast<const u32x2 *>(in + p * 8));
         return;

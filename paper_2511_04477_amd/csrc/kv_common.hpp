@@ -102,6 +102,21 @@ __device__ __forceinline__ size_t weight_at(const Cache &c, uint32_t page, int h
     return ((size_t)page * (size_t)c.kv_heads + (size_t)head) * kBlock;
 }
 
+// Lane l's value of lanes 0 .. l together; lane 63 has all.
+template <class F>
+__device__ __forceinline__ uint32_t over_lanes(uint32_t v, F f) {
+    v = f(v, (uint32_t)__builtin_amdgcn_update_dpp(0, (int)v, 0x111, 0xf, 0xf, false));      // row_shr:1
+    v = f(v, (uint32_t)__builtin_amdgcn_update_dpp(0, (int)v, 0x112, 0xf, 0xf, false));
+    v = f(v, (uint32_t)__builtin_amdgcn_update_dpp(0, (int)v, 0x114, 0xf, 0xf, false));
+    v = f(v, (uint32_t)__builtin_amdgcn_update_dpp(0, (int)v, 0x118, 0xf, 0xf, false));
+    v = f(v, (uint32_t)__builtin_amdgcn_update_dpp(0, (int)v, 0x142, 0xa, 0xf, false));      // row_bcast:15
+    return f(v, (uint32_t)__builtin_amdgcn_update_dpp(0, (int)v, 0x143, 0xc, 0xf, false));   // row_bcast:31
+}
+__device__ __forceinline__ uint32_t sum_upto(uint32_t v) {
+    return over_lanes(v, [](uint32_t x, uint32_t y) { return x + y; });
+}
+__device__ __forceinline__ uint32_t lane_of(uint32_t v, int lane) { return (uint32_t)__builtin_amdgcn_readlane((int)v, lane); }
+
 // Eight stored bytes as the fp16 numbers code (exact).
 __device__ __forceinline__ f16x8 codes_f16(u32x2 w) {
     const f16x2 bias = {(_Float16)1152.0f, (_Float16)1152.0f};      // 1024, which the bytes are put over, and 128
@@ -125,7 +140,7 @@ inline int check_cache(const spqt_kv_cache *c, bool tail) {
     if (c->pages < 1 || c->pages > 0x7FFFFFFF || c->sequences < 1 || c->sequences > 65535) return SPQT_ESHAPE;
     if (c->max_blocks < 1 || c->max_blocks > 1 << 24 || c->kv_heads < 1 || c->kv_heads > 16384) return SPQT_ESHAPE;
     if (c->head_dim < 64 || c->head_dim > SPQT_KV_MAX_DIM || c->head_dim % 64 != 0) return SPQT_ESHAPE;
-    if ((uintptr_t)c->codes % 16 != 0 || (uintptr_t)c->scales % 8 != 0 || (uintptr_t)c->tail % 16 != 0 || (uintptr_t)c->weights % 4 != 0 ||
+    if ((uintptr_t)c->codes % 16 != 0 || (uintptr_t)c->scales % 8 != 0 || (uintptr_t)c->tail % 16 != 0 || (uintptr_t)c->weights % 16 != 0 ||
         (uintptr_t)c->table % 4 != 0 || (uintptr_t)c->lengths % 4 != 0)
         return SPQT_EALIGN;
     return SPQT_OK;

@@ -16,13 +16,13 @@ __device__ __forceinline__ uint32_t rank_of(float w) {
 }
 
 constexpr int kSelectWaves = kSelectThreads / 64, kCopies = 16;
-constexpr int kNearby = 34816;                            // ranks in shared memory, 136 KB
+constexpr int kNearby = 32768;                            // ranks in shared memory, 128 KB
 
 // One workgroup per sequence and head.  The rank of the lightest token that is kept is found eight bits at a time from counts of those bits, 16 copies of them
 // for the lanes to keep out of each other's way; then every thread walks a stretch of tokens in order, a kept one taking the next place.
-// What bounds it: one CU per sequence and head, for 5 passes over the tokens' ranks.  They stay in shared memory where there are at most 34816 of them.
+// What bounds it: one CU per sequence and head, for 5 passes over the tokens' ranks.  They stay in shared memory where there are at most 32768 of them.
 __global__ __launch_bounds__(kSelectThreads) void spqt_kv_select_kernel(Cache c, int keep, int recent, int32_t *new_lengths, int32_t *kept) {
-    extern __shared__ uint32_t ranks[];
+    extern __shared__ __attribute__((aligned(16))) uint32_t ranks[];
     __shared__ int counts[256 * kCopies];
     __shared__ int wave_sums[2][kSelectWaves];
     __shared__ uint32_t found_prefix;
@@ -40,106 +40,140 @@ __global__ __launch_bounds__(kSelectThreads) void spqt_kv_select_kernel(Cache c,
     }
 
     const int32_t *table = c.table + (size_t)s * c.max_blocks;
-    auto choose = [&](auto rank_at) {
-    // least: the rank of the lightest one picked; rest: how many of that rank are picked
-    uint32_t least = 0;
-    int rest = pick;
-    for (int shift = 24; shift >= 0; shift -= 8) {
-        for (int i = tid; i < 256 * kCopies; i += kSelectThreads) counts[i] = 0;
-        __syncthreads();
-#pragma unroll 4
-        for (int t = tid; t < older; t += kSelectThreads) {
-            const uint32_t rank = rank_at(t);
-            if (shift == 24 || (rank ^ least) >> (shift + 8) == 0) atomicAdd(&counts[(rank >> shift & 255) * kCopies + (lane & (kCopies - 1))], 1);
-        }
-        __syncthreads();
-        if (tid < 256) {
-            int sum = 0;
+    // four(t): the ranks of tokens t .. t + 3, 0 (no token's rank) for those from `older` on; t is a multiple of 4 below `upto`
+    const int upto = (older + 4 * kSelectThreads - 1) / (4 * kSelectThreads) * (4 * kSelectThreads);
+    auto choose = [&](auto four) {
+        // least: the rank of the lightest one picked; rest: how many of that rank are picked
+        uint32_t least = 0;
+        int rest = pick;
+        for (int shift = 24; shift >= 0; shift -= 8) {
+            for (int i = tid; i < 256 * kCopies; i += kSelectThreads) counts[i] = 0;
+            __syncthreads();
+            int *mine = counts + (lane & (kCopies - 1));
+#pragma unroll 2
+            for (int t = 4 * tid; t < upto; t += 4 * kSelectThreads) {
+                const u32x4 rank = four(t);
 #pragma unroll
-            for (int i = 0; i < kCopies; ++i) sum += counts[tid * kCopies + (i + tid) % kCopies];
-            counts[tid * kCopies] = sum;
-        }
-        __syncthreads();
-        if (tid < 64) {
-            // lane l holds the four highest digits from 255 - 4 l down
-            int mine[4], sum = 0;
-#pragma unroll
-            for (int i = 0; i < 4; ++i) sum += mine[i] = counts[(255 - 4 * lane - i) * kCopies];
-            int before = sum;
-#pragma unroll
-            for (int step = 1; step < 64; step *= 2) {
-                const int other = __shfl_up(before, step);
-                before += lane >= step ? other : 0;
+                for (int i = 0; i < 4; ++i)
+                    if (shift == 24 || (rank[i] ^ least) >> (shift + 8) == 0) atomicAdd(mine + (rank[i] >> shift & 255) * kCopies, 1);
             }
-            before -= sum;
+            __syncthreads();
+            if (tid < 256) {
+                int sum = 0;
+#pragma unroll
+                for (int i = 0; i < kCopies; ++i) sum += counts[tid * kCopies + (i + tid) % kCopies];
+                counts[tid * kCopies] = sum;
+            }
+            __syncthreads();
+            if (tid < 64) {
+                // lane l holds the four highest digits from 255 - 4 l down
+                int here[4], sum = 0;
+#pragma unroll
+                for (int i = 0; i < 4; ++i) sum += here[i] = counts[(255 - 4 * lane - i) * kCopies];
+                int before = (int)sum_upto((uint32_t)sum) - sum;
+#pragma unroll
+                for (int i = 0; i < 4; ++i) {
+                    if (before < rest && before + here[i] >= rest) {
+                        found_prefix = least | (uint32_t)(255 - 4 * lane - i) << shift;
+                        found_rest = rest - before;
+                    }
+                    before += here[i];
+                }
+            }
+            __syncthreads();
+            least = found_prefix;
+            rest = found_rest;
+        }
+
+        // every wavefront walks its stretch, 256 tokens at a time, once to count and once to write
+        const int steps = upto / 256, begin = steps * wave / kSelectWaves * 256, end = steps * (wave + 1) / kSelectWaves * 256;
+        int heavier = 0, ties = 0;
+#pragma unroll 2
+        for (int t = begin + 4 * lane; t < end; t += 256) {
+            const u32x4 rank = four(t);
 #pragma unroll
             for (int i = 0; i < 4; ++i) {
-                if (before < rest && before + mine[i] >= rest) {
-                    found_prefix = least | (uint32_t)(255 - 4 * lane - i) << shift;
-                    found_rest = rest - before;
-                }
-                before += mine[i];
+                heavier += rank[i] > least;
+                ties += rank[i] == least;
             }
         }
-        __syncthreads();
-        least = found_prefix;
-        rest = found_rest;
-    }
-
-    // an odd stretch each, so that the lanes' ranks are in different banks
-    const int stretch = ((older + kSelectThreads - 1) / kSelectThreads) | 1;
-    const int begin = tid * stretch < older ? tid * stretch : older, end = begin + stretch < older ? begin + stretch : older;
-    int heavier = 0, ties = 0;
-    for (int t = begin; t < end; ++t) {
-        const uint32_t rank = rank_at(t);
-        heavier += rank > least;
-        ties += rank == least;
-    }
-    auto before_me = [&](int mine, int *sums) {           // the sum of the threads before this one
-        int upto = mine;
-#pragma unroll
-        for (int step = 1; step < 64; step *= 2) {
-            const int other = __shfl_up(upto, step);
-            upto += lane >= step ? other : 0;
+        heavier = (int)lane_of(sum_upto((uint32_t)heavier), 63);
+        ties = (int)lane_of(sum_upto((uint32_t)ties), 63);
+        if (lane == 0) {
+            wave_sums[0][wave] = heavier;
+            wave_sums[1][wave] = ties;
         }
-        if (lane == 63) sums[wave] = upto;
         __syncthreads();
-        int before = upto - mine;
-        for (int w = 0; w < wave; ++w) before += sums[w];
-        return before;
-    };
-    const int ties_before = before_me(ties, wave_sums[0]);
-    int left = rest - ties_before;                        // of the ties that are picked
-    left = left < 0 ? 0 : left;
-    int place = before_me(heavier + (ties < left ? ties : left), wave_sums[1]);
-    for (int t = begin; t < end; ++t) {
-        const uint32_t rank = rank_at(t);
-        const bool tie = rank == least && left > 0;
-        left -= tie;
-        if (rank > least || tie) out[place++] = t;
-    }
-    for (int i = tid; i < late; i += kSelectThreads) out[pick + i] = older + i;
+        int place = 0, left = rest;                       // of the ties that are picked
+        for (int w = 0; w < wave; ++w) {
+            const int here = left < wave_sums[1][w] ? left : wave_sums[1][w];
+            place += wave_sums[0][w] + here;
+            left -= here;
+        }
+        for (int t = begin + 4 * lane; t < end; t += 256) {
+            const u32x4 rank = four(t);
+            bool picked[4];
+            int mine = 0;
+#pragma unroll
+            for (int i = 0; i < 4; ++i) picked[i] = rank[i] > least;
+            if (left > 0 && __ballot(rank[0] == least || rank[1] == least || rank[2] == least || rank[3] == least)) {
+                int tied = 0;
+#pragma unroll
+                for (int i = 0; i < 4; ++i) tied += rank[i] == least;
+                const int all = (int)sum_upto((uint32_t)tied);
+                int before = all - tied;
+#pragma unroll
+                for (int i = 0; i < 4; ++i)
+                    if (rank[i] == least) picked[i] = before++ < left;
+                const int here = (int)lane_of((uint32_t)all, 63);
+                left -= left < here ? left : here;
+            }
+#pragma unroll
+            for (int i = 0; i < 4; ++i) mine += picked[i];
+            const int all = (int)sum_upto((uint32_t)mine);
+            int *to = out + place + all - mine;
+#pragma unroll
+            for (int i = 0; i < 4; ++i)
+                if (picked[i]) *to++ = t + i;
+            place += (int)lane_of((uint32_t)all, 63);
+        }
+        for (int i = tid; i < late; i += kSelectThreads) out[pick + i] = older + i;
     };
     if (older <= kNearby) {
-        // a block per wavefront at a time, whose pages are looked up at once
-        const int blocks = (older + kBlock - 1) / kBlock;
-        for (int b0 = wave; b0 < blocks; b0 += 64 * kSelectWaves) {
-            const int mine = b0 + lane * kSelectWaves;
-            const uint32_t page = mine < blocks ? (uint32_t)table[mine] : 0u;
-#pragma unroll 8
-            for (int i = 0; i < 64; ++i) {
-                const int b = b0 + i * kSelectWaves;
-                if (b >= blocks) break;
-                const uint32_t here = (uint32_t)__builtin_amdgcn_readlane((int)page, i);
-                ranks[b * kBlock + lane] = here < c.pages ? rank_of(c.weights[weight_at(c, here, head) + lane]) : ~0u;
-            }
+        // A wavefront's blocks, whose pages are looked up at once, and all their weights are on their way together.
+        constexpr int kMost = kNearby / kBlock / kSelectWaves;
+        static_assert(kMost <= 64 && kMost * kBlock * kSelectWaves == kNearby && kNearby % (4 * kSelectThreads) == 0, "blocks of a wavefront");
+        const int blocks = (older + kBlock - 1) / kBlock, mine = wave + lane * kSelectWaves;
+        const uint32_t page = mine < blocks ? (uint32_t)table[mine] : ~0u;
+        float w[kMost];
+#pragma unroll
+        for (int i = 0; i < kMost; ++i) {
+            const uint32_t here = lane_of(page, i);
+            if (here < c.pages) w[i] = c.weights[weight_at(c, here, head) + lane];
+        }
+#pragma unroll
+        for (int i = 0; i < kMost; ++i) {
+            const uint32_t here = lane_of(page, i);
+            const int b = wave + i * kSelectWaves, t = b * kBlock + lane;
+            if (b * kBlock < upto) ranks[t] = t >= older ? 0u : (here < c.pages ? rank_of(w[i]) : ~0u);
         }
         __syncthreads();
-        choose([&](int t) { return ranks[t]; });
+        choose([&](int t) { return *reinterpret_cast<const u32x4 *>(ranks + t); });
     } else {
         choose([&](int t) {
-            const uint32_t page = (uint32_t)table[t / kBlock];
-            return page < c.pages ? rank_of(c.weights[weight_at(c, page, head) + t % kBlock]) : ~0u;
+            u32x4 rank = {0u, 0u, 0u, 0u};
+            if (t < older) {
+                const uint32_t page = (uint32_t)table[t / kBlock];
+                if (page < c.pages) {
+                    const f32x4 w = *reinterpret_cast<const f32x4 *>(c.weights + weight_at(c, page, head) + t % kBlock);
+                    rank = u32x4{rank_of(w.x), rank_of(w.y), rank_of(w.z), rank_of(w.w)};
+                } else {
+                    rank = ~rank;
+                }
+#pragma unroll
+                for (int i = 1; i < 4; ++i) rank[i] = t + i < older ? rank[i] : 0u;
+            }
+            return rank;
         });
     }
 }
@@ -175,15 +209,21 @@ __global__ __launch_bounds__(kTileThreads) void spqt_kv_move_kernel(Cache c, int
     __syncthreads();
     uint32_t pair = 0;
     if (which == 0) {
-        for (int p = (int)threadIdx.x; p < to * (D / 8); p += kTileThreads) {
-            const int i = p / (D / 8), d = p % (D / 8) * 8;
-            const u32x2 bytes = *reinterpret_cast<const u32x2 *>(c.codes + codes_at(c, pages[i], head, 0) + tokens[i] * D + d);
+        u32x2 bytes[D / 32];
+#pragma unroll
+        for (int n = 0; n < D / 32; ++n) {
+            const int p = (int)threadIdx.x + n * kTileThreads, i = p / (D / 8);
+            bytes[n] = *reinterpret_cast<const u32x2 *>(c.codes + codes_at(c, pages[i], head, 0) + tokens[i] * D + p % (D / 8) * 8);
+        }
+#pragma unroll
+        for (int n = 0; n < D / 32; ++n) {
+            const int p = (int)threadIdx.x + n * kTileThreads, i = p / (D / 8);
             u32x4 x;
 #pragma unroll
             for (int j = 0; j < 4; ++j)
-                x[j] = values_of<BF16>(bytes[j / 2] >> (16 * (j % 2)) & 255, bytes[j / 2] >> (16 * (j % 2) + 8) & 255, scales[i]);
-            tile.put(i, d, x);
-            pair = larger_pair(larger_pair(pair, x.x), larger_pair(x.y, larger_pair(x.z, x.w)));
+                x[j] = values_of<BF16>(bytes[n][j / 2] >> (16 * (j % 2)) & 255, bytes[n][j / 2] >> (16 * (j % 2) + 8) & 255, scales[i]);
+            tile.put(i, p % (D / 8) * 8, x);
+            if (i < to) pair = larger_pair(larger_pair(pair, x.x), larger_pair(x.y, larger_pair(x.z, x.w)));
         }
     } else {
         // a token per lane: those that lie in one page have their bytes of an element in one line
@@ -219,7 +259,7 @@ extern "C" int spqt_kv_evict(const spqt_kv_cache *cache, int keep, int recent, c
     if (keep > 1 << 30 || new_blocks < 1 || new_blocks > 1 << 24 || (int64_t)new_blocks * kBlock < keep) return SPQT_ESHAPE;
     if ((uintptr_t)new_table % 4 != 0 || (uintptr_t)new_lengths % 4 != 0 || (uintptr_t)kept % 4 != 0) return SPQT_EALIGN;
     // as many ranks in shared memory as the sequences' tables have room for
-    const int64_t room = (int64_t)cache->max_blocks * kBlock;
+    const int64_t room = ((int64_t)cache->max_blocks * kBlock + 4 * kSelectThreads - 1) / (4 * kSelectThreads) * (4 * kSelectThreads);
     const size_t bytes = (size_t)(room < kNearby ? room : kNearby) * 4;
     hipLaunchKernelGGL(spqt_kv_select_kernel, dim3(cache->kv_heads, cache->sequences), dim3(kSelectThreads), bytes, (hipStream_t)stream, view(*cache), keep, recent,
                        new_lengths, kept);

@@ -37,21 +37,6 @@ __device__ __forceinline__ Span span_of(const Cache &c, const Call &a, int s) {
     return v;
 }
 
-// Lane l's value of lanes 0 .. l together; lane 63 has all.
-template <class F>
-__device__ __forceinline__ uint32_t over_lanes(uint32_t v, F f) {
-    v = f(v, (uint32_t)__builtin_amdgcn_update_dpp(0, (int)v, 0x111, 0xf, 0xf, false));      // row_shr:1
-    v = f(v, (uint32_t)__builtin_amdgcn_update_dpp(0, (int)v, 0x112, 0xf, 0xf, false));
-    v = f(v, (uint32_t)__builtin_amdgcn_update_dpp(0, (int)v, 0x114, 0xf, 0xf, false));
-    v = f(v, (uint32_t)__builtin_amdgcn_update_dpp(0, (int)v, 0x118, 0xf, 0xf, false));
-    v = f(v, (uint32_t)__builtin_amdgcn_update_dpp(0, (int)v, 0x142, 0xa, 0xf, false));      // row_bcast:15
-    return f(v, (uint32_t)__builtin_amdgcn_update_dpp(0, (int)v, 0x143, 0xc, 0xf, false));   // row_bcast:31
-}
-__device__ __forceinline__ uint32_t sum_upto(uint32_t v) {
-    return over_lanes(v, [](uint32_t x, uint32_t y) { return x + y; });
-}
-__device__ __forceinline__ uint32_t lane_of(uint32_t v, int lane) { return (uint32_t)__builtin_amdgcn_readlane((int)v, lane); }
-
 // Attention of up to 16 rows (of one kv head and sequence) over some of its blocks, by one wavefront: the running statistics and sums.
 template <int D, bool BF16>
 struct Wave {

@@ -459,6 +459,7 @@ EVICTIONS = [
     (2, 192, "float16", [190, 500], 250, 7),
     (8, 64, "float16", [3000, 2049, 1024], 1111, 64),
     (1, 128, "float16", [1025], 1024, 0),
+    (1, 64, "bfloat16", [40000, 33001], 5000, 100),    # more than the selection holds in shared memory
 ]
 
 

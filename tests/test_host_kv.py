@@ -32,7 +32,7 @@ def rows(data=1 << 20, sequence=256, row=256, head=128):
 BAD_CACHES = [(dict(codes=None), EINVAL), (dict(scales=None), EINVAL), (dict(table=None), EINVAL), (dict(lengths=None), EINVAL), (dict(type=2), EINVAL),
               (dict(pages=0), ESHAPE), (dict(pages=1 << 31), ESHAPE), (dict(sequences=0), ESHAPE), (dict(sequences=65536), ESHAPE), (dict(max_blocks=0), ESHAPE),
               (dict(kv_heads=0), ESHAPE), (dict(kv_heads=16385), ESHAPE), (dict(head_dim=96), ESHAPE), (dict(head_dim=0), ESHAPE), (dict(head_dim=320), ESHAPE),
-              (dict(codes=(1 << 20) + 8), EALIGN), (dict(scales=(1 << 20) + 4), EALIGN), (dict(table=(1 << 20) + 2), EALIGN)]
+              (dict(codes=(1 << 20) + 8), EALIGN), (dict(scales=(1 << 20) + 4), EALIGN), (dict(table=(1 << 20) + 2), EALIGN), (dict(weights=(1 << 20) + 4), EALIGN)]
 BAD_ROWS = [(dict(data=None), EINVAL), (dict(head=-8), EINVAL), (dict(data=(1 << 20) + 2), EALIGN), (dict(row=132), EALIGN)]
 
 
