@@ -38,7 +38,7 @@ __device__ __forceinline__ Span span_of(const Cache &c, const Call &a, int s) {
 }
 
 // Attention of up to 16 rows (of one kv head and sequence) over some of its blocks, by one wavefront: the running statistics and sums.
-template <int D, bool BF16>
+template <int D, bool BF16, bool STREAM>
 struct Wave {
     f16x8 q[D / 32];
     Row row;
@@ -47,18 +47,22 @@ struct Wave {
     f32x4 acc[D / 16];
     u32x4 k[4][D / 64], v[D / 16];
 
+    __device__ __forceinline__ static u32x4 sixteen(const uint8_t *from) {
+        const u32x4 *p = reinterpret_cast<const u32x4 *>(from);
+        return STREAM ? __builtin_nontemporal_load(p) : *p;
+    }
     // The codes of a page; `on` 0: sixteen bytes of it over and over, for the last block's successor.
     __device__ __forceinline__ void fetch_keys(const uint8_t *page, uint32_t on, int lane) {
         const uint32_t at = (uint32_t)((lane & 15) * D + 16 * (lane >> 4)) & on, step = (uint32_t)D & on;
 #pragma unroll
         for (int t = 0; t < 4; ++t)
 #pragma unroll
-            for (int j = 0; j < D / 64; ++j) k[t][j] = *reinterpret_cast<const u32x4 *>(page + (at + 16 * t * step) + (on ? 64 * j : 0));
+            for (int j = 0; j < D / 64; ++j) k[t][j] = sixteen(page + (at + 16 * t * step) + (on ? 64 * j : 0));
     }
     __device__ __forceinline__ void fetch_values(const uint8_t *page, uint32_t on, int lane) {
         const uint32_t at = (uint32_t)((lane & 15) * kBlock + 16 * (lane >> 4)) & on;
 #pragma unroll
-        for (int i = 0; i < D / 16; ++i) v[i] = *reinterpret_cast<const u32x4 *>(page + at + 16 * i * kBlock);
+        for (int i = 0; i < D / 16; ++i) v[i] = sixteen(page + at + 16 * i * kBlock);
     }
     // One block, whose codes have been fetched; the next one's are requested as soon as the registers are free.
     __device__ __forceinline__ void block(int number, float scale_k, float scale_v, const uint8_t *next, uint32_t on, int lane) {
@@ -199,7 +203,7 @@ struct Wave {
 //   - otherwise all units' blocks, in order, are divided evenly, so that workgroups end together whatever the lengths are.
 // A workgroup's blocks are divided evenly among its wavefronts.  A unit that lies within one wavefront's share is written by it; the parts of one that lies
 // within one workgroup's meet in shared memory; those of a longer one in the workspace, where the workgroup that comes last joins them, in order.
-template <int D, bool BF16>
+template <int D, bool BF16, bool STREAM>
 __global__ __launch_bounds__(step_threads(D)) void spqt_kv_step_kernel(Cache c, Call a, Space space, int sequences, int tiles) {
     constexpr int kStepWaves = step_threads(D) / 64;
     constexpr uint32_t kLongest = 4 * kStepWaves;         // blocks of a unit that is not divided where blocks are few
@@ -310,7 +314,7 @@ __global__ __launch_bounds__(step_threads(D)) void spqt_kv_step_kernel(Cache c, 
     auto tile_of = [&](const Place &p) { return tiles == 1 ? 0 : (int)(p.unit % (uint32_t)tiles); };
     auto head_of = [&](const Place &p) { return tiles == 1 ? (int)p.unit : (int)(p.unit / (uint32_t)tiles); };
 
-    Wave<D, BF16> w;
+    Wave<D, BF16, STREAM> w;
     // the rows' sums so far, in units of 2^top, to this wavefront's place in shared memory
     auto put_down = [&]() {
         const float total = columns_sum(w.total), drop = w.unit * (1.0f / kLift);
@@ -527,9 +531,16 @@ void launch_step(const spqt_kv_cache &cache, const Call &a, void *counters, void
     s.arrived = (uint32_t *)counters;
     s.stats = (float *)space;
     s.sums = s.stats + 2 * kShares * 32;
+    // Codes that are read past the caches where they have room for more than half of the 256 MB cache: 131000 tokens of 70B heads 62.4 / 57.0 us, 40 sequences of up
+    // to 9500 tokens of 8B heads 76.8 / 73.9; less than that may still be there from the last call, 4095 tokens of 7B heads 14.7 / 15.0, 13B drafts 22.9 / 23.7.
+    const bool streams = (int64_t)cache.sequences * cache.max_blocks * cache.kv_heads * cache.head_dim * 2 * kBlock > (int64_t)128 << 20;
     dispatch(cache, [&](auto dim, auto bf16) {
         constexpr int D = decltype(dim)::value;
-        hipLaunchKernelGGL((spqt_kv_step_kernel<D, decltype(bf16)::value>), dim3(kShares), dim3(step_threads(D)), 0, stream, view(cache), a, s, cache.sequences, tiles);
+        auto launch = [&](auto kernel) {
+            hipLaunchKernelGGL(kernel, dim3(kShares), dim3(step_threads(D)), 0, stream, view(cache), a, s, cache.sequences, tiles);
+        };
+        if (streams) launch(spqt_kv_step_kernel<D, decltype(bf16)::value, true>);
+        else launch(spqt_kv_step_kernel<D, decltype(bf16)::value, false>);
     });
 }
 
