@@ -196,17 +196,18 @@ struct Wave {
     }
 };
 
-// Up to 16 rows of a kv head and sequence, a unit, share one pass over its blocks.  The blocks of all units are dealt out to the workgroups in one of two
-// ways, which all workgroups work out from the lengths:
-//   - few blocks: every workgroup takes up to `each` blocks of ONE unit, a block or a few for each of its wavefronts.  Units that are short go to one
-//     workgroup, since joining the sums of several costs some 4 us, as long as a wavefront takes for several blocks;
+// Up to 16 rows of a kv head and sequence, a unit, share one pass over its blocks.  The blocks of all units are dealt out to at most 256 workgroups in one of
+// three ways, which all workgroups work out from the lengths:
+//   - short units, up to four blocks for each of a workgroup's wavefronts, go to a workgroup each if there is one for every unit: joining the sums of
+//     several workgroups costs some 4 us, as long as a wavefront takes for several blocks;
+//   - where units can be divided into even parts of at most a quarter more than their share of a workgroup, every workgroup takes such a part;
 //   - otherwise all units' blocks, in order, are divided evenly, so that workgroups end together whatever the lengths are.
 // A workgroup's blocks are divided evenly among its wavefronts.  A unit that lies within one wavefront's share is written by it; the parts of one that lies
 // within one workgroup's meet in shared memory; those of a longer one in the workspace, where the workgroup that comes last joins them, in order.
 template <int D, bool BF16, bool STREAM>
 __global__ __launch_bounds__(step_threads(D)) void spqt_kv_step_kernel(Cache c, Call a, Space space, int sequences, int tiles) {
     constexpr int kStepWaves = step_threads(D) / 64;
-    constexpr uint32_t kLongest = 4 * kStepWaves;         // blocks of a unit that is not divided where blocks are few
+    constexpr uint32_t kLongest = 4 * kStepWaves;         // blocks of a unit that is not divided
     __shared__ float sums[kStepWaves][16][D + 4];
     __shared__ float stats[kStepWaves][2][16];
     __shared__ uint32_t order[2];
@@ -217,25 +218,41 @@ __global__ __launch_bounds__(step_threads(D)) void spqt_kv_step_kernel(Cache c, 
     Span nearby = {0, 0, 0, 0};
     if (lane < sequences) nearby = span_of(c, a, lane);
     auto blocks_from = [&](int s0) { return s0 == 0 ? (uint32_t)nearby.blocks : (s0 + lane < sequences ? (uint32_t)span_of(c, a, s0 + lane).blocks : 0u); };
-    uint32_t all = 0, most = 0, in_steps = 0;             // blocks, the longest unit's, and in whole steps of the workgroup's wavefronts
+    uint32_t all = 0, most = 0;                           // blocks, and the longest unit's
     for (int s0 = 0; s0 < sequences; s0 += 64) {
         const uint32_t n = blocks_from(s0);
         all += lane_of(sum_upto(n), 63);
-        in_steps += lane_of(sum_upto((n + kStepWaves - 1) / kStepWaves), 63);
         const uint32_t longest = lane_of(over_lanes(n, [](uint32_t x, uint32_t y) { return x > y ? x : y; }), 63);
         most = longest > most ? longest : most;
     }
     all *= units_each;
-    const bool few = in_steps * units_each <= (uint32_t)kShares;          // (in_steps <= all: no overflow either)
-    uint32_t each = kStepWaves;                                           // blocks of a workgroup
-    if (few && most <= kLongest)
-        while (each < most) each *= 2;                                    // (a power of two of them, as the division below is by one)
-    // places in the order of all units: workgroups' shares where blocks are few, blocks otherwise
-    auto size_of = [&](uint32_t n) { return few ? (n + each - 1) / each : n; };
-    uint32_t shares, more = 0;
-    if (few) {
-        shares = (each > kStepWaves ? (uint32_t)sequences : in_steps) * units_each;
+    // workgroups, if each has at most this many blocks of one unit (all of it or an even part)
+    auto parts_of = [&](uint32_t n, uint32_t each) { return (n + each - 1) / each; };
+    auto groups_with = [&](uint32_t each) {
+        uint32_t n = 0;
+        for (int s0 = 0; s0 < sequences; s0 += 64) n += lane_of(sum_upto(s0 + lane < sequences ? parts_of(blocks_from(s0), each) : 0u), 63);
+        return n * units_each;
+    };
+    uint32_t each, shares;
+    bool aligned;
+    if (most <= kLongest && (uint32_t)sequences * units_each <= (uint32_t)kShares && all <= kShares * kStepWaves) {
+        each = most;
+        shares = (uint32_t)sequences * units_each;
+        aligned = true;
     } else {
+        each = (all + kShares - 1) / kShares;
+        if (each < kStepWaves) each = kStepWaves;
+        const uint32_t limit = each + each / 4;
+        do {
+            shares = groups_with(each);
+            aligned = shares <= (uint32_t)kShares;
+            if (!aligned) each += each / 16 + 1;
+        } while (!aligned && each <= limit);
+    }
+    // places in the order of all units: workgroups where each has blocks of one unit, blocks otherwise
+    auto size_of = [&](uint32_t n) { return aligned ? parts_of(n, each) : n; };
+    uint32_t more = 0;
+    if (!aligned) {
         shares = all < kShares * kStepWaves ? (all + kStepWaves - 1) / kStepWaves : (uint32_t)kShares;
         each = all / shares;
         more = all % shares;                                              // so many workgroups have one block more
@@ -289,16 +306,18 @@ __global__ __launch_bounds__(step_threads(D)) void spqt_kv_step_kernel(Cache c, 
         }
     };
 
-    // this workgroup's blocks and the unit that the first one is of; few blocks are counted from their unit's start
+    // this workgroup's blocks and the unit that the first one is of; those of one unit are counted from its start
+    auto even_part = [](uint32_t n, uint32_t part, uint32_t parts) { return n / parts * part + (part < n % parts ? part : n % parts); };
     Place group_first;
     uint32_t group_begin, group_end, from = 0, to = 0;                    // from .. to: the workgroups of that unit, if all of this one's blocks are of it
     bool one_unit;
-    if (few) {
+    if (aligned) {
         group_first = find(blockIdx.x);
+        const uint32_t blocks = (uint32_t)group_first.span.blocks, parts = parts_of(blocks, each);
         from = group_first.start;
-        to = from + size_of((uint32_t)group_first.span.blocks) - 1;
-        group_begin = (blockIdx.x - from) * each;
-        group_end = group_begin + each < (uint32_t)group_first.span.blocks ? group_begin + each : (uint32_t)group_first.span.blocks;
+        to = from + parts - 1;
+        group_begin = even_part(blocks, blockIdx.x - from, parts);
+        group_end = even_part(blocks, blockIdx.x - from + 1, parts);
         group_first.start = 0;
         one_unit = true;
     } else {
@@ -454,7 +473,7 @@ __global__ __launch_bounds__(step_threads(D)) void spqt_kv_step_kernel(Cache c, 
     // A device-scope store has reached every XCD when it is acknowledged; the counters are raised after all threads' stores are.
     asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
     __syncthreads();
-    const uint32_t first_from = few ? from : share_of(group_first.start), last_from = few ? 0u : share_of(group_last.start);
+    const uint32_t first_from = aligned ? from : share_of(group_first.start), last_from = aligned ? 0u : share_of(group_last.start);
     if (threadIdx.x == 0) {
         if (first_meets) order[0] = __hip_atomic_fetch_add(space.arrived + first_from, 1u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
         if (last_meets) order[1] = __hip_atomic_fetch_add(space.arrived + last_from, 1u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
@@ -475,7 +494,7 @@ __global__ __launch_bounds__(step_threads(D)) void spqt_kv_step_kernel(Cache c, 
 #pragma unroll
             for (int j = 0; j < kAhead; ++j) {
                 const uint32_t g = g0 + j * helpers <= to ? g0 + j * helpers : to;
-                const size_t slot = 2 * (size_t)g + (!few && begin_of(g) < u.start ? 1 : 0);
+                const size_t slot = 2 * (size_t)g + (!aligned && begin_of(g) < u.start ? 1 : 0);
                 stat[j] = get_word(space.stats + (slot * 16 + row) * 2);
 #pragma unroll
                 for (int d = 0; d < kPart / 2; ++d) y[j][d] = get_word(space.sums + (slot * 16 + row) * D + my_d + 2 * d);
@@ -510,7 +529,7 @@ __global__ __launch_bounds__(step_threads(D)) void spqt_kv_step_kernel(Cache c, 
         }
         if (my_row < rows) write_part(u, row, m, x);
     };
-    if (first_meets) join(group_first, order[0], first_from, few ? to : share_of(first_stop - 1));
+    if (first_meets) join(group_first, order[0], first_from, aligned ? to : share_of(first_stop - 1));
     if (last_meets) join(group_last, order[1], last_from, share_of(group_last.start + (uint32_t)group_last.span.blocks - 1));
 }
 
