@@ -147,23 +147,22 @@ __global__ __launch_bounds__(Shape<D>::kThreads) void spqt_kv_prompt_kernel(Cach
 
     // Pages and scales of 64 blocks from `base` on, one per lane: looked up rarely, so that no turn waits for a chain of loads.
     const int32_t *table = c.table + (size_t)s * c.max_blocks + begin;
-    uint32_t pages = 0;
-    float scales[2] = {0.0f, 0.0f};
+    uint32_t places = 0;                                      // of the page and head among all pages' heads: their codes are within the memory there is
+    float scales_k = 0.0f, scales_v = 0.0f, inverses_v = 0.0f;
     int base = 0;
     auto look_up = [&](int b) {
         base = b;
         const int at = b + lane < n ? b + lane : n - 1;
-        pages = (uint32_t)table[at];
-        const bool there = pages < c.pages;
-        if (!there) pages = 0;
-#pragma unroll
-        for (int which = 0; which < 2; ++which) {
-            scales[which] = c.scales[scale_at(c, pages, head, which)];
-            if (!there) scales[which] = __builtin_nanf("");
-        }
+        uint32_t page = (uint32_t)table[at];
+        const bool there = page < c.pages;
+        if (!there) page = 0;
+        places = page * (uint32_t)c.kv_heads + (uint32_t)head;
+        scales_k = there ? c.scales[scale_at(c, page, head, 0)] : __builtin_nanf("");
+        scales_v = there ? c.scales[scale_at(c, page, head, 1)] : __builtin_nanf("");
+        inverses_v = 1.0f / scales_v;
     };
-    auto codes_of = [&](int b) { return c.codes + codes_at(c, (uint32_t)__builtin_amdgcn_readlane((int)pages, b - base), head, 0); };
-    auto scale_of = [&](int b, int which) { return as_float((uint32_t)__builtin_amdgcn_readlane((int)as_u32(scales[which]), b - base)); };
+    auto codes_of = [&](int b) { return c.codes + (size_t)lane_of(places, b - base) * (2 * kBlock * D); };
+    auto scalar = [&](float v, int b) { return as_float(lane_of(as_u32(v), b - base)); };
 
     f32x16 p[2];
     f16x8 lifted[4];
@@ -192,7 +191,7 @@ __global__ __launch_bounds__(Shape<D>::kThreads) void spqt_kv_prompt_kernel(Cach
             __builtin_amdgcn_sched_barrier(0);
         }
     };
-    auto probabilities = [&](int block, float scale_k, float scale_v, auto masked) {
+    auto probabilities = [&](int block, float scale_k, float scale_v, float inverse_v, auto masked) {
         const float by = scale * scale_k;
         if (decltype(masked)::value) {
 #pragma unroll
@@ -216,7 +215,7 @@ __global__ __launch_bounds__(Shape<D>::kThreads) void spqt_kv_prompt_kernel(Cach
         top = most;
         total *= shrink;
         if (sees) {
-            shrink *= unit / scale_v;
+            shrink *= unit * inverse_v;
             unit = scale_v;
         }
         const float lifted_from = 15.0f - from;
@@ -266,10 +265,10 @@ __global__ __launch_bounds__(Shape<D>::kThreads) void spqt_kv_prompt_kernel(Cach
             __builtin_amdgcn_s_setprio(0);
             meet();
             if (b + 3 - base >= 64) look_up(b);
-            const float scale_k = scale_of(b, 0), scale_v = scale_of(b, 1);
+            const float scale_k = scalar(scales_k, b), scale_v = scalar(scales_v, b), inverse_v = scalar(inverses_v, b);
             const int block = begin + b;
-            if (block * kBlock >= full_low && block * kBlock + kBlock - 1 <= full_high) probabilities(block, scale_k, scale_v, std::false_type());
-            else probabilities(block, scale_k, scale_v, std::true_type());
+            if (block * kBlock >= full_low && block * kBlock + kBlock - 1 <= full_high) probabilities(block, scale_k, scale_v, inverse_v, std::false_type());
+            else probabilities(block, scale_k, scale_v, inverse_v, std::true_type());
             stage(b + later);
             if (!later || b + 1 < n) meet();
         }
