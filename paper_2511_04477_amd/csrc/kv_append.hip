@@ -6,12 +6,12 @@ namespace {
 using namespace spqt;
 using namespace spqt::kv;
 
-// One workgroup per block that the call writes to, head and side (keys or values); the first one does the sequence's first and last block,
+// One workgroup per block that the call writes to, head and side (keys or values), the heads of a token one after the other as they lie in memory; the first one does the sequence's first and last block,
 // one after the other, since the first reads from the tail what the last one overwrites there.
 template <int D, bool BF16>
 __global__ __launch_bounds__(kTileThreads) void spqt_kv_append_kernel(Cache c, Rows keys, Rows values, int rows, const int32_t *counts) {
     __shared__ Tile<D> tile;
-    const int s = blockIdx.z, head = blockIdx.y >> 1, which = blockIdx.y & 1;
+    const int s = blockIdx.z, head = blockIdx.x >> 1, which = blockIdx.x & 1;
     const int length = length_of(c, s), count = count_of(counts, s, rows);
     if (length == 0 || count == 0) return;
     const int row0 = length - count, start = row0 < 0 ? 0 : row0;             // position of row 0, and of the first token that there is
@@ -21,8 +21,8 @@ __global__ __launch_bounds__(kTileThreads) void spqt_kv_append_kernel(Cache c, R
     uint16_t *tail = c.tail + (((size_t)s * c.kv_heads + head) * 2 + which) * (size_t)(kBlock * D);
     const int32_t *table = c.table + (size_t)s * c.max_blocks;
 
-    int block = first + (int)blockIdx.x;
-    if (blockIdx.x > 0 && block >= last) return;
+    int block = first + (int)blockIdx.y;
+    if (blockIdx.y > 0 && block >= last) return;
     for (;;) {
         const int base = block * kBlock;
         const int from = start > base ? start - base : 0, to = length - base < kBlock ? length - base : kBlock;
@@ -57,7 +57,7 @@ __global__ __launch_bounds__(kTileThreads) void spqt_kv_append_kernel(Cache c, R
             if (threadIdx.x == 0) *scales = scale;
             if (which == 0 && c.weights && (int)threadIdx.x >= from && (int)threadIdx.x < to) c.weights[weight_at(c, page, head) + threadIdx.x] = 0.0f;
         }
-        if (blockIdx.x > 0 || block == last) return;
+        if (blockIdx.y > 0 || block == last) return;
         block = last;
         __syncthreads();                           // the tile is free again
     }
@@ -69,9 +69,9 @@ template <int D, bool BF16>
 __global__ __launch_bounds__(kTileThreads) void spqt_kv_read_kernel(Cache c, Rows keys, Rows values, int rows, const int32_t *counts) {
     constexpr int kLine = kBlock / 4 + 1;                 // words of an element's tokens, and one
     __shared__ uint32_t codes[D * kLine];
-    const int s = blockIdx.z, head = blockIdx.y >> 1, which = blockIdx.y & 1;
+    const int s = blockIdx.z, head = blockIdx.x >> 1, which = blockIdx.x & 1;
     const int length = length_of(c, s), count = count_of(counts, s, rows), row0 = length - count;
-    const int block = block_of(row0) + (int)blockIdx.x, base = block * kBlock;
+    const int block = block_of(row0) + (int)blockIdx.y, base = block * kBlock;
     if (base - row0 >= rows) return;
     const Rows r = which ? values : keys;
     uint16_t *out = r.data + s * r.sequence + head * r.head;
@@ -133,7 +133,7 @@ extern "C" int spqt_kv_append(const spqt_kv_cache *cache, const spqt_kv_rows *k,
     const int rc = check_call(cache, true, k, v, rows, counts);
     if (rc != SPQT_OK) return rc;
     const int most = (rows + kBlock - 2) / kBlock + 1;                    // blocks that `rows` tokens can lie in
-    const dim3 grid(most > 2 ? most - 1 : 1, 2 * cache->kv_heads, cache->sequences);
+    const dim3 grid(2 * cache->kv_heads, most > 2 ? most - 1 : 1, cache->sequences);
     dispatch(*cache, [&](auto dim, auto bf16) {
         hipLaunchKernelGGL((spqt_kv_append_kernel<decltype(dim)::value, decltype(bf16)::value>), grid, dim3(kTileThreads), 0, (hipStream_t)stream, view(*cache),
                            view(*k), view(*v), rows, counts);
@@ -144,7 +144,7 @@ extern "C" int spqt_kv_append(const spqt_kv_cache *cache, const spqt_kv_rows *k,
 extern "C" int spqt_kv_read(const spqt_kv_cache *cache, const spqt_kv_rows *k_out, const spqt_kv_rows *v_out, int rows, const int32_t *counts, void *stream) {
     const int rc = check_call(cache, false, k_out, v_out, rows, counts);
     if (rc != SPQT_OK) return rc;
-    const dim3 grid((rows + kBlock - 2) / kBlock + 1, 2 * cache->kv_heads, cache->sequences);
+    const dim3 grid(2 * cache->kv_heads, (rows + kBlock - 2) / kBlock + 1, cache->sequences);
     dispatch(*cache, [&](auto dim, auto bf16) {
         hipLaunchKernelGGL((spqt_kv_read_kernel<decltype(dim)::value, decltype(bf16)::value>), grid, dim3(kTileThreads), 0, (hipStream_t)stream, view(*cache),
                            view(*k_out), view(*v_out), rows, counts);

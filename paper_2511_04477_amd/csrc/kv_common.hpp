@@ -151,7 +151,7 @@ inline int check_rows(const spqt_kv_rows *r) {
     if ((uintptr_t)r->data % 16 != 0 || r->sequence % 8 != 0 || r->row % 8 != 0 || r->head % 8 != 0) return SPQT_EALIGN;
     return SPQT_OK;
 }
-constexpr int kMaxRows = 1 << 24;
+constexpr int kMaxRows = 1 << 21;
 
 inline Cache view(const spqt_kv_cache &c) {
     return {(uint8_t *)c.codes, c.scales, (uint16_t *)c.tail, c.weights, c.table, c.lengths, (uint32_t)c.pages, c.max_blocks, c.kv_heads, c.head_dim};

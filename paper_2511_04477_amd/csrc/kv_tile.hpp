@@ -57,12 +57,34 @@ __device__ __forceinline__ void store_tile(const Cache &c, const Tile<D> &tile, 
     const float inverse = 1.0f / scale;
     uint8_t *out = c.codes + codes_at(c, page, head, which);
     if (which == 0) {
-        for (int p = from * (D / 8) + (int)threadIdx.x; p < to * (D / 8); p += kTileThreads) {
-            const u32x2 *x = reinterpret_cast<const u32x2 *>(&tile.v[p / (D / 8)][p % (D / 8) * 8]);
-            uint32_t c[8];
+        for (int p = from * (D / 16) + (int)threadIdx.x; p < to * (D / 16); p += kTileThreads) {
+            const u32x2 *x = reinterpret_cast<const u32x2 *>(&tile.v[p / (D / 16)][p % (D / 16) * 16]);
+            uint32_t c[16];
 #pragma unroll
-            for (int i = 0; i < 8; ++i) c[i] = coded(half_of<BF16>(x[i / 4][i / 2 % 2], i % 2), inverse);
-            *reinterpret_cast<u32x2 *>(out + p * 8) = u32x2{bytes_of(c[0], c[1], c[2], c[3], inverse), bytes_of(c[4], c[5], c[6], c[7], inverse)};
+            for (int i = 0; i < 16; ++i) c[i] = coded(half_of<BF16>(x[i / 4][i / 2 % 2], i % 2), inverse);
+            u32x4 w;
+#pragma unroll
+            for (int i = 0; i < 4; ++i) w[i] = bytes_of(c[4 * i], c[4 * i + 1], c[4 * i + 2], c[4 * i + 3], inverse);
+            *reinterpret_cast<u32x4 *>(out + p * 16) = w;
+        }
+        return;
+    }
+    if (from == 0 && to == kBlock) {                      // sixteen tokens of two elements at a time
+        for (int p = (int)threadIdx.x; p < D * 2; p += kTileThreads) {
+            const int d = p / 4 * 2, quarter = p % 4;
+            u32x4 w[2];
+#pragma unroll
+            for (int n = 0; n < 4; ++n) {
+                uint32_t x[4];
+#pragma unroll
+                for (int i = 0; i < 4; ++i) x[i] = *reinterpret_cast<const uint32_t *>(&tile.v[16 * n + 4 * quarter + i][d]);
+#pragma unroll
+                for (int e = 0; e < 2; ++e)
+                    w[e][n] = bytes_of(coded(half_of<BF16>(x[0], e), inverse), coded(half_of<BF16>(x[1], e), inverse), coded(half_of<BF16>(x[2], e), inverse),
+                                       coded(half_of<BF16>(x[3], e), inverse), inverse);
+            }
+#pragma unroll
+            for (int e = 0; e < 2; ++e) *reinterpret_cast<u32x4 *>(out + (d + e) * kBlock + 16 * quarter) = w[e];
         }
         return;
     }
