@@ -20,7 +20,7 @@ LIB = os.path.join(PKG, "libspqt.so")
 SOURCES = ["pack.cpp", "quant_cb.cpp", "gather.hip", "gemv.hip", "gemv_cb.hip", "gemv_cb8.hip", "gemv_cb2.hip", "gemv_list.hip",
            "gemv_bal.hip"]
 # The key/value cache: in libspqt.so only, since it has no reducers and no stamps.
-KV_SOURCES = ["kv_append.hip", "kv_attend.hip", "kv_step.hip", "kv_prompt.hip", "kv_evict.hip"]
+KV_SOURCES = ["kv_append.hip", "kv_attend.hip", "kv_step.hip", "kv_prompt.hip", "kv_weigh.hip", "kv_evict.hip"]
 CALIB_LIB = os.path.join(PKG, "libspqt_calib.so")       # benchmark-only helper kernels
 CALIB_SOURCES = ["calib.hip", "baseline_rowmajor.hip"]
 # The same kernels with wall-clock stamps per wavefront (python -m paper_2511_04477_amd.timeline).

@@ -162,6 +162,9 @@ bool is_prompt(int rows, int group);
 size_t prompt_bytes(int dim);
 void launch_prompt(const spqt_kv_cache &cache, const Call &a, void *space, hipStream_t stream);
 
+// What every token weighed in a call whose sums are known (kv_weigh.hip).
+void launch_weigh(const spqt_kv_cache &cache, const Call &a, hipStream_t stream);
+
 }  // namespace kv
 }  // namespace spqt
 #endif
