@@ -19,7 +19,7 @@ OBJ = os.path.join(PKG, "_build")
 LIB = os.path.join(PKG, "libspqt.so")
 SOURCES = ["pack.cpp", "quant_cb.cpp", "gather.hip", "gemv.hip", "gemv_cb.hip", "gemv_cb8.hip", "gemv_cb2.hip", "gemv_list.hip",
            "gemv_bal.hip"]
-# The key/value cache: in libspqt.so only, since it has no reducers and no stamps.
+# The key/value cache: one set of objects for all variants of the library, since it has neither their reducers nor their stamps.
 KV_SOURCES = ["kv_append.hip", "kv_attend.hip", "kv_step.hip", "kv_prompt.hip", "kv_weigh.hip", "kv_evict.hip"]
 CALIB_LIB = os.path.join(PKG, "libspqt_calib.so")       # benchmark-only helper kernels
 CALIB_SOURCES = ["calib.hip", "baseline_rowmajor.hip"]
@@ -97,6 +97,8 @@ def build(verbose: bool = False) -> str:
             _jobs(GIVEUP_LIB, GIVEUP_SOURCES, defines=("SPQT_TEST_GIVE_UP=1",), tag="gu_"),
             _jobs(HANDOVER_LIB, SOURCES, defines=("SPQT_TEST_HAND_OVER=1",), tag="ho_"),
             _jobs(LIB, SOURCES + KV_SOURCES)]
+    kv = [os.path.join(OBJ, os.path.splitext(s)[0] + ".o") for s in KV_SOURCES]
+    plan = [(cs, (lib, objs + kv if lib in (TIMELINE_LIB, HANDOVER_LIB) else objs)) for cs, (lib, objs) in plan]
     # every object of every library in one pool (longest first), then the links
     compiles = sorted((c for cs, _ in plan for c in cs), key=lambda c: -os.path.getsize(c[-1]))
     fastcall = FASTCALL_LIB + f".tmp{os.getpid()}"
