@@ -14,7 +14,7 @@ extern "C" int spqt_kv_workspace_bytes(int sequences, int rows, int q_heads, int
     if ((int64_t)rows * group > 1 << 28) return SPQT_ESHAPE;
     // one kind of call's partial sums or the other's
     size_t bytes = step_bytes(head_dim);
-    if (is_prompt(rows, group) && prompt_bytes(head_dim) > bytes) bytes = prompt_bytes(head_dim);
+    if (is_prompt(sequences, rows, group, kv_heads, head_dim, max_blocks) && prompt_bytes(head_dim) > bytes) bytes = prompt_bytes(head_dim);
     *out_bytes = kWorkspaceHead + kStepCounters + bytes;
     return SPQT_OK;
 }
@@ -32,7 +32,7 @@ extern "C" int spqt_kv_attention(const spqt_kv_cache *cache, const spqt_kv_rows 
     if ((uintptr_t)lse % 4 != 0 || (uintptr_t)counts % 4 != 0 || (uintptr_t)workspace % 256 != 0) return SPQT_EALIGN;
     if (workspace_bytes < need) return SPQT_ESIZE;
     const Call a = {view(*q), view(*out), lse, counts, rows, q_heads, q_heads / cache->kv_heads, window, scale, decay};
-    const bool prompt = is_prompt(rows, a.group);
+    const bool prompt = is_prompt(cache->sequences, rows, a.group, cache->kv_heads, cache->head_dim, cache->max_blocks);
     if (!prompt && !step_fits(*cache, a)) return SPQT_ESHAPE;
     char *counters = (char *)workspace + kWorkspaceHead, *space = counters + kStepCounters;
     if (prompt) launch_prompt(*cache, a, space, (hipStream_t)stream);

@@ -9,7 +9,8 @@ namespace kv {
 
 constexpr float kLog2e = 1.4426950408889634f, kLn2 = 0.6931471805599453f;
 constexpr float kNone = -__builtin_inff();
-// Probabilities go to the matrix instructions as two fp16 numbers, 22 bits in all, times 2^15: fp16's smallest number is 2^-39 of the largest one.
+// Probabilities go to the matrix instructions as fp16 numbers, two of them (22 bits in all) where rows are few and one (11 bits) where they are many, times 2^15: fp16's smallest
+// number is 2^-39 of the largest one.
 constexpr float kLift = 0x1p15f;
 
 struct Call {
@@ -158,7 +159,7 @@ bool step_fits(const spqt_kv_cache &cache, const Call &a);
 void launch_step(const spqt_kv_cache &cache, const Call &a, void *counters, void *space, hipStream_t stream);
 
 // Many rows (kv_prompt.hip): whether a call is of that kind, what such calls need of the workspace at most, and the call.
-bool is_prompt(int rows, int group);
+bool is_prompt(int sequences, int rows, int group, int kv_heads, int dim, int max_blocks);
 size_t prompt_bytes(int dim);
 void launch_prompt(const spqt_kv_cache &cache, const Call &a, void *space, hipStream_t stream);
 

@@ -200,7 +200,7 @@ struct Wave {
 // three ways, which all workgroups work out from the lengths:
 //   - short units, up to four blocks for each of a workgroup's wavefronts, go to a workgroup each if there is one for every unit: joining the sums of
 //     several workgroups costs some 4 us, as long as a wavefront takes for several blocks;
-//   - where units can be divided into even parts of at most a quarter more than their share of a workgroup, every workgroup takes such a part;
+//   - where units can be divided into even parts of at most half more than their share of a workgroup, every workgroup takes such a part;
 //   - otherwise all units' blocks, in order, are divided evenly, so that workgroups end together whatever the lengths are.
 // A workgroup's blocks are divided evenly among its wavefronts.  A unit that lies within one wavefront's share is written by it; the parts of one that lies
 // within one workgroup's meet in shared memory; those of a longer one in the workspace, where the workgroup that comes last joins them, in order.
@@ -242,7 +242,7 @@ __global__ __launch_bounds__(step_threads(D)) void spqt_kv_step_kernel(Cache c, 
     } else {
         each = (all + kShares - 1) / kShares;
         if (each < kStepWaves) each = kStepWaves;
-        const uint32_t limit = each + each / 4;
+        const uint32_t limit = each + each / 2;
         do {
             shares = groups_with(each);
             aligned = shares <= (uint32_t)kShares;
@@ -258,6 +258,8 @@ __global__ __launch_bounds__(step_threads(D)) void spqt_kv_step_kernel(Cache c, 
         more = all % shares;                                              // so many workgroups have one block more
     }
     if (blockIdx.x >= shares) return;
+    // Workgroups go to the 8 XCDs in turn: each gets a stretch of the order, so that the tiles of a head, which read the same blocks, share an L2.
+    const uint32_t xcd = blockIdx.x % 8, place = shares / 8 * xcd + (xcd < shares % 8 ? xcd : shares % 8) + blockIdx.x / 8;
     auto begin_of = [&](uint32_t g) { return g * each + (g < more ? g : more); };
     auto share_of = [&](uint32_t block) { return block < more * (each + 1) ? block / (each + 1) : more + (block - more * (each + 1)) / each; };
 
@@ -312,17 +314,17 @@ __global__ __launch_bounds__(step_threads(D)) void spqt_kv_step_kernel(Cache c, 
     uint32_t group_begin, group_end, from = 0, to = 0;                    // from .. to: the workgroups of that unit, if all of this one's blocks are of it
     bool one_unit;
     if (aligned) {
-        group_first = find(blockIdx.x);
+        group_first = find(place);
         const uint32_t blocks = (uint32_t)group_first.span.blocks, parts = parts_of(blocks, each);
         from = group_first.start;
         to = from + parts - 1;
-        group_begin = even_part(blocks, blockIdx.x - from, parts);
-        group_end = even_part(blocks, blockIdx.x - from + 1, parts);
+        group_begin = even_part(blocks, place - from, parts);
+        group_end = even_part(blocks, place - from + 1, parts);
         group_first.start = 0;
         one_unit = true;
     } else {
-        group_begin = begin_of(blockIdx.x);
-        group_end = begin_of(blockIdx.x + 1);
+        group_begin = begin_of(place);
+        group_end = begin_of(place + 1);
         group_first = find(group_begin);
         one_unit = group_end <= group_first.start + (uint32_t)group_first.span.blocks;
     }
@@ -418,7 +420,7 @@ __global__ __launch_bounds__(step_threads(D)) void spqt_kv_step_kernel(Cache c, 
     };
     auto publish_part = [&](const Meeting &m, const float (&x)[kPart]) {
         if (my_row >= live_rows(group_first)) return;
-        const size_t slot = 2 * (size_t)blockIdx.x;
+        const size_t slot = 2 * (size_t)place;
 #pragma unroll
         for (int d = 0; d < kPart; d += 2) put_word(space.sums + (slot * 16 + my_row) * D + my_d + d, x[d], x[d + 1]);
         if (threadIdx.x % kRowThreads == 0) put_word(space.stats + (slot * 16 + my_row) * 2, m.top, m.total);
@@ -457,7 +459,7 @@ __global__ __launch_bounds__(step_threads(D)) void spqt_kv_step_kernel(Cache c, 
             if (stop <= group_end) {
                 write_row(p, m, w.acc, 1.0f);
             } else if (column < live_rows(p)) {
-                const size_t slot = 2 * (size_t)blockIdx.x + 1;
+                const size_t slot = 2 * (size_t)place + 1;
 #pragma unroll
                 for (int i = 0; i < D / 16; ++i)
 #pragma unroll

@@ -427,6 +427,85 @@ def test_scales_that_are_not_positive(gpu, rows, scale):
     compare(gpu, c, q if scale >= 0 else -q, None, 100, out, lse, scale=abs(scale), weights=c.weights, before=torch.zeros(c.weights.shape))
 
 
+# More rows than a few whatever the tables have room for; and those that are a few unless the tables have much of it.
+MANY = [
+    (8, 1, 128, "float16", [2100], None, 70, 0),           # tokens in parts
+    (6, 1, 192, "bfloat16", [1100, 1030], [93, 60], 93, 0),
+    (4, 1, 256, "float16", [1300], None, 140, 0),
+    (4, 2, 64, "bfloat16", [1500, 30, 0, 800], [300, 30, 0, 1], 300, 300),
+    (8, 2, 64, "float16", [40], None, 150, 0),             # rows before the first token see nothing
+    (3, 3, 128, "bfloat16", [700], None, 600, 3),
+    (64, 8, 128, "bfloat16", [2100, 40], [66, 1], 66, 100),
+]
+EITHER = [c for c in CASES if 64 < c[6] * (c[0] // c[1]) <= 512]
+
+
+def widen(c):
+    """Room for some 2.5 million tokens in the tables."""
+    wide = c.torch.full((c.seqs, 40_000), -1, dtype=c.torch.int32, device="cuda")
+    wide[:, : c.max_blocks] = c.table
+    c.table = wide
+
+
+@pytest.mark.parametrize("case,wide", [(c, False) for c in MANY] + [(c, True) for c in EITHER], ids=lambda c: "-".join(str(x) for x in c).replace(" ", "") if isinstance(c, tuple) else None)
+def test_attention_of_many_rows(gpu, case, wide):
+    heads, kv_heads, dim, dtype, lengths, counts, rows, window = case
+    c, q = case_cache(gpu, case, 33)
+    few = attend(gpu, c, q, counts, window)
+    if wide:
+        widen(c)
+        compare(gpu, c, q, counts, window, *few)
+    c.weights.zero_()
+    before = c.weights.cpu()
+    out, lse = attend(gpu, c, q, counts, window, weigh=True)
+    compare(gpu, c, q, counts, window, out, lse, weights=c.weights, before=before)
+    again, lse_again = attend(gpu, c, q, counts, window)
+    assert out.equal(again) and lse.equal(lse_again)
+
+
+@pytest.mark.parametrize("wide", [False, True])
+def test_rows_beside_those_that_see_no_number(gpu, wide):
+    """A block that holds none, with rows in sixteens of which some see it, and with more rows than a few."""
+    torch, _ = gpu
+    c = Cache(gpu, 1, 2, 64, torch.bfloat16, 4, 41)
+    c.append(256)
+    q = torch.randn((1, 150, 4, 64), generator=c.gen).bfloat16().cuda()
+    if wide:
+        widen(c)
+    good, good_lse = attend(gpu, c, q, None)
+    for which in (0, 1):
+        scales = c.scales.clone()
+        c.scales[int(c.table_host[0, 2]), 1, which] = math.nan
+        out, lse = attend(gpu, c, q, None)
+        c.scales.copy_(scales)
+        hit = torch.zeros((150, 4), dtype=torch.bool, device="cuda")
+        hit[22:, 2:] = True                            # rows are at 106 .. 255
+        assert bool(out[0][hit].isnan().all())
+        assert out[0][~hit].equal(good[0][~hit]) and lse[0][~hit].equal(good_lse[0][~hit])
+
+
+@pytest.mark.parametrize("scale", [0.0, -0.3])
+def test_scales_that_are_not_positive_with_many_rows(gpu, scale):
+    torch, _ = gpu
+    c = Cache(gpu, 1, 2, 128, torch.float16, 3, 44)
+    c.append(150)
+    c.weights.zero_()
+    widen(c)
+    q = torch.randn((1, 40, 4, 128), generator=c.gen).half().cuda()
+    out, lse = attend(gpu, c, q, None, window=100, scale=scale, weigh=True)
+    compare(gpu, c, q if scale >= 0 else -q, None, 100, out, lse, scale=abs(scale), weights=c.weights, before=torch.zeros(c.weights.shape))
+
+
+def test_rows_of_sequences_that_cannot_be_divided_evenly(gpu):
+    """Three tiles of a head over blocks of very different numbers; workgroups that have parts of several units."""
+    for seqs, heads, kv_heads in ((5, 6, 1), (21, 3, 1), (70, 2, 2)):
+        lengths = [1 + 997 * (i * i + 3) % 1900 for i in range(seqs)]
+        case = (heads, kv_heads, 64, "float16", lengths, None, 8 if heads == 6 else 1, 0)
+        c, q = case_cache(gpu, case, 34)
+        out, lse = attend(gpu, c, q, None)
+        compare(gpu, c, q, None, 0, out, lse)
+
+
 def test_attention_over_pages_beyond_four_gigabytes(gpu):
     torch, spqt = gpu
     pages = 36_000                                     # 8 heads, 128: 128 KB a page, 4.7 GB
