@@ -20,8 +20,9 @@ constexpr int kNearby = 32768;                            // ranks in shared mem
 
 // One workgroup per sequence and head.  The rank of the lightest token that is kept is found eight bits at a time from counts of those bits, 16 copies of them
 // for the lanes to keep out of each other's way; then every thread walks a stretch of tokens in order, a kept one taking the next place.
-// What bounds it: one CU per sequence and head, for 6 passes over the tokens' ranks.  They stay in shared memory where there are at most 32768 of them (a wavefront reads
-// 4 bytes a token once); sequences of 27000 and 33001 tokens of 8 heads, 8192 kept, 24 us (read from memory in every pass: 78); 2300 of 32 heads, 2048 kept, 11 us.
+// What bounds it: one CU per sequence and head, for 6 passes over the tokens' ranks.  They stay in shared memory where there are at most 32768 of them (read
+// once, 4 bytes a token): sequences of 27000 and 33001 tokens of 8 heads, 8192 kept, 24 us, and 17 more if every pass reads them from memory, as it does beyond; 2300 of 32 heads,
+// 2048 kept, 10 us.
 __global__ __launch_bounds__(kSelectThreads) void spqt_kv_select_kernel(Cache c, int keep, int recent, int32_t *new_lengths, int32_t *kept) {
     extern __shared__ __attribute__((aligned(16))) uint32_t ranks[];
     __shared__ int counts[256 * kCopies];
@@ -141,23 +142,29 @@ __global__ __launch_bounds__(kSelectThreads) void spqt_kv_select_kernel(Cache c,
         for (int i = tid; i < late; i += kSelectThreads) out[pick + i] = older + i;
     };
     if (older <= kNearby) {
-        // A wavefront's blocks, whose pages are looked up at once, and all their weights are on their way together.
-        constexpr int kMost = kNearby / kBlock / kSelectWaves;
-        static_assert(kMost <= 64 && kMost * kBlock * kSelectWaves == kNearby && kNearby % (4 * kSelectThreads) == 0, "blocks of a wavefront");
+        // A wavefront's blocks, whose pages are looked up at once, and all their weights are on their way together.  Up to 8192 tokens a copy
+        // of the code has no steps for more: 2300 tokens of 32 heads 34.2 us for 35.3 (eviction and read), 4000 of 8 heads 22.2 for 23.3; from 9000 on 65.9 for 65.8.
         const int blocks = (older + kBlock - 1) / kBlock, mine = wave + lane * kSelectWaves;
         const uint32_t page = mine < blocks ? (uint32_t)table[mine] : ~0u;
-        float w[kMost];
+        auto fetch = [&](auto most) {
+            constexpr int kMost = decltype(most)::value;
+            float w[kMost];
 #pragma unroll
-        for (int i = 0; i < kMost; ++i) {
-            const uint32_t here = lane_of(page, i);
-            if (here < c.pages) w[i] = c.weights[weight_at(c, here, head) + lane];
-        }
+            for (int i = 0; i < kMost; ++i) {
+                const uint32_t here = lane_of(page, i);
+                if (here < c.pages) w[i] = c.weights[weight_at(c, here, head) + lane];
+            }
 #pragma unroll
-        for (int i = 0; i < kMost; ++i) {
-            const uint32_t here = lane_of(page, i);
-            const int b = wave + i * kSelectWaves, t = b * kBlock + lane;
-            if (b * kBlock < upto) ranks[t] = t >= older ? 0u : (here < c.pages ? rank_of(w[i]) : ~0u);
-        }
+            for (int i = 0; i < kMost; ++i) {
+                const uint32_t here = lane_of(page, i);
+                const int b = wave + i * kSelectWaves, t = b * kBlock + lane;
+                if (b * kBlock < upto) ranks[t] = t >= older ? 0u : (here < c.pages ? rank_of(w[i]) : ~0u);
+            }
+        };
+        constexpr int kAll = kNearby / kBlock / kSelectWaves, kFew = 8;
+        static_assert(kAll <= 64 && kAll * kBlock * kSelectWaves == kNearby && kNearby % (4 * kSelectThreads) == 0, "blocks of a wavefront");
+        if (upto <= kFew * kBlock * kSelectWaves) fetch(std::integral_constant<int, kFew>());
+        else fetch(std::integral_constant<int, kAll>());
         __syncthreads();
         choose([&](int t) { return *reinterpret_cast<const u32x4 *>(ranks + t); });
     } else {

@@ -13,6 +13,7 @@ typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
 constexpr int kThreads = 256, kWaves = kThreads / 64;
 
 // A few rows: a wavefront per block, which goes over all rows.
+// What bounds it: the keys, 16001 tokens of 2 sequences of 8 heads of 128 (33 MB, from the cache behind memory) 12.7 us = 2.6 TB/s, a start and one chain of loads per block.
 template <int D, bool BF16>
 __global__ __launch_bounds__(kThreads) void spqt_kv_weigh_few_kernel(Cache c, Call a) {
     const int s = blockIdx.z, head = blockIdx.y, lane = threadIdx.x & 63, column = lane & 15, quarter = lane >> 4;
@@ -67,7 +68,8 @@ __global__ __launch_bounds__(kThreads) void spqt_kv_weigh_few_kernel(Cache c, Ca
 
 // Many rows: a workgroup per block, whose wavefronts hold its keys as 16-bit numbers of the queries' type (a code is exact in either) and take every eighth (fourth)
 // 32 of the rows that see it.  With S^T = K Q^T a lane has one row and half of each 32 tokens; its tokens' sums meet at the end.
-// What bounds it: 32 exponentials and as many multiply-adds and additions a lane for 16 matrix instructions.
+// What bounds it: 32 exponentials and as many multiply-adds and additions a lane for 16 matrix instructions: 4001 rows of 32 / 8 heads from an empty cache 139 us, 1024 rows of 64 / 8
+// heads over 8192 tokens 196 us.
 constexpr int many_threads(int dim) { return dim > 128 ? 256 : 512; }
 
 template <int D, bool BF16>
