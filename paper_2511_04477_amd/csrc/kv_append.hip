@@ -71,7 +71,7 @@ __global__ __launch_bounds__(kTileThreads) void spqt_kv_append_kernel(Cache c, R
 // x = code * scale, rounded to the rows' type: the only rounding.
 // One workgroup per block that the call reads from, head and side.  Keys go straight through; values go through shared memory as they are, and come out
 // four tokens of eight elements at a time, so that a row's elements leave 16 bytes a lane.
-// What bounds it: 1 byte in and 2 out a value: the same 25.7k tokens (158 MB, with the rows' ends that it clears) 30.4 us = 5.2 TB/s; one token of 4 sequences 3.7 us.
+// What bounds it: 1 byte in and 2 out a value: the same 25.7k tokens (158 MB, and 42 MB of rows that it clears) 30.4 us = 6.6 TB/s; one token of 4 sequences 3.7 us.
 template <int D, bool BF16>
 __global__ __launch_bounds__(kTileThreads) void spqt_kv_read_kernel(Cache c, Rows keys, Rows values, int rows, const int32_t *counts) {
     constexpr int kLine = kBlock / 4 + 1;                 // words of an element's tokens, and one

@@ -7,7 +7,7 @@
 // Probabilities go to the matrix instructions as ONE fp16 number, off by up to 2^-12 of themselves: a second one would cost half as many matrix instructions again.  Against 64 bits
 // an fp16 output of 4001 rows is then 2.5e-4 off instead of the 2.1e-4 of its own rounding, a bf16 one no further than by its rounding (1.7e-3).  Sums stay in 32 bits.
 //
-// What bounds it: matrix and vector instructions of a SIMD side by side; a block takes a SIMD's two wavefronts 64 matrix instructions of 32 cycles and about 600 others, half of them
+// What bounds it: matrix and vector instructions of a SIMD side by side; a block takes a SIMD's two wavefronts 64 matrix instructions of 32 cycles and about 520 others, half of them
 // for the softmax.  1024 rows of 64 / 8 heads of 128 over 32768 tokens 1043 us = 1.04 PFLOP/s (an 8192^3 product: 1.2); 4001 rows of 32 / 8 heads from an empty cache 166 us = 792
 // TFLOP/s, since 504 workgroups of uneven length on 256 CUs leave some idle at the end.
 #include "kv_attend.hpp"
@@ -129,7 +129,7 @@ __global__ __launch_bounds__(Shape<D>::kThreads) void spqt_kv_prompt_kernel(Cach
     Row row = row_of(a, r, head, length, count);
     if (r >= rows) row.high = -1;
     f16x8 q[D / 16];
-    float scale, top = kNone, total = 0.0f, unit = 1.0f;
+    float scale, top = kNone, total = 0.0f, unit = 1.0f, shrink = 1.0f;
     {
         const bool live = row.high >= 0;
         const uint16_t *from = a.q.data + s * a.q.sequence + row.i * a.q.row + row.head * a.q.head;
@@ -174,12 +174,17 @@ __global__ __launch_bounds__(Shape<D>::kThreads) void spqt_kv_prompt_kernel(Cach
     f32x16 p[2];
     f16x8 lifted[4];
     // O += V P of the last block and S = K Q of this one: kProducts matrix instructions in a row, whose other operands are read kAhead ahead.
+    // A wavefront alone on its SIMD goes through the values 32 elements at a time and brings the next 32's sums to their new units beside those products: 4001 rows of 16 / 4 heads of
+    // 256 299 -> 227 us, of 192 184 -> 182.  Where two take turns the one that multiplies has no time for it: heads of 128 174 for 171, of 64 136 for 133.
     constexpr int kAhead = 6, kValueProducts = D / 8, kProducts = kValueProducts + D / 8;
+    constexpr bool kBeside = S::kWaves == 4;
+    auto tile_of = [](int i) { return kBeside ? i / 4 : i % (D / 32); };      // 32 elements and 16 tokens of the i-th product with values
+    auto sixteen_of = [](int i) { return kBeside ? i % 4 : i / (D / 32); };
     auto products = [&](const _Float16 *v, const _Float16 *k, auto skip, auto stop) {
         constexpr int from = decltype(skip)::value ? kValueProducts : 0, to = decltype(stop)::value ? kValueProducts : kProducts;
         f16x8 x[kAhead];
         auto read = [&](int i) {
-            if (i < kValueProducts) return *reinterpret_cast<const f16x8 *>(v + (i % (D / 32) * 32 + column) * S::kValueStride + i / (D / 32) * 16 + 8 * half);
+            if (i < kValueProducts) return *reinterpret_cast<const f16x8 *>(v + (tile_of(i) * 32 + column) * S::kValueStride + sixteen_of(i) * 16 + 8 * half);
             i -= kValueProducts;
             return *reinterpret_cast<const f16x8 *>(k + (i % 2 * 32 + column) * S::kKeyStride + i / 2 * 16 + 8 * half);
         };
@@ -189,7 +194,10 @@ __global__ __launch_bounds__(Shape<D>::kThreads) void spqt_kv_prompt_kernel(Cach
 #pragma unroll
         for (int i = from; i < to; ++i) {
             if (i < kValueProducts) {
-                acc[i % (D / 32)] = __builtin_amdgcn_mfma_f32_32x32x16_f16(x[i % kAhead], lifted[i / (D / 32)], acc[i % (D / 32)], 0, 0, 0);
+                acc[tile_of(i)] = __builtin_amdgcn_mfma_f32_32x32x16_f16(x[i % kAhead], lifted[sixteen_of(i)], acc[tile_of(i)], 0, 0, 0);
+                if (kBeside && i + 4 < kValueProducts)
+#pragma unroll
+                    for (int e = 4 * (i % 4); e < 4 * (i % 4) + 4; ++e) acc[i / 4 + 1][e] *= shrink;
             } else {
                 const int t = (i - kValueProducts) % 2, j = (i - kValueProducts) / 2;
                 p[t] = __builtin_amdgcn_mfma_f32_32x32x16_f16(x[i % kAhead], q[j], j == 0 ? f32x16{} : p[t], 0, 0, 0);
@@ -218,7 +226,7 @@ __global__ __launch_bounds__(Shape<D>::kThreads) void spqt_kv_prompt_kernel(Cach
         const bool sees = !decltype(masked)::value || !(most == kNone);
         most = __builtin_fmaxf(top, sees ? most * by : kNone);
         const float from = most == kNone ? 0.0f : most;
-        float shrink = __builtin_amdgcn_exp2f(top - from);
+        shrink = __builtin_amdgcn_exp2f(top - from);
         top = most;
         total *= shrink;
         if (sees) {
@@ -244,7 +252,7 @@ __global__ __launch_bounds__(Shape<D>::kThreads) void spqt_kv_prompt_kernel(Cach
             }
         total += sum * (1.0f / kLift);
 #pragma unroll
-        for (int i = 0; i < D / 32; ++i) acc[i] *= shrink;
+        for (int i = 0; i < (kBeside ? 1 : D / 32); ++i) acc[i] *= shrink;
     };
 
     if (n > 0) {

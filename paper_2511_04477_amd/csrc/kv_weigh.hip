@@ -13,7 +13,7 @@ typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
 constexpr int kThreads = 256, kWaves = kThreads / 64;
 
 // A few rows: a wavefront per block, which goes over all rows.
-// What bounds it: the keys, 16001 tokens of 2 sequences of 8 heads of 128 (33 MB, from the cache behind memory) 12.7 us = 2.6 TB/s, a start and one chain of loads per block.
+// What bounds it: the keys, 29300 tokens of 8 heads of 128 (30 MB, from the cache behind memory) 12.6 us = 2.4 TB/s: a start, one chain of loads and a tail per block.
 template <int D, bool BF16>
 __global__ __launch_bounds__(kThreads) void spqt_kv_weigh_few_kernel(Cache c, Call a) {
     const int s = blockIdx.z, head = blockIdx.y, lane = threadIdx.x & 63, column = lane & 15, quarter = lane >> 4;
