@@ -12,9 +12,9 @@ extern "C" int spqt_kv_workspace_bytes(int sequences, int rows, int q_heads, int
         return SPQT_ESHAPE;
     const int group = q_heads / kv_heads;
     if ((int64_t)rows * group > 1 << 28) return SPQT_ESHAPE;
-    // one kind of call's partial sums or the other's
+    // either kind of call's partial sums, whatever the room of the tables, so that a workspace for more sequences, rows or blocks serves less of them
     size_t bytes = step_bytes(head_dim);
-    if (is_prompt(sequences, rows, group, kv_heads, head_dim, max_blocks) && prompt_bytes(head_dim) > bytes) bytes = prompt_bytes(head_dim);
+    if ((int64_t)rows * group > kFewRows && prompt_bytes(head_dim) > bytes) bytes = prompt_bytes(head_dim);
     *out_bytes = kWorkspaceHead + kStepCounters + bytes;
     return SPQT_OK;
 }

@@ -159,6 +159,7 @@ bool step_fits(const spqt_kv_cache &cache, const Call &a);
 void launch_step(const spqt_kv_cache &cache, const Call &a, void *counters, void *space, hipStream_t stream);
 
 // Many rows (kv_prompt.hip): whether a call is of that kind, what such calls need of the workspace at most, and the call.
+constexpr int kFewRows = 64;                              // of a kv head, that are a few in any call
 bool is_prompt(int sequences, int rows, int group, int kv_heads, int dim, int max_blocks);
 size_t prompt_bytes(int dim);
 void launch_prompt(const spqt_kv_cache &cache, const Call &a, void *space, hipStream_t stream);

@@ -364,9 +364,10 @@ namespace kv {
 // Up to 64 rows of a kv head are a few.  Up to 512 are, in sixteens, where that makes few blocks to go through (with the room of the tables), at most as many as 20000 of 128
 // elements.  As a few / here, heads of 128: 80, 256 and 512 rows of each of 8 over 4000 tokens (2500, 8000, 16000 blocks) 16.4 / 38.4, 23.3 / 33.1, 31.3 / 36.6 us; 80, 128 and 256
 // over 32000 (20000, 32000, 64000) 41 / 63, 53 / 55, 95 / 53.  Heads of 192: 12500 blocks 37 / 46, 20000 61 / 43; of 256: 4000 33 / 42, 8000 47 / 47, 16000 61 / 49; of 64: 32000 35 / 46, 48000 58 / 47.
+// Sixteens of a few blocks have to have a workgroup each (their start and end count): 512 sixteens of 3 blocks 17.9 / 14.5, 800 of 5 22.5 / 21.1, 256 of 3 7.9 / 15.9; 320 of 16 25.2 / 36.0.
 bool is_prompt(int sequences, int rows, int group, int kv_heads, int dim, int max_blocks) {
-    const int64_t all = (int64_t)rows * group;
-    return all > 512 || (all > 64 && (int64_t)sequences * kv_heads * ((all + 15) / 16) * max_blocks > 20000 * 128 / dim);
+    const int64_t all = (int64_t)rows * group, units = (int64_t)sequences * kv_heads * ((all + 15) / 16);
+    return all > 512 || (all > kFewRows && ((units > 256 && max_blocks < 8) || units * max_blocks > 20000 * 128 / dim));
 }
 
 size_t prompt_bytes(int dim) { return (size_t)kParted * rows_of(dim) * (dim + 2) * 4; }

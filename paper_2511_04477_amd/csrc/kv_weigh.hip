@@ -218,7 +218,7 @@ void launch_weigh(const spqt_kv_cache &cache, const Call &a, hipStream_t stream)
         constexpr int D = decltype(dim)::value;
         constexpr bool B = decltype(bf16)::value;
         const int y = cache.max_blocks < 32768 ? cache.max_blocks : 32768;
-        if ((int64_t)a.rows * a.group > 64)
+        if ((int64_t)a.rows * a.group > kFewRows)
             hipLaunchKernelGGL((spqt_kv_weigh_many_kernel<D, B>), dim3(cache.kv_heads, y, (unsigned)cache.sequences * ((cache.max_blocks + y - 1) / y)),
                                dim3(many_threads(D)), 0, stream, view(cache), a, cache.sequences);
         else

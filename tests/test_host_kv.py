@@ -109,6 +109,17 @@ def test_workspace_sizes():
             size(*bad)
 
 
+@pytest.mark.parametrize("dim", [64, 128, 192, 256])
+def test_a_workspace_for_more_serves_less(dim):
+    size = spqt.spqt_kv_workspace_bytes
+    steps = [1, 3, 16, 64, 65, 200, 512, 513, 4000]
+    for sequences in (1, 5, 300):
+        for blocks in (1, 7, 8, 400, 100_000):
+            sizes = [size(sequences, rows, 8, 8, dim, blocks) for rows in steps]
+            assert sizes == sorted(sizes)
+            assert sizes == [size(1, rows, 8, 8, dim, 1) for rows in steps]
+
+
 def test_binding_refuses_what_is_not_on_the_gpu():
     import torch
     codes, scales = torch.zeros((2, 1, 2, 64, 64), dtype=torch.uint8), torch.zeros((2, 1, 2))
