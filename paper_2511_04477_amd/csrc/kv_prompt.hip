@@ -4,12 +4,13 @@
 // With S^T = K Q^T a lane of v_mfma_f32_32x32x16_f16 has one row of Q and half of each 32 tokens, and what it has of P^T is an operand of
 // O^T = V^T P^T if a line of V^T holds the tokens in that order: per 16 tokens the fours 0 and 2 for the lower lanes, 1 and 3 for the upper ones.
 //
-// Probabilities go to the matrix instructions as ONE fp16 number, off by up to 2^-12 of themselves: a second one would cost half as many matrix instructions again.  Against 64 bits
-// an fp16 output of 4001 rows is then 2.5e-4 off instead of the 2.1e-4 of its own rounding, a bf16 one no further than by its rounding (1.7e-3).  Sums stay in 32 bits.
+// Probabilities go to the matrix instructions as two fp16 numbers, 22 bits in all, as they do where rows are few: what a row gets does not depend on which kernel a call takes.  One number
+// would save a third of the products' instructions (4001 rows of 32 / 8 heads of 128 169 us for 211, 1024 rows over 32768 tokens 1050 for 1498), and every output would be off by up to 2^-11
+// of sum p |v|: against 64 bits 2.5e-4 of an fp16 output instead of the 2.1e-4 of its own rounding.
 //
-// What bounds it: matrix and vector instructions of a SIMD side by side; a block takes a SIMD's two wavefronts 64 matrix instructions of 32 cycles and about 520 others, half of them
-// for the softmax.  1024 rows of 64 / 8 heads of 128 over 32768 tokens 1043 us = 1.04 PFLOP/s (an 8192^3 product: 1.2); 4001 rows of 32 / 8 heads from an empty cache 166 us = 792
-// TFLOP/s, since 504 workgroups of uneven length on 256 CUs leave some idle at the end.
+// What bounds it: matrix and vector instructions of a SIMD side by side; a block takes a SIMD's two wavefronts 96 matrix instructions of 32 cycles and about 620 others, more than
+// half of them for the softmax.  1024 rows of 64 / 8 heads of 128 over 32768 tokens 1498 us = 0.72 PFLOP/s (1.08 of what the instructions multiply; an 8192^3 product: 1.2); 4001 rows of
+// 32 / 8 heads from an empty cache 211 us, since 504 workgroups of uneven length on 256 CUs leave some idle at the end.
 #include "kv_attend.hpp"
 
 namespace {
@@ -172,7 +173,7 @@ __global__ __launch_bounds__(Shape<D>::kThreads) void spqt_kv_prompt_kernel(Cach
     auto scalar = [&](float v, int b) { return as_float(lane_of(as_u32(v), b - base)); };
 
     f32x16 p[2];
-    f16x8 lifted[4];
+    f16x8 lifted[4], rest[4];                                // probabilities and what their first number leaves
     // O += V P of the last block and S = K Q of this one: kProducts matrix instructions in a row, whose other operands are read kAhead ahead.
     // A wavefront alone on its SIMD goes through the values 32 elements at a time and brings the next 32's sums to their new units beside those products: 4001 rows of 16 / 4 heads of
     // 256 299 -> 227 us, of 192 184 -> 182.  Where two take turns the one that multiplies has no time for it: heads of 128 174 for 171, of 64 136 for 133.
@@ -195,6 +196,7 @@ __global__ __launch_bounds__(Shape<D>::kThreads) void spqt_kv_prompt_kernel(Cach
         for (int i = from; i < to; ++i) {
             if (i < kValueProducts) {
                 acc[tile_of(i)] = __builtin_amdgcn_mfma_f32_32x32x16_f16(x[i % kAhead], lifted[sixteen_of(i)], acc[tile_of(i)], 0, 0, 0);
+                acc[tile_of(i)] = __builtin_amdgcn_mfma_f32_32x32x16_f16(x[i % kAhead], rest[sixteen_of(i)], acc[tile_of(i)], 0, 0, 0);
                 if (kBeside && i + 4 < kValueProducts)
 #pragma unroll
                     for (int e = 4 * (i % 4); e < 4 * (i % 4) + 4; ++e) acc[i / 4 + 1][e] *= shrink;
@@ -247,8 +249,12 @@ __global__ __launch_bounds__(Shape<D>::kThreads) void spqt_kv_prompt_kernel(Cach
                     sum += x[i];
                 }
                 const f16x2 h = __builtin_convertvector(x, f16x2);
-                lifted[2 * t + e / 8][e % 8] = h[0];
-                lifted[2 * t + e / 8][e % 8 + 1] = h[1];
+                const f16x2 l = __builtin_convertvector(f32x2{x[0] - (float)h[0], x[1] - (float)h[1]}, f16x2);
+#pragma unroll
+                for (int i = 0; i < 2; ++i) {
+                    lifted[2 * t + e / 8][e % 8 + i] = h[i];
+                    rest[2 * t + e / 8][e % 8 + i] = l[i];
+                }
             }
         total += sum * (1.0f / kLift);
 #pragma unroll
