@@ -5,13 +5,14 @@
 // O^T = V^T P^T if a line of V^T holds the tokens in that order: per 16 tokens the fours 0 and 2 for the lower lanes, 1 and 3 for the upper ones.
 //
 // Probabilities go to the matrix instructions as two fp16 numbers, 22 bits in all, as they do where rows are few: what a row gets does not depend on which kernel a call takes.  One number
-// would save a third of the products' instructions (4001 rows of 32 / 8 heads of 128 169 us for 211, 1024 rows over 32768 tokens 1050 for 1498), and every output would be off by up to 2^-11
+// would save a third of the products' instructions (4001 rows of 32 / 8 heads of 128 166 us for 208, 1024 rows over 32768 tokens 1042 for 1397), and every output would be off by up to 2^-11
 // of sum p |v|: against 64 bits 2.5e-4 of an fp16 output instead of the 2.1e-4 of its own rounding.
 //
 // What bounds it: matrix and vector instructions of a SIMD side by side; a block takes a SIMD's two wavefronts 96 matrix instructions of 32 cycles and about 620 others, more than
-// half of them for the softmax.  1024 rows of 64 / 8 heads of 128 over 32768 tokens 1498 us = 0.72 PFLOP/s (1.08 of what the instructions multiply; an 8192^3 product: 1.2); 4001 rows of
-// 32 / 8 heads from an empty cache 211 us, since 504 workgroups of uneven length on 256 CUs leave some idle at the end.
+// half of them for the softmax.  1024 rows of 64 / 8 heads of 128 over 32768 tokens 1397 us = 0.77 PFLOP/s (1.16 of what the instructions multiply; an 8192^3 product: 1.2); 4001 rows of
+// 32 / 8 heads from an empty cache 208 us, since 504 workgroups of uneven length on 256 CUs leave some idle at the end.
 #include "kv_attend.hpp"
+#include "kv_units.hpp"
 
 namespace {
 
@@ -27,6 +28,14 @@ struct Shape {
     static constexpr int kKeyStride = D + 8, kValueStride = kBlock + 8;      // fp16 numbers; 16 lines are in 16 different sets of banks
 };
 
+// Heads of 128 have no registers left for what the compiler keeps from before the loop, places in shared and global memory: it would lie in scratch memory, which every turn waits for
+// (1024 rows of 64 / 8 heads over 32768 tokens 1707 us for 1397; heads of 64 145 for 156, of 256 261 for 267 the other way round).
+template <int D>
+__device__ __forceinline__ int worked_out_anew(int v) {
+    if (D == 128) asm("" : "+v"(v));
+    return v;
+}
+
 // A thread's part of a block's keys or values, on its way from codes to numbers.
 template <int D>
 struct StagedKeys {
@@ -35,9 +44,10 @@ struct StagedKeys {
 
     template <class F>
     __device__ __forceinline__ void each(F f) {
+        const int thread = worked_out_anew<D>(threadIdx.x);
 #pragma unroll
         for (int i = 0; i < kParts; ++i) {
-            const int at = threadIdx.x + i * kThreads;
+            const int at = thread + i * kThreads;
             if (D * 4 % kThreads == 0 || at < D * 4) f(part[i], at);
         }
     }
@@ -59,9 +69,10 @@ struct StagedValues {
 
     template <class F>
     __device__ __forceinline__ void each(F f) {
+        const int thread = worked_out_anew<D>(threadIdx.x);
 #pragma unroll
         for (int i = 0; i < kParts; ++i) {
-            const int at = threadIdx.x + i * kThreads;
+            const int at = thread + i * kThreads;
             if (D * 4 % kThreads == 0 || at < D * 4) f(part[i], at / 4, at / 2 % 2, at % 2);
         }
     }
@@ -130,7 +141,9 @@ __global__ __launch_bounds__(Shape<D>::kThreads) void spqt_kv_prompt_kernel(Cach
     Row row = row_of(a, r, head, length, count);
     if (r >= rows) row.high = -1;
     f16x8 q[D / 16];
-    float scale, top = kNone, total = 0.0f, unit = 1.0f, shrink = 1.0f;
+    float scale, total = 0.0f, shrink = 1.0f;
+    Units units;
+    units.start();
     {
         const bool live = row.high >= 0;
         const uint16_t *from = a.q.data + s * a.q.sequence + row.i * a.q.row + row.head * a.q.head;
@@ -156,7 +169,7 @@ __global__ __launch_bounds__(Shape<D>::kThreads) void spqt_kv_prompt_kernel(Cach
     // Pages and scales of 64 blocks from `base` on, one per lane: looked up rarely, so that no turn waits for a chain of loads.
     const int32_t *table = c.table + (size_t)s * c.max_blocks + begin;
     uint32_t places = 0;                                      // of the page and head among all pages' heads: their codes are within the memory there is
-    float scales_k = 0.0f, scales_v = 0.0f, inverses_v = 0.0f;
+    float scales_k = 0.0f, scales_v = 0.0f, inverses_v = 0.0f;             // (1 / the part from 1/2 to 1 of scales_v)
     int base = 0;
     auto look_up = [&](int b) {
         base = b;
@@ -167,7 +180,7 @@ __global__ __launch_bounds__(Shape<D>::kThreads) void spqt_kv_prompt_kernel(Cach
         places = page * (uint32_t)c.kv_heads + (uint32_t)head;
         scales_k = there ? c.scales[scale_at(c, page, head, 0)] : __builtin_nanf("");
         scales_v = there ? c.scales[scale_at(c, page, head, 1)] : __builtin_nanf("");
-        inverses_v = 1.0f / scales_v;
+        inverses_v = 1.0f / __builtin_amdgcn_frexp_mantf(scales_v);
     };
     auto codes_of = [&](int b) { return c.codes + (size_t)lane_of(places, b - base) * (2 * kBlock * D); };
     auto scalar = [&](float v, int b) { return as_float(lane_of(as_u32(v), b - base)); };
@@ -184,10 +197,12 @@ __global__ __launch_bounds__(Shape<D>::kThreads) void spqt_kv_prompt_kernel(Cach
     auto products = [&](const _Float16 *v, const _Float16 *k, auto skip, auto stop) {
         constexpr int from = decltype(skip)::value ? kValueProducts : 0, to = decltype(stop)::value ? kValueProducts : kProducts;
         f16x8 x[kAhead];
+        const int here = worked_out_anew<D>(lane);
+        const int line = here & 31, part = here >> 5 << 3;
         auto read = [&](int i) {
-            if (i < kValueProducts) return *reinterpret_cast<const f16x8 *>(v + (tile_of(i) * 32 + column) * S::kValueStride + sixteen_of(i) * 16 + 8 * half);
+            if (i < kValueProducts) return *reinterpret_cast<const f16x8 *>(v + (tile_of(i) * 32 + line) * S::kValueStride + sixteen_of(i) * 16 + part);
             i -= kValueProducts;
-            return *reinterpret_cast<const f16x8 *>(k + (i % 2 * 32 + column) * S::kKeyStride + i / 2 * 16 + 8 * half);
+            return *reinterpret_cast<const f16x8 *>(k + (i % 2 * 32 + line) * S::kKeyStride + i / 2 * 16 + part);
         };
 #pragma unroll
         for (int i = from; i < from + kAhead; ++i) x[i % kAhead] = read(i);
@@ -211,13 +226,14 @@ __global__ __launch_bounds__(Shape<D>::kThreads) void spqt_kv_prompt_kernel(Cach
     auto probabilities = [&](int block, float scale_k, float scale_v, float inverse_v, auto masked) {
         const float by = scale * scale_k;
         if (decltype(masked)::value) {
+            uint32_t first = (uint32_t)(block * kBlock + 4 * half - row.low);
+            const uint32_t seen = row.high < row.low ? 0u : (uint32_t)(row.high - row.low) + 1u;
+            asm("" : "+v"(first));                            // else the 32 tokens' places are kept in registers from before the loop
 #pragma unroll
             for (int t = 0; t < 2; ++t)
 #pragma unroll
-                for (int e = 0; e < 16; ++e) {
-                    const int token = block * kBlock + 32 * t + 8 * (e / 4) + 4 * half + e % 4;
-                    if (!(token >= row.low && token <= row.high)) p[t][e] = kNone;
-                }
+                for (int e = 0; e < 16; ++e)
+                    if (first + (uint32_t)(32 * t + 8 * (e / 4) + e % 4) >= seen) p[t][e] = kNone;
         }
         float most = p[0][0];
 #pragma unroll
@@ -225,17 +241,9 @@ __global__ __launch_bounds__(Shape<D>::kThreads) void spqt_kv_prompt_kernel(Cach
 #pragma unroll
             for (int e = 0; e < 16; ++e) most = __builtin_fmaxf(most, p[t][e]);
         most = halves_max(most);
-        const bool sees = !decltype(masked)::value || !(most == kNone);
-        most = __builtin_fmaxf(top, sees ? most * by : kNone);
-        const float from = most == kNone ? 0.0f : most;
-        shrink = __builtin_amdgcn_exp2f(top - from);
-        top = most;
-        total *= shrink;
-        if (sees) {
-            shrink *= unit * inverse_v;
-            unit = scale_v;
-        }
-        const float lifted_from = 15.0f - from;
+        const Units::Step step = units.see(!decltype(masked)::value || !(most == kNone), most * by, __builtin_amdgcn_frexp_mantf(scale_v), inverse_v, (float)__builtin_amdgcn_frexp_expf(scale_v));
+        total *= step.total;
+        shrink = step.sums;
         float sum = 0.0f;
 #pragma unroll
         for (int t = 0; t < 2; ++t)
@@ -244,7 +252,7 @@ __global__ __launch_bounds__(Shape<D>::kThreads) void spqt_kv_prompt_kernel(Cach
                 f32x2 x;
 #pragma unroll
                 for (int i = 0; i < 2; ++i) {
-                    const float y = __builtin_amdgcn_exp2f(__builtin_fmaf(p[t][e + i], by, lifted_from));
+                    const float y = __builtin_amdgcn_exp2f(__builtin_fmaf(p[t][e + i], by, -step.less));
                     x[i] = decltype(masked)::value && p[t][e + i] == kNone ? 0.0f : y;
                     sum += x[i];
                 }
@@ -256,7 +264,7 @@ __global__ __launch_bounds__(Shape<D>::kThreads) void spqt_kv_prompt_kernel(Cach
                     rest[2 * t + e / 8][e % 8 + i] = l[i];
                 }
             }
-        total += sum * (1.0f / kLift);
+        total += sum * step.back;
 #pragma unroll
         for (int i = 0; i < (kBeside ? 1 : D / 32); ++i) acc[i] *= shrink;
     };
@@ -297,12 +305,12 @@ __global__ __launch_bounds__(Shape<D>::kThreads) void spqt_kv_prompt_kernel(Cach
     }
 
     Meeting sum;
-    sum.top = top;
+    sum.top = units.top;
     const auto both = __builtin_amdgcn_permlane32_swap(as_u32(total), as_u32(total), false, false);
     sum.total = as_float(both[0]) + as_float(both[1]);
     if (parts.n > 1) {
         const size_t slot = ((((size_t)s * c.kv_heads + head) * tiles + tile) * parts.n + blockIdx.y) * S::kRows + wave * 32 + column;
-        const float by = unit * (1.0f / kLift);
+        const float by = units.drop();
 #pragma unroll
         for (int i = 0; i < D / 32; ++i)
 #pragma unroll
@@ -313,7 +321,7 @@ __global__ __launch_bounds__(Shape<D>::kThreads) void spqt_kv_prompt_kernel(Cach
     }
     if (r >= rows) return;
     uint16_t *out = a.out.data + s * a.out.sequence + row.i * a.out.row + row.head * a.out.head + 4 * half;
-    const float by = unit * (1.0f / kLift) * sum.inverse();
+    const float by = units.drop() * sum.inverse();
 #pragma unroll
     for (int i = 0; i < D / 32; ++i)
 #pragma unroll

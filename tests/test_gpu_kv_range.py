@@ -8,7 +8,7 @@ leaves: half of 2^-24 in units of 2^-15 of the largest value scale there is.  Th
 import pytest
 
 from oracle import kv as oracle
-from test_gpu_kv import E, EITHER, MANY, attend, case_cache, gpu, widen  # noqa: F401
+from test_gpu_kv import Cache, E, EITHER, MANY, attend, case_cache, gpu, widen  # noqa: F401
 
 pytestmark = pytest.mark.gpu
 
@@ -42,3 +42,42 @@ def test_probabilities_have_twenty_two_bits_in_every_kernel(gpu, case, wide):  #
         widen(c)
     out, _ = attend(gpu, c, q, case[5], case[7])
     assert within(c, q, case[5], case[7], out) <= 1.0
+
+
+# sizes of the values, a block each: a block of zeros has the scale 2^-100
+STEEP = [
+    ("float16", [8.0] * 40 + [0.0]),
+    ("float16", [1.0] * 140 + [0.0] + [1.0] * 4),
+    ("bfloat16", [1000.0, 0.0]),
+    ("float16", [1000.0] * 10 + [0.0] + [1000.0] * 2),     # one part, with many rows
+    ("float16", [100.0] * 46 + [0.0] + [100.0] * 17),      # several parts: the block of zeros is the seventh of its part
+    ("bfloat16", [1e30, 1e-30, 1.0, 1e20, 0.0, 1e-10, 1e12] * 2),
+    ("float16", [0.0, 6e-8, 0.0, 1e-4, 60000.0, 0.0]),
+]
+# query heads, kv heads, rows, wide tables: a few rows, some that are a few or many by the tables' room, many rows
+FORMS = [(8, 2, 1, False), (8, 1, 12, False), (8, 1, 12, True), (8, 1, 70, False)]
+
+
+def steep_cache(gpu, dtype, sizes, kv_heads, dim, seed):  # noqa: F811
+    torch, _ = gpu
+    c = Cache(gpu, 1, kv_heads, dim, getattr(torch, dtype), len(sizes), seed)
+    x = torch.randn((1, 64 * len(sizes), 2 * kv_heads, dim), generator=c.gen)
+    each = torch.tensor(sizes, dtype=torch.float64).float().repeat_interleave(64)[None, :, None, None]
+    x[:, :, kv_heads:] = each * (0.9 + 0.01 * x[:, :, kv_heads:])          # values of one sign and about one size
+    c.append(64 * len(sizes), x=x.to(c.dtype))
+    return c
+
+
+@pytest.mark.parametrize("dim", [64, 128, 192, 256])
+@pytest.mark.parametrize("heads,kv_heads,rows,wide", FORMS)
+@pytest.mark.parametrize("dtype,sizes", STEEP, ids=lambda x: x if isinstance(x, str) else f"{len(x)}x{x[0]}")
+def test_blocks_of_zeros_and_of_very_different_values(gpu, dtype, sizes, heads, kv_heads, rows, wide, dim):  # noqa: F811
+    """Rows that weigh all tokens about the same."""
+    torch, _ = gpu
+    c = steep_cache(gpu, dtype, sizes, kv_heads, dim, len(sizes) + dim)
+    q = (0.05 * torch.randn((1, rows, heads, dim), generator=c.gen)).to(c.dtype).cuda()
+    if wide:
+        widen(c)
+    out, lse = attend(gpu, c, q, None)
+    assert bool(torch.isfinite(out).all()) and bool(torch.isfinite(lse).all())
+    assert within(c, q, None, 0, out) <= 1.0
