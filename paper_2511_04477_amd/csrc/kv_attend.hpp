@@ -9,8 +9,7 @@ namespace kv {
 
 constexpr float kLog2e = 1.4426950408889634f, kLn2 = 0.6931471805599453f;
 constexpr float kNone = -__builtin_inff();
-// Probabilities go to the matrix instructions as two fp16 numbers, 22 bits in all, times 2^15: fp16's smallest number is 2^-39 of the largest one.
-constexpr float kLift = 0x1p15f;
+// Probabilities go to the matrix instructions as two fp16 numbers, 22 bits in all, the largest of them about 2^15 (kv_units.hpp): fp16's smallest number is 2^-39 of that.
 
 struct Call {
     Rows q, out;

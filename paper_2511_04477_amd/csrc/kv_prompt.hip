@@ -142,7 +142,7 @@ __global__ __launch_bounds__(Shape<D>::kThreads) void spqt_kv_prompt_kernel(Cach
     if (r >= rows) row.high = -1;
     f16x8 q[D / 16];
     float scale, total = 0.0f, shrink = 1.0f;
-    Units units;
+    BlockUnits units;
     units.start();
     {
         const bool live = row.high >= 0;
@@ -241,7 +241,7 @@ __global__ __launch_bounds__(Shape<D>::kThreads) void spqt_kv_prompt_kernel(Cach
 #pragma unroll
             for (int e = 0; e < 16; ++e) most = __builtin_fmaxf(most, p[t][e]);
         most = halves_max(most);
-        const Units::Step step = units.see(!decltype(masked)::value || !(most == kNone), most * by, __builtin_amdgcn_frexp_mantf(scale_v), inverse_v, (float)__builtin_amdgcn_frexp_expf(scale_v));
+        const BlockUnits::Step step = units.see(!decltype(masked)::value || !(most == kNone), most * by, __builtin_amdgcn_frexp_mantf(scale_v), inverse_v, (float)__builtin_amdgcn_frexp_expf(scale_v));
         total *= step.total;
         shrink = step.sums;
         float sum = 0.0f;

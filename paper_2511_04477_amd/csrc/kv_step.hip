@@ -9,6 +9,7 @@
 // and below that the chain of one workgroup: 1.5 us to its blocks, 3 for table, codes, products, 1 to join its wavefronts, 4 to join several workgroups: 8.3 us over 333 tokens
 // of 8 heads, 14.7 over 4095 of 32 (33.6 MB).  40 sequences of 400 to 9500 tokens of 8 heads (346 MB) 74 us = 4.7 TB/s.
 #include "kv_attend.hpp"
+#include "kv_units.hpp"
 
 namespace {
 
@@ -46,7 +47,8 @@ template <int D, bool BF16, bool STREAM>
 struct Wave {
     f16x8 q[D / 32];
     Row row;
-    float scale, top, total, unit; // the row's running maximum, this lane's part of its sum, the scale that acc is in
+    float scale, total;                  // (this lane's part of the row's sum)
+    LevelUnits units;
     int full_low, full_high;             // every row sees the tokens from full_low to full_high
     f32x4 acc[D / 16];
     u32x4 k[4][D / 64], v[D / 16];
@@ -99,17 +101,9 @@ struct Wave {
             most = kNone;
             by = 1.0f;
         }
-        most = __builtin_fmaxf(top, most == kNone ? kNone : most * by);
-        const float from = most == kNone ? 0.0f : most;      // nothing seen yet: 2^(-inf - 0)
-        float shrink = __builtin_amdgcn_exp2f(top - from);
-        total *= shrink;
-        top = most;
-        if (scale_v > unit) {
-            shrink *= unit / scale_v;
-            unit = scale_v;
-        }
-        const float ratio = scale_v / unit * kLift;
-        f16x8 lifted[2], rest[2];                            // a probability in units of `unit`
+        const LevelUnits::Step step = units.see(most != kNone, most * by, __builtin_amdgcn_frexp_mantf(scale_v), (float)__builtin_amdgcn_frexp_expf(scale_v));
+        total *= step.total;
+        f16x8 lifted[2], rest[2];                            // what the matrix instructions get for a probability
         float sum = 0.0f;
 #pragma unroll
         for (int t = 0; t < 4; ++t)
@@ -118,9 +112,9 @@ struct Wave {
                 f32x2 y;
 #pragma unroll
                 for (int i = 0; i < 2; ++i) {
-                    const float x = __builtin_amdgcn_exp2f(__builtin_fmaf(p[t][e + i], by, -from));
+                    const float x = __builtin_amdgcn_exp2f(__builtin_fmaf(p[t][e + i], by, -step.from));
                     sum += x;
-                    y[i] = x * ratio;
+                    y[i] = x * step.lift;
                 }
                 const f16x2 h = __builtin_convertvector(y, f16x2);
                 const f16x2 l = __builtin_convertvector(f32x2{y[0] - (float)h[0], y[1] - (float)h[1]}, f16x2);
@@ -139,9 +133,9 @@ struct Wave {
                 for (int e = 0; e < 4; ++e)
                     if (p[t][e] == kNone) lifted[t / 2][4 * (t % 2) + e] = rest[t / 2][4 * (t % 2) + e] = (_Float16)0.0f;
         }
-        if (__ballot(shrink != 1.0f))
+        if (__ballot(step.sums != 1.0f))
 #pragma unroll
-            for (int i = 0; i < D / 16; ++i) acc[i] *= shrink;
+            for (int i = 0; i < D / 16; ++i) acc[i] *= step.sums;
 #pragma unroll
         for (int i = 0; i < D / 16; ++i) {
 #pragma unroll
@@ -187,9 +181,8 @@ struct Wave {
             if (done == 0) {
                 scale = positive_scale(a.scale, raw) * kLog2e;
                 scale *= queries_f16<BF16>(raw, q, 16);
-                top = kNone;
+                units.start();
                 total = 0.0f;
-                unit = 0x1p-120f;
 #pragma unroll
                 for (int i = 0; i < D / 16; ++i) acc[i] = {0.0f, 0.0f, 0.0f, 0.0f};
             }
@@ -344,11 +337,11 @@ __global__ __launch_bounds__(step_threads(D)) void spqt_kv_step_kernel(Cache c, 
     Wave<D, BF16, STREAM> w;
     // the rows' sums so far, in units of 2^top, to this wavefront's place in shared memory
     auto put_down = [&]() {
-        const float total = columns_sum(w.total), drop = w.unit * (1.0f / kLift);
+        const float total = columns_sum(w.total), drop = w.units.drop();
 #pragma unroll
         for (int i = 0; i < D / 16; ++i) *reinterpret_cast<f32x4 *>(&sums[wave][column][16 * i + 4 * quarter]) = w.acc[i] * drop;
         if (quarter == 0) {
-            stats[wave][0][column] = w.top;
+            stats[wave][0][column] = w.units.top;
             stats[wave][1][column] = total;
         }
     };
@@ -399,9 +392,9 @@ __global__ __launch_bounds__(step_threads(D)) void spqt_kv_step_kernel(Cache c, 
             put_down();
         } else if (upto == stop) {
             Meeting m;
-            m.top = w.top;
+            m.top = w.units.top;
             m.total = columns_sum(w.total);
-            write_row(p, m, w.acc, w.unit * (1.0f / kLift));
+            write_row(p, m, w.acc, w.units.drop());
         } else {
             open = true;
         }
@@ -449,9 +442,9 @@ __global__ __launch_bounds__(step_threads(D)) void spqt_kv_step_kernel(Cache c, 
         if (open) {
             const uint32_t stop = p.start + (uint32_t)p.span.blocks;
             Meeting m;
-            m.top = w.top;
+            m.top = w.units.top;
             m.total = columns_sum(w.total);
-            const float drop = w.unit * (1.0f / kLift);
+            const float drop = w.units.drop();
 #pragma unroll
             for (int i = 0; i < D / 16; ++i) w.acc[i] *= drop;
             for (int v = wave + 1; v < kStepWaves; ++v) {

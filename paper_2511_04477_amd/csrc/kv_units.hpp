@@ -1,5 +1,5 @@
-// The powers of two that a row's running sums are in units of, while attention of many rows goes through blocks of tokens with value scales of any size.  Arithmetic alone, for the device
-// and, where a test compiles it, the host.
+// The powers of two that a row's running sums are in units of, while attention goes through blocks of tokens with value scales of any size.  Arithmetic alone, for the device and, where a
+// test compiles it, the host.
 #ifndef SPQT_KV_UNITS_HPP
 #define SPQT_KV_UNITS_HPP
 
@@ -19,11 +19,43 @@ SPQT_BOTH float power_of_two(float x) { return exp2f(x); }
 // Scores are in powers of two, a block's values are codes times part * 2^exponent with part from 1/2 to 1 (or NaN).  With m the largest score of a block that the row sees,
 //   top    >= every score so far: a probability is 2^(score - top), at most 1
 //   level  >= m + exponent of every block so far: no token adds more than 2^level times its code to the sums
+// Both are whole numbers, so sums go to new units without rounding.  Neither a block of zeros (exponent -99) nor one of very large values takes the sums out of fp32's range, and what
+// fp16 numbers leave of a probability is measured by the row's largest terms, not by a block that it does not see or gives no weight.
+
+// A few rows: the sums are in units of 2^(level - 15), which change seldom, and a token's number for the matrix instructions is probability * lift, at most 2^15.
+struct LevelUnits {
+    float top, level;
+
+    struct Step {
+        float total, sums;          // factors that bring the sum of the probabilities and the sums of values to the new units
+        float from;                 // a probability is 2^(score - from)
+        float lift;
+    };
+    SPQT_BOTH void start() { top = level = -__builtin_inff(); }
+    // A block; `most` is the largest score, not used if the row sees none of it.  (A NaN among the scores changes no unit.)
+    SPQT_BOTH Step see(bool sees, float most, float part, float exponent) {
+        const float none = -__builtin_inff(), here = sees ? __builtin_ceilf(most) : none;
+        const float old_top = top, old_level = level;
+        top = __builtin_fmaxf(top, here);
+        level = __builtin_fmaxf(level, here + exponent);
+        const float middle = level == none ? 0.0f : level;
+        Step s;
+        s.from = top == none ? 0.0f : top;
+        s.total = power_of_two(old_top - s.from);
+        s.sums = power_of_two(old_level - middle);
+        // (past 2^126 only where all of the block's probabilities are below 2^-110)
+        s.lift = sees ? part * power_of_two(__builtin_fminf(exponent + s.from - middle + 15.0f, 126.0f)) : 0.0f;
+        return s;
+    }
+    // The factor from the sums' units to units of 2^top.
+    SPQT_BOTH float drop() const { return level == -__builtin_inff() ? 0x1p-15f : power_of_two(level - top) * 0x1p-15f; }
+};
+
+// Many rows: a factor for every token would cost as much as its rounding, and the sums go to new units with every block anyway.
 //   place  the sums are in units of 2^(place - 15) * part: those of the last block, place = top + exponent, but no further from the level than 2^-60 and 2^14
-// A token's number for the matrix instructions is its probability times 2^15, unless place was held back: 2^(score - less()), at most 2^15.  Then neither a block of zeros (exponent -99)
-// nor one of very large values takes the sums out of fp32's range (they are below 2^60 * 2^15 * 127 * 2^30 tokens), and half of fp16's smallest number is never more than 2^-24 of
-// what the row's largest term may be (2^level).  All three are whole numbers.
-struct Units {
+// A token's number is its probability times 2^15, unless place was held back: 2^(score - less), at most 2^15.  The sums are below 2^60 * 2^15 * 127 * 2^30 tokens, and half of fp16's
+// smallest number is never more than 2^-25 of 2^level.
+struct BlockUnits {
     float top, level, place, part;
 
     struct Step {

@@ -3,9 +3,11 @@
 Attention's tolerance, per output, with u = 2^-11 (fp16) or 2^-8 (bf16), e = 2^-24 and the oracle's sums sway = scale sum |q| |k| and
 spread = sum p |v|: a score is off by at most d = (D + 8) e sway, a probability by 2 d + (L + 64) e of itself and by 2^-21, since it is held in
 two fp16 numbers (2^-11 of 2^-11 of itself at most, and as much again for the numbers that it is made of); but no less than fp16's smallest step
-leaves: half of 2^-24 in units of 2^-15 of the largest value scale there is.  The output: u |out| + spread times that + L e spread + L 2^-40 times
-127 of that scale, and half of the type's smallest number."""
+leaves: half of 2^-24 in units of 2^-15 of the largest term of the ROW, the product of a probability and its block's value scale, of which the units
+may be four times (whole powers of two of either).  Many rows: of the largest probability times the largest scale that the row sees, though no more
+than 2^14 of the former.  The output: u |out| + spread times that + L e spread + L 2^-40 times 127 of that unit, and half of the type's smallest number."""
 import pytest
+import torch
 
 from oracle import kv as oracle
 from test_gpu_kv import Cache, E, EITHER, MANY, attend, case_cache, gpu, widen  # noqa: F401
@@ -20,8 +22,31 @@ SIXTEENS = [
 ]
 
 
+def largest_terms(c, q, each, window, scale):
+    """For every row and query head: the largest product of a probability and its block's value scale, and of any probability and any such scale."""
+    S, n, Hq, dim = q.shape
+    H = c.codes.shape[1]
+    codes, scales, q = c.codes.cpu(), c.scales.cpu().double(), q.cpu().double()
+    found = torch.zeros((2, S, n, Hq), dtype=torch.float64)
+    for s in range(S):
+        L = c.length_of[s]
+        for h in range(H):
+            k = oracle.token_values(codes, scales, c.table_host[s], h, 0, L)
+            of = scales[c.table_host[s].long(), h, 1].repeat_interleave(64)[:L]
+            for i in range(each[s]):
+                at = L - each[s] + i
+                low = max(0, at - window + 1) if window > 0 else 0
+                if at < 0:
+                    continue
+                for j in range(h * (Hq // H), (h + 1) * (Hq // H)):
+                    p = torch.softmax((k[low : at + 1] @ q[s, i, j]) * scale, 0)
+                    found[0, s, i, j] = (p * of[low : at + 1]).max()
+                    found[1, s, i, j] = p.max() * of[low : at + 1].max()
+    return found
+
+
 def within(c, q, counts, window, out, scale=None, held=2.0 ** -21):
-    torch = c.torch
+    """The largest error, in units of what is allowed."""
     seqs, rows, heads, dim = q.shape
     each = [rows] * seqs if counts is None else counts
     scale = dim ** -0.5 if scale is None else scale
@@ -29,8 +54,10 @@ def within(c, q, counts, window, out, scale=None, held=2.0 ** -21):
     L = max(c.length_of)
     u, smallest = (2.0 ** -11, 2.0 ** -24) if q.dtype == torch.float16 else (2.0 ** -8, 2.0 ** -133)
     off = 2 * (dim + 8) * E * sway + (L + 64) * E + held
-    floor = L * 2.0 ** -40 * 127 * float(c.scales[c.table[:, : -(-L // 64)].long()][..., 1].max())
-    bound = u * want.abs() + (spread * (off[..., None] + L * E) + floor) * (1 + u) + smallest / 2
+    term, separate = largest_terms(c, q, each, window, scale)
+    many = rows * heads // c.kv_heads > 64               # (those that the kernel for a few rows takes all the same are no further off)
+    floor = L * 2.0 ** -38 * 127 * (torch.minimum(separate, term * 2.0 ** 14) if many else term)
+    bound = u * want.abs() + (spread * (off[..., None] + L * E) + floor[..., None]) * (1 + u) + smallest / 2
     return float(((out.cpu().double() - want).abs() / bound).max())
 
 
@@ -59,7 +86,6 @@ FORMS = [(8, 2, 1, False), (8, 1, 12, False), (8, 1, 12, True), (8, 1, 70, False
 
 
 def steep_cache(gpu, dtype, sizes, kv_heads, dim, seed):  # noqa: F811
-    torch, _ = gpu
     c = Cache(gpu, 1, kv_heads, dim, getattr(torch, dtype), len(sizes), seed)
     x = torch.randn((1, 64 * len(sizes), 2 * kv_heads, dim), generator=c.gen)
     each = torch.tensor(sizes, dtype=torch.float64).float().repeat_interleave(64)[None, :, None, None]
@@ -73,11 +99,47 @@ def steep_cache(gpu, dtype, sizes, kv_heads, dim, seed):  # noqa: F811
 @pytest.mark.parametrize("dtype,sizes", STEEP, ids=lambda x: x if isinstance(x, str) else f"{len(x)}x{x[0]}")
 def test_blocks_of_zeros_and_of_very_different_values(gpu, dtype, sizes, heads, kv_heads, rows, wide, dim):  # noqa: F811
     """Rows that weigh all tokens about the same."""
-    torch, _ = gpu
     c = steep_cache(gpu, dtype, sizes, kv_heads, dim, len(sizes) + dim)
     q = (0.05 * torch.randn((1, rows, heads, dim), generator=c.gen)).to(c.dtype).cuda()
     if wide:
         widen(c)
     out, lse = attend(gpu, c, q, None)
     assert bool(torch.isfinite(out).all()) and bool(torch.isfinite(lse).all())
+    assert within(c, q, None, 0, out) <= 1.0
+
+
+@pytest.mark.parametrize("dim", [64, 128, 192, 256])
+@pytest.mark.parametrize("size", [1e6, 1e12, 1e30])
+@pytest.mark.parametrize("rows", [4, 65])
+def test_large_values_that_other_rows_see(gpu, rows, size, dim):  # noqa: F811
+    """The first row sees one token of the block of large values, the rows beside it none; every wavefront has several blocks."""
+    c = steep_cache(gpu, "bfloat16", [size] + [1.0] * 15, 2, dim, 7 + dim)
+    window = 1024 - rows - 63 + 1
+    q = (0.05 * torch.randn((1, rows, 8, dim), generator=c.gen)).bfloat16().cuda()
+    for wide in (False, True):
+        if wide:
+            widen(c)
+        out, _ = attend(gpu, c, q, None, window)
+        assert float(out[:, 0].min()) > size * 1e-4 and float(out[:, 1:].max()) < 2.0 and float(out[:, 1:].min()) > 0.5
+        assert within(c, q, None, window, out) <= 1.0
+
+
+@pytest.mark.parametrize("dim", [64, 128, 192, 256])
+@pytest.mark.parametrize("place", [0, 1])
+@pytest.mark.parametrize("heads,kv_heads,rows,wide", FORMS)
+def test_large_values_that_get_no_weight(gpu, heads, kv_heads, rows, wide, place, dim):  # noqa: F811
+    """A block of large values whose keys point away from every query, before and after the others: probabilities of 2^-140 and less."""
+    sizes = [1.0] * 16
+    sizes[place] = 1e20
+    c = Cache(gpu, 1, kv_heads, dim, torch.bfloat16, 16, 11 + dim)
+    x = torch.randn((1, 1024, 2 * kv_heads, dim), generator=c.gen)
+    each = torch.tensor(sizes).repeat_interleave(64)[None, :, None, None]
+    x[:, :, kv_heads:] = each * (0.9 + 0.01 * x[:, :, kv_heads:])
+    x[:, :, :kv_heads] = torch.where(each > 1, -10.0, 0.1) + 0.1 * x[:, :, :kv_heads]
+    c.append(1024, x=x.bfloat16())
+    q = (1.5 + 0.01 * torch.randn((1, rows, heads, dim), generator=c.gen)).bfloat16().cuda()
+    if wide:
+        widen(c)
+    out, _ = attend(gpu, c, q, None)
+    assert float(out.max()) < 2.0 and float(out.min()) > 0.5
     assert within(c, q, None, 0, out) <= 1.0

@@ -14,10 +14,20 @@ SOURCE = """
 #include "kv_units.hpp"
 using namespace spqt::kv;
 
+static auto see(BlockUnits &u, bool sees, float most, float part, float exponent) { return u.see(sees, most, part, 1.0f / part, exponent); }
+static auto see(LevelUnits &u, bool sees, float most, float part, float exponent) { return u.see(sees, most, part, exponent); }
+static float probability(const BlockUnits::Step &step, float score, float &number) { return (number = exp2f(score - step.less)) * step.back; }
+static float probability(const LevelUnits::Step &step, float score, float &number) {
+    const float p = exp2f(score - step.from);
+    number = p * step.lift;
+    return p;
+}
+
 // One row over `blocks` blocks of n tokens each: scores in powers of two, one code a token, a scale a block, `sees` 0 for a block that the row does not see.
 // result: out in fp32, the largest number of a token, the largest sum on the way.
-extern "C" void row(int blocks, int n, const float *scores, const float *codes, const float *scales, const int *sees, float *result) {
-    Units units;
+template <class U>
+static void go(int blocks, int n, const float *scores, const float *codes, const float *scales, const int *sees, float *result) {
+    U units;
     units.start();
     float acc = 0.0f, total = 0.0f, lifted = 0.0f, largest = 0.0f;
     for (int b = 0; b < blocks; ++b) {
@@ -25,12 +35,12 @@ extern "C" void row(int blocks, int n, const float *scores, const float *codes, 
         const float part = frexpf(scales[b], &exponent);
         float most = -__builtin_inff();
         for (int t = 0; t < n; ++t) most = fmaxf(most, scores[b * n + t]);
-        const Units::Step step = units.see(sees[b] != 0, most, part, 1.0f / part, (float)exponent);
+        const auto step = see(units, sees[b] != 0, most, part, (float)exponent);
         acc *= step.sums;
         total *= step.total;
         for (int t = 0; t < n && sees[b]; ++t) {
-            const float y = exp2f(scores[b * n + t] - step.less);
-            total += y * step.back;
+            float y;
+            total += probability(step, scores[b * n + t], y);
             acc += y * codes[b * n + t];
             lifted = fmaxf(lifted, y);
             largest = fmaxf(largest, fabsf(acc));
@@ -40,16 +50,22 @@ extern "C" void row(int blocks, int n, const float *scores, const float *codes, 
     result[1] = lifted;
     result[2] = largest;
 }
+extern "C" void by_block(int blocks, int n, const float *scores, const float *codes, const float *scales, const int *sees, float *result) {
+    go<BlockUnits>(blocks, n, scores, codes, scales, sees, result);
+}
+extern "C" void by_level(int blocks, int n, const float *scores, const float *codes, const float *scales, const int *sees, float *result) {
+    go<LevelUnits>(blocks, n, scores, codes, scales, sees, result);
+}
 """
 
 
-@pytest.fixture(scope="module")
-def row(tmp_path_factory):
+@pytest.fixture(scope="module", params=["by_block", "by_level"])
+def row(request, tmp_path_factory):
     d = tmp_path_factory.mktemp("units")
     (d / "units.cpp").write_text(SOURCE)
     subprocess.run(["g++", "-std=c++17", "-O2", "-shared", "-fPIC", "-I", os.path.join(ROOT, "include"), "-I",
                     os.path.join(ROOT, "paper_2511_04477_amd", "csrc"), "-o", str(d / "units.so"), str(d / "units.cpp")], check=True)
-    function = ctypes.CDLL(str(d / "units.so")).row
+    function = getattr(ctypes.CDLL(str(d / "units.so")), request.param)
 
     def call(blocks):
         """blocks: (scores, codes, scale, sees); what the row is in fp32 and in 64 bits, and how far apart they may be."""
