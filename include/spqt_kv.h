@@ -80,8 +80,10 @@ int spqt_kv_workspace_bytes(int sequences, int rows, int q_heads, int kv_heads, 
 
 /* Attention of the call's rows over the cache.  Query head j reads kv head j / (q_heads / kv_heads).  Row i at position p sees
  * the tokens t <= p of its sequence, and with window > 0 only those with t > p - window.
- *   out  = sum over t of softmax(scale * q . k_t) v_t            sums and statistics in fp32; 16 bit, strided as q
+ *   out  = sum over t of softmax(scale * q . k_t) v_t            16 bit (at most the type's largest number), strided as q
  *   lse  = ln sum over t of exp(scale * q . k_t)                 fp32 [sequences][rows][q_heads], optional
+ * Sums and statistics are fp32; for the products with the values a probability has 22 bits, but no finer than about 2^-40 of the row's
+ * largest product of a probability and its block's scale.
  * A row that sees nothing, and a row from counts[s] on, has out 0 and lse -infinity.
  * decay: with cache->weights, and lse given, every token t of the sequence gets
  *   weights = decay * weights + sum over the call's rows and the heads that read its kv head of its probability

@@ -9,6 +9,8 @@ namespace kv {
 
 constexpr float kLog2e = 1.4426950408889634f, kLn2 = 0.6931471805599453f;
 constexpr float kNone = -__builtin_inff();
+// A row's sums of values are put down in units of 2^(its maximum + kRoom): those of 2^30 tokens of bf16's largest number are within fp32's range.
+constexpr int kRoom = 32;
 // Probabilities go to the matrix instructions as two fp16 numbers, 22 bits in all, the largest of them about 2^15 (kv_units.hpp): fp16's smallest number is 2^-39 of that.
 
 struct Call {
@@ -35,7 +37,7 @@ __device__ __forceinline__ Row row_of(const Call &a, int r, int head, int length
     return w;
 }
 
-// What the rows' sums over some tokens and over others make together: (top, total, x) with x in units of 2^top.
+// What the rows' sums over some tokens and over others make together: (top, total, x) with x in units of 2^(top + kRoom).
 struct Meeting {
     float top = kNone, total = 0.0f;
     __device__ __forceinline__ void add(float other_top, float other_total, float &mine, float &others) {
@@ -45,7 +47,7 @@ struct Meeting {
         total = total * mine + other_total * others;
         top = most;
     }
-    __device__ __forceinline__ float inverse() const { return total == 0.0f ? 0.0f : 1.0f / total; }
+    __device__ __forceinline__ float inverse() const { return total == 0.0f ? 0.0f : 0x1p32f / total; }
     __device__ __forceinline__ float lse() const { return total == 0.0f ? kNone : (top == kNone ? 0.0f : top) * kLn2 + __builtin_logf(total); }
 };
 

@@ -75,6 +75,17 @@ __device__ __forceinline__ uint32_t bytes_of(uint32_t a, uint32_t b, uint32_t c,
     return inverse != inverse ? 0x80808080u : low | high;
 }
 
+// The same for numbers that are finite or NaN and at most 127 times a scale: the type's largest number where they round to infinity.  127 scale_of(65504) = 65563.75 does; a bf16 never,
+// since 127 scale is less than 2^-10 above the largest |x| and the largest bf16 number 2^-9 below where rounding leaves the type.
+template <bool BF16>
+__device__ __forceinline__ uint32_t narrow2_within(float a, float b) {
+    typedef uint16_t u16x2 __attribute__((ext_vector_type(2)));
+    const uint32_t x = narrow2<BF16>(a, b);
+    if (BF16) return x;
+    const u16x2 finite = __builtin_elementwise_min(__builtin_bit_cast(u16x2, (x & 0x7FFF7FFFu) ^ 0x7C007C00u), u16x2{1, 1});     // 0 for an infinity
+    return __builtin_bit_cast(uint32_t, (u16x2)(__builtin_bit_cast(u16x2, x) + finite - u16x2{1, 1}));
+}
+
 // Two cached values as a reader gets them.
 template <bool BF16>
 __device__ __forceinline__ uint32_t values_of(uint32_t first, uint32_t second, float scale) {

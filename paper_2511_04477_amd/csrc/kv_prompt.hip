@@ -96,7 +96,7 @@ __device__ __forceinline__ float halves_max(float v) {
     return __builtin_fmaxf(as_float(r[0]), as_float(r[1]));
 }
 
-// Where the tokens are divided into parts: what each of them makes of a row, in units of 2^(its maximum).
+// Where the tokens are divided into parts: what each of them makes of a row, in units of 2^(its maximum + kRoom).
 struct Parts {
     int n;
     float *sums;         // [sequence][kv head][256 (128) rows][part][row][D]
@@ -308,26 +308,30 @@ __global__ __launch_bounds__(Shape<D>::kThreads) void spqt_kv_prompt_kernel(Cach
     sum.top = units.top;
     const auto both = __builtin_amdgcn_permlane32_swap(as_u32(total), as_u32(total), false, false);
     sum.total = as_float(both[0]) + as_float(both[1]);
+    const int drop = units.drop() - kRoom;
+#pragma unroll
+    for (int i = 0; i < D / 32; ++i)
+#pragma unroll
+        for (int e = 0; e < 16; ++e) acc[i][e] = __builtin_ldexpf(acc[i][e] * units.part, drop);
     if (parts.n > 1) {
         const size_t slot = ((((size_t)s * c.kv_heads + head) * tiles + tile) * parts.n + blockIdx.y) * S::kRows + wave * 32 + column;
-        const float by = units.drop();
 #pragma unroll
         for (int i = 0; i < D / 32; ++i)
 #pragma unroll
             for (int e = 0; e < 16; e += 4)
-                *reinterpret_cast<f32x4 *>(parts.sums + slot * D + 32 * i + 2 * e + 4 * half) = f32x4{acc[i][e], acc[i][e + 1], acc[i][e + 2], acc[i][e + 3]} * by;
+                *reinterpret_cast<f32x4 *>(parts.sums + slot * D + 32 * i + 2 * e + 4 * half) = f32x4{acc[i][e], acc[i][e + 1], acc[i][e + 2], acc[i][e + 3]};
         if (half == 0) *reinterpret_cast<f32x2 *>(parts.stats + slot * 2) = f32x2{sum.top, sum.total};
         return;
     }
     if (r >= rows) return;
     uint16_t *out = a.out.data + s * a.out.sequence + row.i * a.out.row + row.head * a.out.head + 4 * half;
-    const float by = units.drop() * sum.inverse();
+    const float by = sum.inverse();
 #pragma unroll
     for (int i = 0; i < D / 32; ++i)
 #pragma unroll
         for (int e = 0; e < 16; e += 4) {
             *reinterpret_cast<u32x2 *>(out + 32 * i + 2 * e) =
-                u32x2{narrow2<BF16>(acc[i][e] * by, acc[i][e + 1] * by), narrow2<BF16>(acc[i][e + 2] * by, acc[i][e + 3] * by)};
+                u32x2{narrow2_within<BF16>(acc[i][e] * by, acc[i][e + 1] * by), narrow2_within<BF16>(acc[i][e + 2] * by, acc[i][e + 3] * by)};
         }
     if (a.lse && half == 0) a.lse[((size_t)s * a.rows + row.i) * a.q_heads + row.head] = sum.lse();
 }
@@ -356,7 +360,7 @@ __global__ __launch_bounds__(256) void spqt_kv_parts_kernel(Call a, int kv_heads
     uint16_t *out = a.out.data + s * a.out.sequence + i * a.out.row + q_head * a.out.head + d;
     const float by = m.inverse();
 #pragma unroll
-    for (int e = 0; e < kEach; e += 2) *reinterpret_cast<uint32_t *>(out + e) = narrow2<BF16>(x[e] * by, x[e + 1] * by);
+    for (int e = 0; e < kEach; e += 2) *reinterpret_cast<uint32_t *>(out + e) = narrow2_within<BF16>(x[e] * by, x[e + 1] * by);
     if (a.lse && threadIdx.x % 32 == 0) a.lse[((size_t)s * a.rows + i) * a.q_heads + q_head] = m.lse();
 }
 

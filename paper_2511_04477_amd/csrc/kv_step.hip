@@ -147,6 +147,14 @@ struct Wave {
         }
         fetch_values(next + kBlock * D, on, lane);
     }
+    // The sums to units of 2^(top + kRoom).
+    __device__ __forceinline__ void settle() {
+        const int drop = units.drop() - kRoom;
+#pragma unroll
+        for (int i = 0; i < D / 16; ++i)
+#pragma unroll
+            for (int e = 0; e < 4; ++e) acc[i][e] = __builtin_ldexpf(acc[i][e], drop);
+    }
     // Blocks first .. first + n - 1 of the sequence.  Pages and scales of 64 of them are looked up at once, one per lane; the loads of the first ones go out
     // one chain after the other, the queries' among them.
     __device__ __forceinline__ void run(const Cache &c, const Call &a, const Span &span, int s, int head, int tile, int first, int n, int lane) {
@@ -190,6 +198,7 @@ struct Wave {
             for (int i = 0; i < here; ++i)
                 block(b0 + i, scale_of(i, 0), scale_of(i, 1), codes_of(i + 1 < here ? i + 1 : i), i + 1 < here ? ~0u : 0u, lane);
         }
+        settle();
     }
 };
 
@@ -335,26 +344,26 @@ __global__ __launch_bounds__(step_threads(D)) void spqt_kv_step_kernel(Cache c, 
     auto head_of = [&](const Place &p) { return tiles == 1 ? (int)p.unit : (int)(p.unit / (uint32_t)tiles); };
 
     Wave<D, BF16, STREAM> w;
-    // the rows' sums so far, in units of 2^top, to this wavefront's place in shared memory
+    // the rows' sums so far to this wavefront's place in shared memory
     auto put_down = [&]() {
-        const float total = columns_sum(w.total), drop = w.units.drop();
+        const float total = columns_sum(w.total);
 #pragma unroll
-        for (int i = 0; i < D / 16; ++i) *reinterpret_cast<f32x4 *>(&sums[wave][column][16 * i + 4 * quarter]) = w.acc[i] * drop;
+        for (int i = 0; i < D / 16; ++i) *reinterpret_cast<f32x4 *>(&sums[wave][column][16 * i + 4 * quarter]) = w.acc[i];
         if (quarter == 0) {
             stats[wave][0][column] = w.units.top;
             stats[wave][1][column] = total;
         }
     };
     // a lane's row of a unit, from its (whole) sums in registers
-    auto write_row = [&](const Place &p, const Meeting &m, const f32x4 (&x)[D / 16], float by) {
+    auto write_row = [&](const Place &p, const Meeting &m, const f32x4 (&x)[D / 16]) {
         const int r = tile_of(p) * 16 + column;
         if (r >= a.rows * a.group) return;
         const int i = r / a.group, head = head_of(p) * a.group + r % a.group;
         uint16_t *out = a.out.data + p.s * a.out.sequence + i * a.out.row + head * a.out.head + 4 * quarter;
-        by *= m.inverse();
+        const float by = m.inverse();
 #pragma unroll
         for (int d = 0; d < D / 16; ++d) {
-            *reinterpret_cast<u32x2 *>(out + 16 * d) = u32x2{narrow2<BF16>(x[d][0] * by, x[d][1] * by), narrow2<BF16>(x[d][2] * by, x[d][3] * by)};
+            *reinterpret_cast<u32x2 *>(out + 16 * d) = u32x2{narrow2_within<BF16>(x[d][0] * by, x[d][1] * by), narrow2_within<BF16>(x[d][2] * by, x[d][3] * by)};
         }
         if (a.lse && quarter == 0) a.lse[((size_t)p.s * a.rows + i) * a.q_heads + head] = m.lse();
     };
@@ -374,7 +383,7 @@ __global__ __launch_bounds__(step_threads(D)) void spqt_kv_step_kernel(Cache c, 
         uint16_t *out = a.out.data + p.s * a.out.sequence + i * a.out.row + head * a.out.head + my_d;
         const float by = m.inverse();
 #pragma unroll
-        for (int d = 0; d < kPart; d += 2) *reinterpret_cast<uint32_t *>(out + d) = narrow2<BF16>(x[d] * by, x[d + 1] * by);
+        for (int d = 0; d < kPart; d += 2) *reinterpret_cast<uint32_t *>(out + d) = narrow2_within<BF16>(x[d] * by, x[d + 1] * by);
         if (a.lse && threadIdx.x % kRowThreads == 0) a.lse[((size_t)p.s * a.rows + i) * a.q_heads + head] = m.lse();
     };
     auto live_rows = [&](const Place &p) {
@@ -394,7 +403,7 @@ __global__ __launch_bounds__(step_threads(D)) void spqt_kv_step_kernel(Cache c, 
             Meeting m;
             m.top = w.units.top;
             m.total = columns_sum(w.total);
-            write_row(p, m, w.acc, w.units.drop());
+            write_row(p, m, w.acc);
         } else {
             open = true;
         }
@@ -444,9 +453,6 @@ __global__ __launch_bounds__(step_threads(D)) void spqt_kv_step_kernel(Cache c, 
             Meeting m;
             m.top = w.units.top;
             m.total = columns_sum(w.total);
-            const float drop = w.units.drop();
-#pragma unroll
-            for (int i = 0; i < D / 16; ++i) w.acc[i] *= drop;
             for (int v = wave + 1; v < kStepWaves; ++v) {
                 if (begin_in_group(v) >= stop) break;
                 if (begin_in_group(v) == begin_in_group(v + 1)) continue;
@@ -456,7 +462,7 @@ __global__ __launch_bounds__(step_threads(D)) void spqt_kv_step_kernel(Cache c, 
                 for (int i = 0; i < D / 16; ++i) w.acc[i] = w.acc[i] * mine + *reinterpret_cast<const f32x4 *>(&sums[v][column][16 * i + 4 * quarter]) * others;
             }
             if (stop <= group_end) {
-                write_row(p, m, w.acc, 1.0f);
+                write_row(p, m, w.acc);
             } else if (column < live_rows(p)) {
                 const size_t slot = 2 * (size_t)place + 1;
 #pragma unroll

@@ -16,6 +16,9 @@ SPQT_BOTH float power_of_two(float x) { return __builtin_amdgcn_exp2f(x); }
 SPQT_BOTH float power_of_two(float x) { return exp2f(x); }
 #endif
 
+// (Limits for where there are no numbers.)
+SPQT_BOTH int drop_of(float unit, float top) { return (int)__builtin_fmaxf(-300.0f, __builtin_fminf(300.0f, unit - top)) - 15; }
+
 // Scores are in powers of two, a block's values are codes times part * 2^exponent with part from 1/2 to 1 (or NaN).  With m the largest score of a block that the row sees,
 //   top    >= every score so far: a probability is 2^(score - top), at most 1
 //   level  >= m + exponent of every block so far: no token adds more than 2^level times its code to the sums
@@ -47,8 +50,8 @@ struct LevelUnits {
         s.lift = sees ? part * power_of_two(__builtin_fminf(exponent + s.from - middle + 15.0f, 126.0f)) : 0.0f;
         return s;
     }
-    // The factor from the sums' units to units of 2^top.
-    SPQT_BOTH float drop() const { return level == -__builtin_inff() ? 0x1p-15f : power_of_two(level - top) * 0x1p-15f; }
+    // The sums are that power of two away from units of 2^top.
+    SPQT_BOTH int drop() const { return drop_of(level, top); }
 };
 
 // Many rows: a factor for every token would cost as much as its rounding, and the sums go to new units with every block anyway.
@@ -89,8 +92,8 @@ struct BlockUnits {
         s.back = power_of_two(-lift);
         return s;
     }
-    // The factor from the sums' units to units of 2^top.
-    SPQT_BOTH float drop() const { return (place == -__builtin_inff() ? 1.0f : power_of_two(place - top) * 0x1p-15f) * part; }
+    // The sums times part are that power of two away from units of 2^top.
+    SPQT_BOTH int drop() const { return drop_of(place, top); }
 };
 
 }  // namespace kv

@@ -51,6 +51,7 @@ def within(c, q, counts, window, out, scale=None, held=2.0 ** -21):
     each = [rows] * seqs if counts is None else counts
     scale = dim ** -0.5 if scale is None else scale
     want, _, _, sway, spread, _ = oracle.attention(c.codes.cpu(), c.scales.cpu(), c.table_host, c.length_of, q.cpu(), each, scale, window)
+    want = want.clamp(-torch.finfo(q.dtype).max, torch.finfo(q.dtype).max)      # outputs are the type's numbers, as values read back are
     L = max(c.length_of)
     u, smallest = (2.0 ** -11, 2.0 ** -24) if q.dtype == torch.float16 else (2.0 ** -8, 2.0 ** -133)
     off = 2 * (dim + 8) * E * sway + (L + 64) * E + held
@@ -142,4 +143,23 @@ def test_large_values_that_get_no_weight(gpu, heads, kv_heads, rows, wide, place
         widen(c)
     out, _ = attend(gpu, c, q, None)
     assert float(out.max()) < 2.0 and float(out.min()) > 0.5
+    assert within(c, q, None, 0, out) <= 1.0
+
+
+@pytest.mark.parametrize("dim", [64, 128, 192, 256])
+@pytest.mark.parametrize("heads,kv_heads,rows,wide", FORMS)
+@pytest.mark.parametrize("blocks", [1, 30, 100])
+@pytest.mark.parametrize("dtype", ["float16", "bfloat16"])
+def test_the_largest_values_there_are(gpu, dtype, blocks, heads, kv_heads, rows, wide, dim):  # noqa: F811
+    """Sums over up to 6400 tokens that meet in shared memory and in the workspace; 127 scale is beyond the type's largest number."""
+    c = Cache(gpu, 1, kv_heads, dim, getattr(torch, dtype), blocks, 13 + dim)
+    x = torch.randn((1, 64 * blocks, 2 * kv_heads, dim), generator=c.gen)
+    signs = torch.where(torch.arange(dim) % 3 == 0, -1.0, 1.0)
+    x[:, :, kv_heads:] = torch.finfo(c.dtype).max * signs
+    c.append(64 * blocks, x=x.to(c.dtype))
+    q = (0.05 * torch.randn((1, rows, heads, dim), generator=c.gen)).to(c.dtype).cuda()
+    if wide:
+        widen(c)
+    out, _ = attend(gpu, c, q, None)                       # (6 of 70 rows lie before the first of 64 tokens)
+    assert bool(torch.isfinite(out).all())
     assert within(c, q, None, 0, out) <= 1.0

@@ -16,6 +16,8 @@ using namespace spqt::kv;
 
 static auto see(BlockUnits &u, bool sees, float most, float part, float exponent) { return u.see(sees, most, part, 1.0f / part, exponent); }
 static auto see(LevelUnits &u, bool sees, float most, float part, float exponent) { return u.see(sees, most, part, exponent); }
+static float part_of(const BlockUnits &u) { return u.part; }
+static float part_of(const LevelUnits &) { return 1.0f; }
 static float probability(const BlockUnits::Step &step, float score, float &number) { return (number = exp2f(score - step.less)) * step.back; }
 static float probability(const LevelUnits::Step &step, float score, float &number) {
     const float p = exp2f(score - step.from);
@@ -46,7 +48,7 @@ static void go(int blocks, int n, const float *scores, const float *codes, const
             largest = fmaxf(largest, fabsf(acc));
         }
     }
-    result[0] = acc * (units.drop() / (total == 0.0f ? 1.0f : total));
+    result[0] = ldexpf(acc * part_of(units), units.drop() - 32) * (0x1p32f / (total == 0.0f ? 1.0f : total));
     result[1] = lifted;
     result[2] = largest;
 }
