@@ -84,7 +84,8 @@ int spqt_packed_bytes(int64_t M, int64_t K, int group, size_t *out_bytes);
  * that consumes a word puts it back to zero, so every call leaves the workspace all zeros: calls on
  * one stream, or replays of one graph, may share one workspace whatever their M, K, batch, launch
  * shape, kernel (dense / sparse / one launch) or layout (group, column-block, 8-bit), provided it is
- * large enough for each.  Two calls that may overlap in time (different streams) need two workspaces.
+ * large enough for each.  Two calls that may overlap in time (different streams) need two workspaces, and the
+ * attention of spqt_kv.h needs one of its own kind: it leaves other words and raises the poison flag.
  * Word 0 of the head is a poison flag: should a reducer ever abandon its bounded wait (it cannot
  * while the device makes progress), it writes NaN, raises the flag, and every later call on that
  * workspace yields NaN until spqt_workspace_init is run on it again - a late word of the abandoned

@@ -1,8 +1,8 @@
 /*
  * libspqt - a decoder's key/value cache in 8 bits: the append of new tokens, the attention that reads it, and the
  * eviction of what attention no longer weighs.  Between the GEMVs that make q, k and v and the one that takes the
- * attention's output.  All calls are DEVICE, async, and follow the conventions of spqt.h (status codes, streams, one
- * workspace per stream); lengths stay on the device, so a decode step can be captured in a graph.
+ * attention's output.  All calls are DEVICE, async, and follow the conventions of spqt.h (status codes, streams, a workspace
+ * for each stream); lengths stay on the device, so a decode step can be captured in a graph.
  *
  * A cache is a pool of pages.  A page holds 64 tokens of one layer for all its kv heads:
  *
@@ -89,7 +89,9 @@ int spqt_kv_workspace_bytes(int sequences, int rows, int q_heads, int kv_heads, 
  *   weights = decay * weights + sum over the call's rows and the heads that read its kv head of its probability
  * (decay 0 does not read them).
  * workspace: workspace_bytes >= spqt_kv_workspace_bytes, 256-byte aligned, prepared once with spqt_workspace_init;
- * every call leaves what the next one relies on, so calls on one stream may share one, whatever their shapes. */
+ * every call leaves what the next one relies on, so attention calls on one stream may share one, whatever their shapes.  Not
+ * with GEMVs: these rely on all zeros, and an attention leaves its partial sums.  It raises the flag that makes them yield NaN
+ * on its workspace until spqt_workspace_init, rather than take such a word for one of theirs. */
 int spqt_kv_attention(const spqt_kv_cache *cache, const spqt_kv_rows *q, const spqt_kv_rows *out, float *lse, int rows, const int32_t *counts,
                       int q_heads, float scale, int window, float decay, void *workspace, size_t workspace_bytes, void *stream);
 

@@ -35,8 +35,8 @@ extern "C" int spqt_kv_attention(const spqt_kv_cache *cache, const spqt_kv_rows 
     const bool prompt = is_prompt(cache->sequences, rows, a.group, cache->kv_heads, cache->head_dim, cache->max_blocks);
     if (!prompt && !step_fits(*cache, a)) return SPQT_ESHAPE;
     char *counters = (char *)workspace + kWorkspaceHead, *space = counters + kStepCounters;
-    if (prompt) launch_prompt(*cache, a, space, (hipStream_t)stream);
-    else launch_step(*cache, a, counters, space, (hipStream_t)stream);
+    if (prompt) launch_prompt(*cache, a, workspace, space, (hipStream_t)stream);
+    else launch_step(*cache, a, workspace, counters, space, (hipStream_t)stream);
     if (cache->weights) launch_weigh(*cache, a, (hipStream_t)stream);
     return launched();
 }

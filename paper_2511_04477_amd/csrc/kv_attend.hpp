@@ -152,17 +152,23 @@ __device__ __forceinline__ f32x4 scores_of(const u32x4 (&k)[D / 64], const f16x8
     return s;
 }
 
+// Partial sums stay in the workspace when a call is done, where a GEMV's exchange takes every word that is not 0 for one of its own.  So each call raises the poison flag that makes GEMVs
+// on the workspace give NaN (word 0 of its head): the two kinds of calls have workspaces of their own.
+__device__ __forceinline__ void poison_for_gemv(uint32_t *workspace) {
+    if (blockIdx.x == 0 && blockIdx.y == 0 && blockIdx.z == 0 && threadIdx.x == 0) *workspace = 1u;
+}
+
 // A few rows (kv_step.hip): what such calls need of the workspace, zeros first, and the call.
 constexpr size_t kStepCounters = 1024;                    // bytes of counters at the head of the workspace, all 0 between calls
 size_t step_bytes(int dim);                               // and what follows them
 bool step_fits(const spqt_kv_cache &cache, const Call &a);
-void launch_step(const spqt_kv_cache &cache, const Call &a, void *counters, void *space, hipStream_t stream);
+void launch_step(const spqt_kv_cache &cache, const Call &a, void *workspace, void *counters, void *space, hipStream_t stream);
 
 // Many rows (kv_prompt.hip): whether a call is of that kind, what such calls need of the workspace at most, and the call.
 constexpr int kFewRows = 64;                              // of a kv head, that are a few in any call
 bool is_prompt(int sequences, int rows, int group, int kv_heads, int dim, int max_blocks);
 size_t prompt_bytes(int dim);
-void launch_prompt(const spqt_kv_cache &cache, const Call &a, void *space, hipStream_t stream);
+void launch_prompt(const spqt_kv_cache &cache, const Call &a, void *workspace, void *space, hipStream_t stream);
 
 // What every token weighed in a call whose sums are known (kv_weigh.hip).
 void launch_weigh(const spqt_kv_cache &cache, const Call &a, hipStream_t stream);

@@ -99,6 +99,7 @@ __device__ __forceinline__ float halves_max(float v) {
 // Where the tokens are divided into parts: what each of them makes of a row, in units of 2^(its maximum + kRoom).
 struct Parts {
     int n;
+    uint32_t *head;      // of the workspace
     float *sums;         // [sequence][kv head][256 (128) rows][part][row][D]
     float *stats;        // the same of [2]: a row's maximum and sum
 };
@@ -125,6 +126,7 @@ __global__ __launch_bounds__(Shape<D>::kThreads) void spqt_kv_prompt_kernel(Cach
     const int s = blockIdx.z, head = blockIdx.x % c.kv_heads, tile = tiles - 1 - (int)(blockIdx.x / c.kv_heads);
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), column = lane & 31, half = lane >> 5;
     const int length = length_of(c, s), count = count_of(a.counts, s, a.rows), rows = a.rows * a.group;
+    poison_for_gemv(parts.head);
 
     // the blocks that any row of the workgroup sees
     const int r0 = tile * S::kRows;
@@ -390,7 +392,7 @@ bool is_prompt(int sequences, int rows, int group, int kv_heads, int dim, int ma
 
 size_t prompt_bytes(int dim) { return (size_t)kParted * rows_of(dim) * (dim + 2) * 4; }
 
-void launch_prompt(const spqt_kv_cache &cache, const Call &a, void *space, hipStream_t stream) {
+void launch_prompt(const spqt_kv_cache &cache, const Call &a, void *workspace, void *space, hipStream_t stream) {
     dispatch(cache, [&](auto dim, auto bf16) {
         constexpr int D = decltype(dim)::value;
         constexpr bool B = decltype(bf16)::value;
@@ -398,6 +400,7 @@ void launch_prompt(const spqt_kv_cache &cache, const Call &a, void *space, hipSt
         const int64_t units = (int64_t)tiles * cache.kv_heads * cache.sequences;
         Parts parts;
         parts.n = parts_of(units, cache.max_blocks);
+        parts.head = (uint32_t *)workspace;
         parts.sums = (float *)space;
         parts.stats = parts.sums + (size_t)units * parts.n * Shape<D>::kRows * D;
         hipLaunchKernelGGL((spqt_kv_prompt_kernel<D, B>), dim3((unsigned)tiles * cache.kv_heads, parts.n, cache.sequences), dim3(Shape<D>::kThreads), 0, stream,

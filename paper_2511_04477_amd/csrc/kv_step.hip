@@ -18,6 +18,7 @@ using namespace spqt::kv;
 
 // Where the sums of rows meet: two places for each workgroup, and a counter of what has come for the one unit that begins in it and goes on in others.
 struct Space {
+    uint32_t *head;      // of the workspace
     uint32_t *arrived;   // [kShares], all 0 between calls
     float *stats;        // [2 * kShares][16][2]: the rows' maxima and sums
     float *sums;         // [2 * kShares][16][D]
@@ -220,6 +221,7 @@ __global__ __launch_bounds__(step_threads(D)) void spqt_kv_step_kernel(Cache c, 
     __shared__ uint32_t order[2];
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), column = lane & 15, quarter = lane >> 4;
     const uint32_t units_each = (uint32_t)(c.kv_heads * tiles);          // of a sequence
+    poison_for_gemv(space.head);
 
     // the first 64 sequences stay in the lanes
     Span nearby = {0, 0, 0, 0};
@@ -551,9 +553,10 @@ bool step_fits(const spqt_kv_cache &cache, const Call &a) {
     return (int64_t)cache.sequences * cache.kv_heads * ((a.rows * a.group + 15) / 16) * cache.max_blocks <= 0x7FFFFFFF;
 }
 
-void launch_step(const spqt_kv_cache &cache, const Call &a, void *counters, void *space, hipStream_t stream) {
+void launch_step(const spqt_kv_cache &cache, const Call &a, void *workspace, void *counters, void *space, hipStream_t stream) {
     const int tiles = (a.rows * a.group + 15) / 16;
     Space s;
+    s.head = (uint32_t *)workspace;
     s.arrived = (uint32_t *)counters;
     s.stats = (float *)space;
     s.sums = s.stats + 2 * kShares * 32;

@@ -127,7 +127,7 @@ def spqt_kv_workspace_bytes(sequences: int, rows: int, q_heads: int, kv_heads: i
 
 
 def new_kv_workspace(sequences: int, rows: int, q_heads: int, kv_heads: int, head_dim: int, max_blocks: int, device="cuda"):
-    """Allocate and prepare a workspace tensor for spqt_kv_attention with up to this many rows."""
+    """Allocate and prepare a workspace tensor for spqt_kv_attention with up to this many rows; attention calls of one stream may share it, GEMVs may not."""
     torch = _b._torch or _b._load_torch()
     ws = torch.empty(spqt_kv_workspace_bytes(sequences, rows, q_heads, kv_heads, head_dim, max_blocks), dtype=torch.uint8, device=device)
     _b.spqt_workspace_init(ws)

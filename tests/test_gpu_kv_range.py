@@ -9,8 +9,11 @@ than 2^14 of the former.  The output: u |out| + spread times that + L e spread +
 import pytest
 import torch
 
+import oracle as gemv_oracle
 from oracle import kv as oracle
 from test_gpu_kv import Cache, E, EITHER, MANY, attend, case_cache, gpu, widen  # noqa: F401
+
+from workloads import make_weights, make_x, quantile_threshold
 
 pytestmark = pytest.mark.gpu
 
@@ -163,3 +166,34 @@ def test_the_largest_values_there_are(gpu, dtype, blocks, heads, kv_heads, rows,
     out, _ = attend(gpu, c, q, None)                       # (6 of 70 rows lie before the first of 64 tokens)
     assert bool(torch.isfinite(out).all())
     assert within(c, q, None, 0, out) <= 1.0
+
+
+@pytest.mark.parametrize("case", [(64, 8, 128, "float16", [1500], None, 1, 0), (8, 1, 128, "float16", [2100], None, 70, 0)], ids=["few", "many"])
+def test_a_gemv_does_not_take_words_of_an_attention_for_its_own(gpu, case):  # noqa: F811
+    """On an attention's workspace it gives NaN until the workspace is prepared again; with its own it is right."""
+    _, spqt = gpu
+    M, K = 1024, 2048
+    w, x_np = make_weights(M, K, 77), make_x(K, "laplace", 78)
+    thr = quantile_threshold(x_np, 0.5)
+    want = torch.from_numpy(gemv_oracle.gemv(w["q_rowmajor"], w["scales"], x_np, thr)[0])
+    packed, x = torch.from_numpy(spqt.spqt_pack(w["q_rowmajor"], w["scales"])).cuda(), torch.from_numpy(x_np[0].copy()).cuda()
+    idx, count = torch.empty(K, dtype=torch.int32, device="cuda"), torch.zeros(1, dtype=torch.int32, device="cuda")
+    spqt.spqt_gather(x, thr, idx, count)
+    y = torch.zeros(M, device="cuda")
+    c, q = case_cache(gpu, case, 36)
+    expected, _ = attend(gpu, c, q, None)
+    size = max(spqt.spqt_workspace_bytes(M, K, 1), spqt.spqt_kv_workspace_bytes(1, case[6], case[0], case[1], case[2], 64))
+    ws = torch.empty(size, dtype=torch.uint8, device="cuda")
+
+    def gemv():
+        spqt.spqt_gemv(packed, M, K, x, idx, count, y, ws, splits=4, waves=4)
+        return bool(((y.cpu().double() - want).abs() <= 1e-2 + 2e-3 * want.abs()).all())
+
+    spqt.spqt_workspace_init(ws)
+    assert gemv() and gemv()
+    out, _ = attend(gpu, c, q, None, workspace=ws)         # (a GEMV leaves the workspace all zeros)
+    assert out.equal(expected)
+    gemv()
+    assert bool(y.isnan().all())
+    spqt.spqt_workspace_init(ws)
+    assert gemv()
