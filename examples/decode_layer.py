@@ -79,7 +79,8 @@ class Layer:
         return self.project("o", out.view(rows, -1), 0.0)
 
     def evict(self):
-        spqt.spqt_kv_evict(self.codes, self.scales, self.tail, self.seen, self.table, self.lengths, self.budget, self.recent, self.spare, self.new_lengths, self.kept)
+        spqt.spqt_kv_evict(self.codes, self.scales, self.tail, self.seen, self.table, self.lengths, self.budget, self.recent, self.spare, self.new_lengths, self.kept,
+                           exact=True)              # what stays is moved again and again
         self.table, self.spare = self.spare, self.table
         self.lengths, self.new_lengths = self.new_lengths, self.lengths
         self.in_cache = self.budget

@@ -105,6 +105,14 @@ int spqt_kv_attention(const spqt_kv_cache *cache, const spqt_kv_rows *q, const s
 int spqt_kv_evict(const spqt_kv_cache *cache, int keep, int recent, const int32_t *new_table, int new_blocks, int32_t *new_lengths, int32_t *kept,
                   void *stream);
 
+/* The same for caches that are cut down again and again: codes times their scales are quantized as they are, not by way of 16-bit values.
+ *   new scale = scale(the largest |code * scale| of a block's kept tokens),   new code = code * (scale / new scale), the quotient in fp32, rounded to
+ *   the nearest integer, ties to even
+ * A block whose tokens all stay keeps its scale and its codes for good.  By way of fp16, 127 * scale may be rounded up and ask for the next scale: such a
+ * block grows by 0.03 % with every spqt_kv_evict on average (1 % after 50, 5 % at worst); by way of bf16, it does so once at most. */
+int spqt_kv_evict_exact(const spqt_kv_cache *cache, int keep, int recent, const int32_t *new_table, int new_blocks, int32_t *new_lengths, int32_t *kept,
+                        void *stream);
+
 #ifdef __cplusplus
 }
 #endif

@@ -8,6 +8,7 @@ for its bfloat16), from the definitions:
   code       x / scale rounded to the nearest integer
   a page     bytes code + 128: keys [token][element], values [element][place], place(t) = 16 (t / 4 % 4) + 4 (t / 16) + t % 4
   attention  s_t = scale q . k_t over the tokens that a row sees, p = exp(s - m) / sum, out = sum p_t v_t, lse = m + ln sum
+  moving     (exactly) the scale of the largest |code * scale|, and code * (old scale / new scale), the quotient in fp32, to nearest, ties to even
   eviction   the last `recent` tokens and the heaviest others, the earlier one of two that weigh the same
 """
 from __future__ import annotations
@@ -98,6 +99,15 @@ def attention(codes, scales, table, lengths, q, counts, scale, window):
         weights.append(per_head)
         weight_sway.append(per_sway)
     return out, lse, weights, sway, spread, weight_sway
+
+
+def requantize(parts):
+    """(codes [tokens, dim], their scale) of one head, several blocks' tokens -> (codes, scale) as one block, from code * scale as it is; None and NaN where a scale is none."""
+    if any(math.isnan(s) for _, s in parts):
+        return None, math.nan
+    scale = scale_of(max(float(c.abs().max()) * s for c, s in parts))
+    ratio = lambda s: (torch.tensor(s, dtype=torch.float32) / torch.tensor(scale, dtype=torch.float32)).clamp(max=128.0).double()  # noqa: E731
+    return torch.cat([torch.round(c.double() * ratio(s)) for c, s in parts]).long(), scale
 
 
 def choose(weights, length, keep, recent):

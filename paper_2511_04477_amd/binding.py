@@ -40,7 +40,7 @@ CB_EXPORTS = ["spqt_cb_packed_bytes", "spqt_cb_quantize", "spqt_cb_dequantize", 
               "spqt_cb_gemv_fused", "spqt_cbk_quantize", "spqt_cbk_dequantize", "spqt_cbk_gemv", "spqt_cbk_gemv_fused",
               "spqt_cb8_packed_bytes", "spqt_cb8_quantize", "spqt_cb8_dequantize", "spqt_cb8_gemv", "spqt_cb8_gemv_fused", "spqt_cb8_gemv_rows",
               "spqt_cb2_packed_bytes", "spqt_cb2_quantize", "spqt_cb2_dequantize", "spqt_cb2_gemv", "spqt_cb2_gemv_fused", "spqt_cb2_gemv_rows"]
-KV_EXPORTS = ["spqt_kv_append", "spqt_kv_read", "spqt_kv_workspace_bytes", "spqt_kv_attention", "spqt_kv_evict"]
+KV_EXPORTS = ["spqt_kv_append", "spqt_kv_read", "spqt_kv_workspace_bytes", "spqt_kv_attention", "spqt_kv_evict", "spqt_kv_evict_exact"]
 CB_CHUNK_BYTES = 18432
 CB8_CHUNK_BYTES = 17408
 CB2_CHUNK_BYTES = 20480
@@ -109,6 +109,7 @@ def lib() -> ctypes.CDLL:
         L.spqt_kv_workspace_bytes.argtypes = [i32, i32, i32, i32, i32, i32, c.POINTER(sz)]
         L.spqt_kv_attention.argtypes = [vp, vp, vp, vp, i32, vp, i32, c.c_float, i32, c.c_float, vp, sz, vp]
         L.spqt_kv_evict.argtypes = [vp, i32, i32, vp, i32, vp, vp, vp]
+        L.spqt_kv_evict_exact.argtypes = L.spqt_kv_evict.argtypes
         for name in EXPORTS[1:] + CB_EXPORTS + KV_EXPORTS:
             getattr(L, name).restype = i32
         # the device functions' addresses, for _fastcall

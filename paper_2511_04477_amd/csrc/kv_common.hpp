@@ -54,25 +54,28 @@ __device__ __forceinline__ uint32_t narrow2(float a, float b) {
     return __builtin_bit_cast(uint32_t, __builtin_convertvector(f32x2{a, b}, f16x2));
 }
 
-// The scale of a block whose largest |x| has these 16 bits (NaN and infinities order above all numbers, and give NaN).
-template <bool BF16>
-__device__ __forceinline__ float scale_of(uint32_t largest) {
-    if (largest >= (BF16 ? 0x7F80u : 0x7C00u)) return __builtin_nanf("");
-    float t = widen<BF16>((uint16_t)largest) / 127.0f;
+// The scale of a block whose largest |x| this is.
+__device__ __forceinline__ float scale_for(float largest) {
+    float t = largest / 127.0f;
     t = t > 0x1p-100f ? t : 0x1p-100f;
     const uint32_t bits = as_u32(t);
     uint32_t odd = (bits & ~0x1FFFu) | 0x1000u;
     if (odd < bits) odd += 0x2000u;
     return as_float(odd);
 }
+// The same from the 16 bits of the largest |x| (NaN and infinities order above all numbers, and give NaN).
+template <bool BF16>
+__device__ __forceinline__ float scale_of(uint32_t largest) {
+    return largest >= (BF16 ? 0x7F80u : 0x7C00u) ? __builtin_nanf("") : scale_for(widen<BF16>((uint16_t)largest));
+}
 
 // The stored byte of x in the lowest bits of a number, given 1 / scale: adding 1.5 2^23 rounds to the nearest integer.  x * inverse is x / scale to 2^-24 of
 // itself, and x / scale is at least 2^-20 of itself away from the middle between two integers, so it rounds as the quotient does.
 __device__ __forceinline__ uint32_t coded(float x, float inverse) { return as_u32(__builtin_fmaf(x, inverse, 12582912.0f + 128.0f)); }
 // Four of them; what is no number, in a block whose scale is none, is stored as 0.
-__device__ __forceinline__ uint32_t bytes_of(uint32_t a, uint32_t b, uint32_t c, uint32_t d, float inverse) {
+__device__ __forceinline__ uint32_t bytes_of(uint32_t a, uint32_t b, uint32_t c, uint32_t d, float scale) {
     const uint32_t low = __builtin_amdgcn_perm(b, a, 0x0C0C0400u), high = __builtin_amdgcn_perm(d, c, 0x04000C0Cu);
-    return inverse != inverse ? 0x80808080u : low | high;
+    return scale != scale ? 0x80808080u : low | high;
 }
 
 // The same for numbers that are finite or NaN and at most 127 times a scale: the type's largest number where they round to infinity.  127 scale_of(65504) = 65563.75 does; a bf16 never,

@@ -186,12 +186,13 @@ __global__ __launch_bounds__(kSelectThreads) void spqt_kv_select_kernel(Cache c,
     }
 }
 
-// Kept tokens as spqt_kv_read gives them, quantized as a new block: x = code * scale rounded to 16 bits, then as in the append.
+// Kept tokens quantized as a new block.  By way of 16 bits: x = code * scale as spqt_kv_read gives it, then as in the append.  EXACT: from code * scale itself, 20 bits at most; a block whose
+// tokens all stay then keeps its scale and codes, since 127 * scale asks for just that scale, while 127 * scale rounded to 11 bits may ask for the next one.  (Either takes the same time: selection and move of the two sequences below 55.4 and 54.9 us, of the 32 heads 24.2 and 24.0.)
 // One workgroup per new page, head and side.  Keys are whole lines of a token; values, a byte of each of D lines, are read a token per lane, since tokens that are kept of one page
 // then share lines.
 // What bounds it: those lines.  27000 and 33001 tokens of 8 heads of 128, 8192 kept of each, 37 us for the 68 MB of the codes that are kept and written; where nearly all are kept
 // (2048 of 2300, 32 heads) 15.7 us for 34 MB.
-template <int D, bool BF16>
+template <int D, bool BF16, bool EXACT>
 __global__ __launch_bounds__(kTileThreads) void spqt_kv_move_kernel(Cache c, int keep, const int32_t *new_table, int new_blocks, const int32_t *kept) {
     __shared__ Tile<D> tile;
     __shared__ uint32_t pages[kBlock], tokens[kBlock];
@@ -219,7 +220,12 @@ __global__ __launch_bounds__(kTileThreads) void spqt_kv_move_kernel(Cache c, int
         if (which == 0 && there) c.weights[weight_at(c, page, head) + threadIdx.x] = 0.0f;
     }
     __syncthreads();
-    uint32_t pair = 0;
+    uint32_t pair = 0;                                    // the largest magnitudes of a pair of numbers, or the largest code * scale
+    auto larger = [&](int token, uint32_t code) {
+        const float x = (float)code * scales[token];
+        pair = as_u32(x) > pair ? as_u32(x) : pair;
+    };
+    auto magnitude = [](uint32_t byte) { return byte > 128 ? byte - 128 : 128 - byte; };
     if (which == 0) {
         u32x2 bytes[D / 32];
 #pragma unroll
@@ -231,23 +237,59 @@ __global__ __launch_bounds__(kTileThreads) void spqt_kv_move_kernel(Cache c, int
         for (int n = 0; n < D / 32; ++n) {
             const int p = (int)threadIdx.x + n * kTileThreads, i = p / (D / 8);
             u32x4 x;
+            uint32_t most = 0;
 #pragma unroll
-            for (int j = 0; j < 4; ++j)
-                x[j] = values_of<BF16>(bytes[n][j / 2] >> (16 * (j % 2)) & 255, bytes[n][j / 2] >> (16 * (j % 2) + 8) & 255, scales[i]);
+            for (int j = 0; j < 4; ++j) {
+                const uint32_t first = bytes[n][j / 2] >> (16 * (j % 2)) & 255, second = bytes[n][j / 2] >> (16 * (j % 2) + 8) & 255;
+                x[j] = EXACT ? first | second << 16 : values_of<BF16>(first, second, scales[i]);
+                most = magnitude(first) > most ? magnitude(first) : most;
+                most = magnitude(second) > most ? magnitude(second) : most;
+            }
             tile.put(i, p % (D / 8) * 8, x);
-            if (i < to) pair = larger_pair(larger_pair(pair, x.x), larger_pair(x.y, larger_pair(x.z, x.w)));
+            if (EXACT && i < to) larger(i, most);
+            if (!EXACT && i < to) pair = larger_pair(larger_pair(pair, x.x), larger_pair(x.y, larger_pair(x.z, x.w)));
         }
     } else {
         // a token per lane: those that lie in one page have their bytes of an element in one line
         const int i = threadIdx.x & 63;
         const uint8_t *in = c.codes + codes_at(c, pages[i], head, 1) + place_of((int)tokens[i]);
         const float scale = scales[i];
+        uint32_t most = 0;
 #pragma unroll 8
         for (int d = (int)(threadIdx.x >> 6) * 2; d < D; d += kTileThreads / 64 * 2) {
-            const uint32_t x = values_of<BF16>(in[d * kBlock], in[(d + 1) * kBlock], scale);
+            const uint32_t first = in[d * kBlock], second = in[(d + 1) * kBlock];
+            const uint32_t x = EXACT ? first | second << 16 : values_of<BF16>(first, second, scale);
             *reinterpret_cast<uint32_t *>(&tile.v[i][d]) = x;
-            if (i < to) pair = larger_pair(pair, x);
+            if (EXACT) {
+                most = magnitude(first) > most ? magnitude(first) : most;
+                most = magnitude(second) > most ? magnitude(second) : most;
+            } else if (i < to) {
+                pair = larger_pair(pair, x);
+            }
         }
+        if (EXACT && i < to) larger(i, most);
+    }
+    if (EXACT) {
+        const uint32_t largest = largest_number(tile, pair);
+        const float scale = largest >= 0x7F800000u ? __builtin_nanf("") : scale_for(as_float(largest));
+        if (!there) return;
+        // old scale / new scale; more than 128 only where the token's codes are all 0
+        if (threadIdx.x < kBlock) scales[threadIdx.x] = __builtin_fminf(scales[threadIdx.x] / scale, 128.0f);
+        __syncthreads();
+        // code times that to the nearest integer, in one rounding
+        auto code = [&](uint32_t pair, int upper, int t) {
+            return as_u32(__builtin_fmaf((float)((int)(upper ? pair >> 16 : pair & 0xFFFFu) - 128), scales[t], 12582912.0f + 128.0f));
+        };
+        store_codes(c, tile, page, head, which, 0, to, scale, code);
+        if (threadIdx.x == 0) c.scales[scale_at(c, page, head, which)] = scale;
+        if (to == kBlock) return;
+        uint16_t *tail = c.tail + (((size_t)s * c.kv_heads + head) * 2 + which) * (size_t)(kBlock * D);
+        for (int p = (int)threadIdx.x; p < to * (D / 2); p += kTileThreads) {
+            const int t = p / (D / 2), d = p % (D / 2) * 2;
+            const uint32_t pair = *reinterpret_cast<const uint32_t *>(&tile.v[t][d]);
+            *reinterpret_cast<uint32_t *>(tail + p * 2) = values_of<BF16>(code(pair, 0, t) & 255, code(pair, 1, t) & 255, scale);
+        }
+        return;
     }
     const float scale = scale_of<BF16>(largest_of(tile, pair));
     if (!there) return;
@@ -262,8 +304,7 @@ __global__ __launch_bounds__(kTileThreads) void spqt_kv_move_kernel(Cache c, int
 
 }  // namespace
 
-extern "C" int spqt_kv_evict(const spqt_kv_cache *cache, int keep, int recent, const int32_t *new_table, int new_blocks, int32_t *new_lengths, int32_t *kept,
-                             void *stream) {
+static int evict(const spqt_kv_cache *cache, int keep, int recent, const int32_t *new_table, int new_blocks, int32_t *new_lengths, int32_t *kept, void *stream, bool exact) {
     const int rc = check_cache(cache, true);
     if (rc != SPQT_OK) return rc;
     if (!cache->weights || !new_table || !new_lengths || !kept || new_lengths == cache->lengths || new_table == cache->table) return SPQT_EINVAL;
@@ -278,8 +319,21 @@ extern "C" int spqt_kv_evict(const spqt_kv_cache *cache, int keep, int recent, c
     const int most = cache->max_blocks < (keep + kBlock - 1) / kBlock ? cache->max_blocks : (keep + kBlock - 1) / kBlock;
     const dim3 grid(most, 2 * cache->kv_heads, cache->sequences);
     dispatch(*cache, [&](auto dim, auto bf16) {
-        hipLaunchKernelGGL((spqt_kv_move_kernel<decltype(dim)::value, decltype(bf16)::value>), grid, dim3(kTileThreads), 0, (hipStream_t)stream, view(*cache), keep,
-                           new_table, new_blocks, kept);
+        auto launch = [&](auto kernel) {
+            hipLaunchKernelGGL(kernel, grid, dim3(kTileThreads), 0, (hipStream_t)stream, view(*cache), keep, new_table, new_blocks, kept);
+        };
+        if (exact) launch(spqt_kv_move_kernel<decltype(dim)::value, decltype(bf16)::value, true>);
+        else launch(spqt_kv_move_kernel<decltype(dim)::value, decltype(bf16)::value, false>);
     });
     return launched();
+}
+
+extern "C" int spqt_kv_evict(const spqt_kv_cache *cache, int keep, int recent, const int32_t *new_table, int new_blocks, int32_t *new_lengths, int32_t *kept,
+                             void *stream) {
+    return evict(cache, keep, recent, new_table, new_blocks, new_lengths, kept, stream, false);
+}
+
+extern "C" int spqt_kv_evict_exact(const spqt_kv_cache *cache, int keep, int recent, const int32_t *new_table, int new_blocks, int32_t *new_lengths, int32_t *kept,
+                                   void *stream) {
+    return evict(cache, keep, recent, new_table, new_blocks, new_lengths, kept, stream, true);
 }

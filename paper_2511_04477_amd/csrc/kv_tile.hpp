@@ -27,10 +27,9 @@ __device__ __forceinline__ uint32_t larger_pair(uint32_t a, uint32_t b) {
     typedef uint16_t u16x2 __attribute__((ext_vector_type(2)));
     return __builtin_bit_cast(uint32_t, __builtin_elementwise_max(__builtin_bit_cast(u16x2, a & 0x7FFF7FFFu), __builtin_bit_cast(u16x2, b & 0x7FFF7FFFu)));
 }
-// The largest magnitude (16 bits) of all threads' pairs.
+// The largest number of all threads'.
 template <int D>
-__device__ __forceinline__ uint32_t largest_of(Tile<D> &tile, uint32_t pair) {
-    uint32_t m = (pair & 0x7FFFu) > (pair >> 16 & 0x7FFFu) ? (pair & 0x7FFFu) : (pair >> 16 & 0x7FFFu);
+__device__ __forceinline__ uint32_t largest_number(Tile<D> &tile, uint32_t m) {
 #pragma unroll
     for (int step = 32; step >= 1; step /= 2) {
         const uint32_t other = (uint32_t)__shfl_xor((int)m, step);
@@ -43,6 +42,11 @@ __device__ __forceinline__ uint32_t largest_of(Tile<D> &tile, uint32_t pair) {
     for (int w = 1; w < kTileThreads / 64; ++w) m = tile.largest[w] > m ? tile.largest[w] : m;
     return m;
 }
+// The largest magnitude (16 bits) of all threads' pairs.
+template <int D>
+__device__ __forceinline__ uint32_t largest_of(Tile<D> &tile, uint32_t pair) {
+    return largest_number(tile, (pair & 0x7FFFu) > (pair >> 16 & 0x7FFFu) ? (pair & 0x7FFFu) : (pair >> 16 & 0x7FFFu));
+}
 
 // The lower or upper one of two numbers.
 template <bool BF16>
@@ -51,20 +55,19 @@ __device__ __forceinline__ float half_of(uint32_t pair, int upper) {
     return widen<false>((uint16_t)(upper ? pair >> 16 : pair & 0xFFFFu));
 }
 
-// Quantizes tokens from .. to - 1 of the tile into the page.
-template <int D, bool BF16>
-__device__ __forceinline__ void store_tile(const Cache &c, const Tile<D> &tile, uint32_t page, int head, int which, int from, int to, float scale) {
-    const float inverse = 1.0f / scale;
+// Quantizes tokens from .. to - 1 of the tile into the page.  code(pair, upper, t): the stored byte, in the lowest bits of a number, of the lower or upper one of two elements of token t.
+template <int D, class F>
+__device__ __forceinline__ void store_codes(const Cache &c, const Tile<D> &tile, uint32_t page, int head, int which, int from, int to, float scale, F code) {
     uint8_t *out = c.codes + codes_at(c, page, head, which);
     if (which == 0) {
         for (int p = from * (D / 16) + (int)threadIdx.x; p < to * (D / 16); p += kTileThreads) {
             const u32x2 *x = reinterpret_cast<const u32x2 *>(&tile.v[p / (D / 16)][p % (D / 16) * 16]);
             uint32_t c[16];
 #pragma unroll
-            for (int i = 0; i < 16; ++i) c[i] = coded(half_of<BF16>(x[i / 4][i / 2 % 2], i % 2), inverse);
+            for (int i = 0; i < 16; ++i) c[i] = code(x[i / 4][i / 2 % 2], i % 2, p / (D / 16));
             u32x4 w;
 #pragma unroll
-            for (int i = 0; i < 4; ++i) w[i] = bytes_of(c[4 * i], c[4 * i + 1], c[4 * i + 2], c[4 * i + 3], inverse);
+            for (int i = 0; i < 4; ++i) w[i] = bytes_of(c[4 * i], c[4 * i + 1], c[4 * i + 2], c[4 * i + 3], scale);
             *reinterpret_cast<u32x4 *>(out + p * 16) = w;
         }
         return;
@@ -76,12 +79,11 @@ __device__ __forceinline__ void store_tile(const Cache &c, const Tile<D> &tile, 
 #pragma unroll
             for (int n = 0; n < 4; ++n) {
                 uint32_t x[4];
+                const int t = 16 * n + 4 * quarter;
 #pragma unroll
-                for (int i = 0; i < 4; ++i) x[i] = *reinterpret_cast<const uint32_t *>(&tile.v[16 * n + 4 * quarter + i][d]);
+                for (int i = 0; i < 4; ++i) x[i] = *reinterpret_cast<const uint32_t *>(&tile.v[t + i][d]);
 #pragma unroll
-                for (int e = 0; e < 2; ++e)
-                    w[e][n] = bytes_of(coded(half_of<BF16>(x[0], e), inverse), coded(half_of<BF16>(x[1], e), inverse), coded(half_of<BF16>(x[2], e), inverse),
-                                       coded(half_of<BF16>(x[3], e), inverse), inverse);
+                for (int e = 0; e < 2; ++e) w[e][n] = bytes_of(code(x[0], e, t), code(x[1], e, t + 1), code(x[2], e, t + 2), code(x[3], e, t + 3), scale);
             }
 #pragma unroll
             for (int e = 0; e < 2; ++e) *reinterpret_cast<u32x4 *>(out + (d + e) * kBlock + 16 * quarter) = w[e];
@@ -96,9 +98,7 @@ __device__ __forceinline__ void store_tile(const Cache &c, const Tile<D> &tile, 
 #pragma unroll
         for (int i = 0; i < 4; ++i) x[i] = *reinterpret_cast<const uint32_t *>(&tile.v[t + i][d]);
 #pragma unroll
-        for (int e = 0; e < 2; ++e)
-            w[e] = bytes_of(coded(half_of<BF16>(x[0], e), inverse), coded(half_of<BF16>(x[1], e), inverse), coded(half_of<BF16>(x[2], e), inverse),
-                            coded(half_of<BF16>(x[3], e), inverse), inverse);
+        for (int e = 0; e < 2; ++e) w[e] = bytes_of(code(x[0], e, t), code(x[1], e, t + 1), code(x[2], e, t + 2), code(x[3], e, t + 3), scale);
 #pragma unroll
         for (int e = 0; e < 2; ++e) {
             uint8_t *at = out + (d + e) * kBlock + word * 4;
@@ -111,6 +111,13 @@ __device__ __forceinline__ void store_tile(const Cache &c, const Tile<D> &tile, 
             }
         }
     }
+}
+
+// The same of 16-bit values.
+template <int D, bool BF16>
+__device__ __forceinline__ void store_tile(const Cache &c, const Tile<D> &tile, uint32_t page, int head, int which, int from, int to, float scale) {
+    const float inverse = 1.0f / scale;
+    store_codes(c, tile, page, head, which, from, to, scale, [&](uint32_t pair, int upper, int) { return coded(half_of<BF16>(pair, upper), inverse); });
 }
 
 }  // namespace kv

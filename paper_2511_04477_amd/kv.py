@@ -157,11 +157,13 @@ def spqt_kv_attention(codes, scales, table, lengths, q, out, workspace, scale=No
                                    float(scale), int(window), float(decay), wp, workspace.numel(), _b._stream_ptr(stream)))
 
 
-def spqt_kv_evict(codes, scales, tail, weights, table, lengths, keep: int, recent: int, new_table, new_lengths, kept, stream=None) -> None:
+def spqt_kv_evict(codes, scales, tail, weights, table, lengths, keep: int, recent: int, new_table, new_lengths, kept, stream=None, exact: bool = False) -> None:
     """Cuts every sequence down to `keep` tokens per kv head, the last `recent` ones and the heaviest others, and moves them to the pages
-    of new_table int32 [sequences, new_blocks].  new_lengths int32 [sequences] and kept int32 [sequences, kv_heads, keep] are written."""
+    of new_table int32 [sequences, new_blocks].  new_lengths int32 [sequences] and kept int32 [sequences, kv_heads, keep] are written.
+    exact: tokens move without a rounding to 16 bits in between (spqt_kv_evict_exact), as caches that are cut down again and again need it."""
+    name = "spqt_kv_evict_exact" if exact else "spqt_kv_evict"
     if _b._fast is not None:
-        rc = _b._fast.kv_evict((_b._lib or lib()).at["spqt_kv_evict"], codes, scales, tail, weights, table, lengths, keep, recent, new_table, new_lengths, kept, stream)
+        rc = _b._fast.kv_evict((_b._lib or lib()).at[name], codes, scales, tail, weights, table, lengths, keep, recent, new_table, new_lengths, kept, stream)
         if rc is not None:
             return _check(rc)
     torch = _b._torch or _b._load_torch()
@@ -170,4 +172,4 @@ def spqt_kv_evict(codes, scales, tail, weights, table, lengths, keep: int, recen
     np_ = _tensor(new_table, torch.int32, (cache.sequences, None), "new_table", device)
     lp = _tensor(new_lengths, torch.int32, (cache.sequences,), "new_lengths", device)
     kp = _tensor(kept, torch.int32, (cache.sequences, cache.kv_heads, int(keep)), "kept", device)
-    _check(lib().spqt_kv_evict(ctypes.byref(cache), int(keep), int(recent), np_, new_table.shape[1], lp, kp, _b._stream_ptr(stream)))
+    _check(getattr(lib(), name)(ctypes.byref(cache), int(keep), int(recent), np_, new_table.shape[1], lp, kp, _b._stream_ptr(stream)))
