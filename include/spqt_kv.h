@@ -26,6 +26,12 @@
  * from the tail: what a block holds depends on its tokens only, not on the calls in which they came.  A block that was
  * given an infinity or a NaN has the scale NaN, and every row that sees a token of it has NaN outputs.
  *
+ * Lengths grow by the appended counts and fall by an eviction only.  An append keeps the open block's scale, and takes the
+ * tail for the values of that block: after lengths that were merely set back it would requantize from tokens that are gone,
+ * or from another block's.  To take tokens back (drafts that were rejected), put back what their append has changed behind
+ * the tokens that stay, and then the lengths: the codes and scales of the page that was open, and the sequence's tail, as
+ * they were before it.  Pages that the tokens have begun need nothing; an append to an empty block reads neither.
+ *
  * Positions.  The call's row i (i < counts[s], or `rows` without counts) of sequence s is the token at position
  * lengths[s] - counts[s] + i.  Lengths outside 0 .. 64 * max_blocks and counts outside 0 .. rows are taken as the nearest
  * of these.  A table entry outside 0 .. pages - 1 is not followed: what would be written there is dropped, and what

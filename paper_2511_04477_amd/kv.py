@@ -10,6 +10,9 @@ A cache is a handful of tensors that the caller owns (`new_kv_cache` makes them)
 `lengths` count the tokens of the call: a decode step adds them first (`lengths += 1`), once for all layers.  16-bit
 tensors [sequences, rows, heads, head_dim] may be slices of a larger one as long as the last dimension is dense and the
 strides are multiples of 8.  `counts`, int32 [sequences], says how many of a call's rows a sequence has (None: all).
+
+Lengths are never merely set back: to take tokens back (drafts that were rejected), put back the codes and scales of the page
+that was open before their append, and the sequence's tail, from copies made then, and the lengths after that.
 """
 from __future__ import annotations
 
@@ -93,7 +96,7 @@ def new_kv_cache(pages: int, kv_heads: int, head_dim: int, sequences: int, dtype
 
 
 def spqt_kv_append(codes, scales, tail, table, lengths, k, v, counts=None, weights=None, stream=None) -> None:
-    """Quantizes k and v [sequences, rows, kv_heads, head_dim] into the cache as the last counts[s] of lengths[s] tokens."""
+    """Quantizes k and v [sequences, rows, kv_heads, head_dim] into the cache as the last counts[s] of lengths[s] tokens, which follow those of earlier calls."""
     if _b._fast is not None:
         rc = _b._fast.kv_append((_b._lib or lib()).at["spqt_kv_append"], codes, scales, tail, table, lengths, k, v, counts, weights, stream)
         if rc is not None:

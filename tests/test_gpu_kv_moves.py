@@ -131,3 +131,33 @@ def test_blocks_of_zeros_and_of_no_numbers_move(gpu):  # noqa: F811
         parts = [(oracle.page_codes(before[0][int(old[0, b]), 0], which)[rows], float(before[1][int(old[0, b]), 0, which])) for b, rows in ((0, slice(0, 14)), (1, slice(0, 36)))]
         expected, scale = oracle.requantize(parts)
         assert float(scales[page, 0, which]) == scale and torch.equal(oracle.page_codes(codes[page, 0], which)[:50], expected)
+
+
+@pytest.mark.parametrize("dtype", ["float16", "bfloat16"])
+@pytest.mark.parametrize("before,drafts", [(70, 5), (70, 90), (64, 3), (127, 1), (60, 200)])
+def test_drafts_that_are_taken_back(gpu, dtype, before, drafts):  # noqa: F811
+    """With the open page and the tail put back, the cache goes on as if they had never come, also with drafts that are larger and that fill the block."""
+    _, spqt = gpu
+    c, d = (Cache(gpu, 2, 2, 128, getattr(torch, dtype), 6, 54) for _ in range(2))
+    x = c.values(before)
+    for one in (c, d):
+        one.append(before, [before, 1], x=x)
+    pages = [int(c.table_host[0, before // 64]), int(c.table_host[1, 0])]
+    saved = [t.clone() for t in (c.codes[pages], c.scales[pages], c.tail)]
+    y = 20.0 * torch.randn((2, drafts, 4, 128), generator=c.gen)
+    c.append(drafts, x=y.to(c.dtype))
+    c.codes[pages], c.scales[pages] = saved[0], saved[1]
+    c.tail.copy_(saved[2])
+    c.length_of = [before, 1]
+    c.tokens = [[t[s][:n] for s, n in enumerate(c.length_of)] for t in c.tokens]
+    z = c.values(40, 1.0)
+    for one in (c, d):
+        one.append(40, x=z)
+    for s, n in enumerate(c.length_of):
+        for b in range(-(-n // 64)):
+            page, here = int(c.table_host[s, b]), min(64, n - 64 * b)
+            assert torch.equal(c.scales[page], d.scales[page])
+            for h in range(2):
+                for which in (0, 1):
+                    assert torch.equal(oracle.page_codes(c.codes[page, h].cpu(), which)[:here], oracle.page_codes(d.codes[page, h].cpu(), which)[:here])
+        assert torch.equal(c.tail[s, :, :, : n % 64].view(torch.int16), d.tail[s, :, :, : n % 64].view(torch.int16))
