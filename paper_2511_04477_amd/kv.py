@@ -34,6 +34,17 @@ class KvRowsView(ctypes.Structure):
     _fields_ = [("data", ctypes.c_void_p), ("sequence", ctypes.c_int64), ("row", ctypes.c_int64), ("head", ctypes.c_int64)]
 
 
+def _int32(v, what):
+    """v as an int that a C int holds; ctypes would keep the lowest 32 bits of any other."""
+    try:
+        n = int(v)
+    except (TypeError, ValueError, OverflowError):
+        raise SpqtError(f"{what}: need an integer") from None
+    if not -(1 << 31) <= n < 1 << 31:
+        raise SpqtError(f"{what}: {n} is beyond 32 bits")
+    return n
+
+
 def _tensor(t, dtype, shape, what, device=None):
     """Device pointer of a contiguous tensor; None in the shape stands for any extent."""
     if not (isinstance(t, _b._torch.Tensor) and t.is_cuda and t.is_contiguous() and t.dtype == dtype):
@@ -68,7 +79,8 @@ def _cache(codes, scales, table, lengths, dtype, tail=None, weights=None):
     return KvCacheView(cp, _tensor(scales, torch.float32, (pages, heads, 2), "scales", codes.device),
                        None if tail is None else _tensor(tail, dtype, (sequences, heads, 2, KV_BLOCK, dim), "tail", codes.device),
                        None if weights is None else _tensor(weights, torch.float32, (pages, heads, KV_BLOCK), "weights", codes.device),
-                       tp, _tensor(lengths, torch.int32, (sequences,), "lengths", codes.device), pages, sequences, blocks, heads, dim,
+                       tp, _tensor(lengths, torch.int32, (sequences,), "lengths", codes.device), pages, _int32(sequences, "sequences"), _int32(blocks, "blocks of the table"),
+                       _int32(heads, "kv heads"), _int32(dim, "head_dim"),
                        1 if dtype == torch.bfloat16 else 0)
 
 
@@ -105,7 +117,7 @@ def spqt_kv_append(codes, scales, tail, table, lengths, k, v, counts=None, weigh
     cache = _cache(codes, scales, table, lengths, dtype, tail, weights)
     shape = (cache.sequences, None, cache.kv_heads, cache.head_dim)
     keys, values = _rows(k, dtype, shape, "k", codes.device), _rows(v, dtype, (cache.sequences, k.shape[1]) + shape[2:], "v", codes.device)
-    _check(lib().spqt_kv_append(ctypes.byref(cache), ctypes.byref(keys), ctypes.byref(values), k.shape[1], _counts(counts, cache, codes.device),
+    _check(lib().spqt_kv_append(ctypes.byref(cache), ctypes.byref(keys), ctypes.byref(values), _int32(k.shape[1], "rows"), _counts(counts, cache, codes.device),
                                 _b._stream_ptr(stream)))
 
 
@@ -119,13 +131,14 @@ def spqt_kv_read(codes, scales, table, lengths, k_out, v_out, counts=None, strea
     cache = _cache(codes, scales, table, lengths, dtype)
     shape = (cache.sequences, None, cache.kv_heads, cache.head_dim)
     keys, values = _rows(k_out, dtype, shape, "k_out", codes.device), _rows(v_out, dtype, (cache.sequences, k_out.shape[1]) + shape[2:], "v_out", codes.device)
-    _check(lib().spqt_kv_read(ctypes.byref(cache), ctypes.byref(keys), ctypes.byref(values), k_out.shape[1], _counts(counts, cache, codes.device),
+    _check(lib().spqt_kv_read(ctypes.byref(cache), ctypes.byref(keys), ctypes.byref(values), _int32(k_out.shape[1], "rows"), _counts(counts, cache, codes.device),
                               _b._stream_ptr(stream)))
 
 
 def spqt_kv_workspace_bytes(sequences: int, rows: int, q_heads: int, kv_heads: int, head_dim: int, max_blocks: int) -> int:
     out = ctypes.c_size_t()
-    _check(lib().spqt_kv_workspace_bytes(sequences, rows, q_heads, kv_heads, head_dim, max_blocks, ctypes.byref(out)))
+    sizes = [_int32(n, "spqt_kv_workspace_bytes") for n in (sequences, rows, q_heads, kv_heads, head_dim, max_blocks)]
+    _check(lib().spqt_kv_workspace_bytes(*sizes, ctypes.byref(out)))
     return out.value
 
 
@@ -156,8 +169,8 @@ def spqt_kv_attention(codes, scales, table, lengths, q, out, workspace, scale=No
     wp = _tensor(workspace, _b._torch.uint8, (None,), "workspace", device)
     if scale is None:
         scale = cache.head_dim ** -0.5
-    _check(lib().spqt_kv_attention(ctypes.byref(cache), ctypes.byref(qv), ctypes.byref(ov), lp, q.shape[1], _counts(counts, cache, device), q.shape[2],
-                                   float(scale), int(window), float(decay), wp, workspace.numel(), _b._stream_ptr(stream)))
+    _check(lib().spqt_kv_attention(ctypes.byref(cache), ctypes.byref(qv), ctypes.byref(ov), lp, _int32(q.shape[1], "rows"), _counts(counts, cache, device),
+                                   _int32(q.shape[2], "q heads"), float(scale), _int32(window, "window"), float(decay), wp, workspace.numel(), _b._stream_ptr(stream)))
 
 
 def spqt_kv_evict(codes, scales, tail, weights, table, lengths, keep: int, recent: int, new_table, new_lengths, kept, stream=None, exact: bool = False) -> None:
@@ -174,5 +187,6 @@ def spqt_kv_evict(codes, scales, tail, weights, table, lengths, keep: int, recen
     device = codes.device
     np_ = _tensor(new_table, torch.int32, (cache.sequences, None), "new_table", device)
     lp = _tensor(new_lengths, torch.int32, (cache.sequences,), "new_lengths", device)
-    kp = _tensor(kept, torch.int32, (cache.sequences, cache.kv_heads, int(keep)), "kept", device)
-    _check(getattr(lib(), name)(ctypes.byref(cache), int(keep), int(recent), np_, new_table.shape[1], lp, kp, _b._stream_ptr(stream)))
+    keep, recent = _int32(keep, "keep"), _int32(recent, "recent")
+    kp = _tensor(kept, torch.int32, (cache.sequences, cache.kv_heads, keep), "kept", device)
+    _check(getattr(lib(), name)(ctypes.byref(cache), keep, recent, np_, _int32(new_table.shape[1], "blocks of new_table"), lp, kp, _b._stream_ptr(stream)))

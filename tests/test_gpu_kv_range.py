@@ -11,7 +11,7 @@ import torch
 
 import oracle as gemv_oracle
 from oracle import kv as oracle
-from test_gpu_kv import Cache, E, EITHER, MANY, attend, case_cache, gpu, widen  # noqa: F401
+from test_gpu_kv import CASES, Cache, E, EITHER, MANY, attend, case_cache, gpu, widen  # noqa: F401
 
 from workloads import make_weights, make_x, quantile_threshold
 
@@ -197,3 +197,36 @@ def test_a_gemv_does_not_take_words_of_an_attention_for_its_own(gpu, case):  # n
     assert bool(y.isnan().all())
     spqt.spqt_workspace_init(ws)
     assert gemv()
+
+
+@pytest.mark.parametrize("fast", [True, False])
+@pytest.mark.parametrize("size", [1 << 31, (1 << 32) + 16, -(1 << 32) + 16, 1 << 64, float("inf"), "many"])
+def test_numbers_beyond_32_bits_are_refused(gpu, size, fast, monkeypatch):  # noqa: F811
+    """Not taken by their lowest 32 bits: a window of 2^32 + 16 would be one of 16."""
+    _, spqt = gpu
+    if not fast:
+        from paper_2511_04477_amd import binding
+        monkeypatch.setattr(binding, "_fast", None)
+    c, q = case_cache(gpu, CASES[2], 37)
+    out, ws = torch.zeros_like(q), spqt.new_kv_workspace(3, 1, 8, 2, 128, 4)
+    with pytest.raises(spqt.SpqtError):
+        spqt.spqt_kv_attention(c.codes, c.scales, c.table, c.lengths, q, out, ws, window=size)
+    new_lengths = torch.zeros(3, dtype=torch.int32, device="cuda")
+    for keep, recent in ((64, size), (size, 3)):
+        kept = torch.zeros((3, 2, 64), dtype=torch.int32, device="cuda")
+        with pytest.raises(spqt.SpqtError):
+            spqt.spqt_kv_evict(c.codes, c.scales, c.tail, c.weights, c.table[:, :2].contiguous(), c.lengths, keep, recent, c.table[:, 2:].contiguous(), new_lengths, kept)
+    assert not bool(out.any()) and not bool(new_lengths.any())
+    for at in range(6):
+        sizes = [3, 1, 8, 2, 128, 4]
+        sizes[at] = size
+        with pytest.raises(spqt.SpqtError):
+            spqt.spqt_kv_workspace_bytes(*sizes)
+
+
+def test_windows_up_to_31_bits_see_everything(gpu):  # noqa: F811
+    c, q = case_cache(gpu, CASES[2], 37)
+    want = attend(gpu, c, q, None)
+    for window in (1 << 24, (1 << 31) - 1):
+        got = attend(gpu, c, q, None, window)
+        assert got[0].equal(want[0]) and got[1].equal(want[1])
