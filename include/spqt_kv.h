@@ -94,6 +94,8 @@ int spqt_kv_workspace_bytes(int sequences, int rows, int q_heads, int kv_heads, 
  * decay: with cache->weights, and lse given, every token t of the sequence gets
  *   weights = decay * weights + sum over the call's rows and the heads that read its kv head of its probability
  * (decay 0 does not read them).
+ * out may be q, element for element, in calls without weights; with weights, whose queries are read once more after out is
+ * written, it must not overlap q (SPQT_EINVAL where both begin at one address), and in any other way it never may.
  * workspace: workspace_bytes >= spqt_kv_workspace_bytes, 256-byte aligned, prepared once with spqt_workspace_init;
  * every call leaves what the next one relies on, so attention calls on one stream may share one, whatever their shapes.  Not
  * with GEMVs: these rely on all zeros, and an attention leaves its partial sums.  It raises the flag that makes them yield NaN

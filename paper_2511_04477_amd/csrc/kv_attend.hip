@@ -28,7 +28,7 @@ extern "C" int spqt_kv_attention(const spqt_kv_cache *cache, const spqt_kv_rows 
     size_t need = 0;
     rc = spqt_kv_workspace_bytes(cache->sequences, rows, q_heads, cache->kv_heads, cache->head_dim, cache->max_blocks, &need);
     if (rc != SPQT_OK) return rc;
-    if (!workspace || window < 0 || scale != scale || decay != decay || (cache->weights && !lse)) return SPQT_EINVAL;
+    if (!workspace || window < 0 || scale != scale || decay != decay || (cache->weights && (!lse || q->data == out->data))) return SPQT_EINVAL;
     if ((uintptr_t)lse % 4 != 0 || (uintptr_t)counts % 4 != 0 || (uintptr_t)workspace % 256 != 0) return SPQT_EALIGN;
     if (workspace_bytes < need) return SPQT_ESIZE;
     const Call a = {view(*q), view(*out), lse, counts, rows, q_heads, q_heads / cache->kv_heads, window, scale, decay};

@@ -155,7 +155,7 @@ def spqt_kv_attention(codes, scales, table, lengths, q, out, workspace, scale=No
     """Attention of q [sequences, rows, q_heads, head_dim] over the cache into out (same shape and type): row i is the token at position
     lengths[s] - counts[s] + i and sees those up to itself, the last `window` of them if window > 0.  scale None: 1 / sqrt(head_dim).
     lse: float32 [sequences, rows, q_heads] or None.  weights (with lse): weights = decay * weights + the probabilities that every
-    cached token got in this call."""
+    cached token got in this call.  out may be q itself in calls without weights."""
     if _b._fast is not None:
         rc = _b._fast.kv_attention((_b._lib or lib()).at["spqt_kv_attention"], codes, scales, table, lengths, q, out, workspace, scale, counts, window, lse, weights, decay, stream)
         if rc is not None:

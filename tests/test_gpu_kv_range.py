@@ -230,3 +230,20 @@ def test_windows_up_to_31_bits_see_everything(gpu):  # noqa: F811
     for window in (1 << 24, (1 << 31) - 1):
         got = attend(gpu, c, q, None, window)
         assert got[0].equal(want[0]) and got[1].equal(want[1])
+
+
+@pytest.mark.parametrize("case", [CASES[i] for i in (2, 7, 8, 12, 14)] + MANY[:2], ids=lambda c: "-".join(str(x) for x in c).replace(" ", ""))
+def test_outputs_over_the_queries(gpu, case):  # noqa: F811
+    """Without weights the same as elsewhere; with weights, whose queries are read after the outputs are written, refused."""
+    _, spqt = gpu
+    c, q = case_cache(gpu, case, 38)
+    counts = None if case[5] is None else torch.tensor(case[5], dtype=torch.int32, device="cuda")
+    want, want_lse = attend(gpu, c, q, case[5], case[7])
+    ws = spqt.new_kv_workspace(len(case[4]), case[6], case[0], case[1], case[2], c.max_blocks)
+    lse, weights = torch.zeros_like(want_lse), c.weights.clone()
+    before = q.clone()
+    with pytest.raises(spqt.SpqtError):
+        spqt.spqt_kv_attention(c.codes, c.scales, c.table, c.lengths, q, q, ws, counts=counts, window=case[7], lse=lse, weights=c.weights)
+    assert q.equal(before) and c.weights.equal(weights)
+    spqt.spqt_kv_attention(c.codes, c.scales, c.table, c.lengths, q, q, ws, counts=counts, window=case[7], lse=lse)
+    assert q.equal(want) and lse.equal(want_lse)

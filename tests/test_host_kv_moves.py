@@ -7,7 +7,7 @@ import torch
 
 import paper_2511_04477_amd as spqt
 from oracle import kv
-from test_host_kv import ESHAPE, EINVAL, cache
+from test_host_kv import EINVAL, ESHAPE, ESIZE, attention, cache, rows
 
 
 def block(seed, dtype=torch.float16, tokens=64, dim=128, size=1.0):
@@ -64,3 +64,10 @@ def test_refusals_are_those_of_the_other_eviction():
                          ((64, 1, None, 2, 1 << 21, 1 << 20), EINVAL)):
         assert evict(ctypes.byref(whole), *args, None) == status
     assert evict(ctypes.byref(cache()), 64, 1, 1 << 21, 2, 1 << 21, 1 << 20, None) == EINVAL
+
+
+def test_outputs_over_the_queries_that_the_weights_need():
+    weighed = dict(lse=1 << 22, size=16)                     # (a workspace that is too small: nothing is launched)
+    assert attention(cache(weights=1 << 20), rows(), rows(), **weighed) == EINVAL
+    assert attention(cache(weights=1 << 20), rows(), rows(data=1 << 21), **weighed) == ESIZE
+    assert attention(cache(), rows(), rows(), **weighed) == ESIZE
