@@ -381,13 +381,16 @@ int rows_of(int dim) { return dim > 128 ? Shape<256>::kRows : Shape<128>::kRows;
 namespace spqt {
 namespace kv {
 
-// Up to 64 rows of a kv head are a few.  Up to 512 are, in sixteens, where that makes few blocks to go through (with the room of the tables), at most as many as 20000 of 128
-// elements.  As a few / here, heads of 128: 80, 256 and 512 rows of each of 8 over 4000 tokens (2500, 8000, 16000 blocks) 16.4 / 38.4, 23.3 / 33.1, 31.3 / 36.6 us; 80, 128 and 256
-// over 32000 (20000, 32000, 64000) 41 / 63, 53 / 55, 95 / 53.  Heads of 192: 12500 blocks 37 / 46, 20000 61 / 43; of 256: 4000 33 / 42, 8000 47 / 47, 16000 61 / 49; of 64: 32000 35 / 46, 48000 58 / 47.
-// Sixteens of a few blocks have to have a workgroup each (their start and end count): 512 sixteens of 3 blocks 17.9 / 14.5, 800 of 5 22.5 / 21.1, 256 of 3 7.9 / 15.9; 320 of 16 25.2 / 36.0.
+// Up to 64 rows of a kv head are a few.  Up to 512 are, in sixteens, where that makes few blocks to go through (with the room of the tables), at most as many as 24000 of 128
+// elements; as 65536 where the rows fill no more than 5/8 of what the workgroups here would take.  As a few / here, heads of 128: 80, 256 and 512 rows of each of 8 over 4000 tokens
+// (2500, 8000, 16000 blocks) 16.5 / 41.5, 23.5 / 38.1, 31.0 / 41.6 us; 256 over 16000 and 32000 (32000, 64000) 53 / 45, 95 / 65; not full: 128 rows over 32000, 64000 and 131000 (32000,
+// 64000, 131000) 53 / 63, 100 / 109, 235 / 204, 80 over 131000 (82000) 166 / 223, 160 over 64000 (80000) 125 / 112.  Heads of 192, full: 16000 44 / 47, 32000 69 / 63, not: 40000 89 / 118; of 256, full: 16000 51 / 54, 32000 98 / 83,
+// not: 20000 86 / 82; of 64, full: 128000 115 / 86, not: 80000 73 / 100.
+// Sixteens of a few blocks have to have a workgroup each (their start and end count): 640 sixteens of 3 blocks 18.6 / 16.1, 4096 of 5 40.6 / 28.4, 2560 of 5 33.4 / 26.8 (but 1024 of 3 15.2 / 20.0).
 bool is_prompt(int sequences, int rows, int group, int kv_heads, int dim, int max_blocks) {
-    const int64_t all = (int64_t)rows * group, units = (int64_t)sequences * kv_heads * ((all + 15) / 16);
-    return all > 512 || (all > kFewRows && ((units > 256 && max_blocks < 8) || units * max_blocks > 20000 * 128 / dim));
+    const int64_t all = (int64_t)rows * group, sixteens = (all + 15) / 16, tiles = (all + rows_of(dim) - 1) / rows_of(dim), units = (int64_t)sequences * kv_heads * sixteens;
+    const int limit = 8 * 16 * sixteens <= 5 * tiles * rows_of(dim) ? 65536 : 24000;
+    return all > 512 || (all > kFewRows && ((units > 256 && max_blocks < 8) || units * max_blocks > limit * 128 / dim));
 }
 
 size_t prompt_bytes(int dim) { return (size_t)kParted * rows_of(dim) * (dim + 2) * 4; }
