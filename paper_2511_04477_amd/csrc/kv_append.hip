@@ -12,7 +12,8 @@ using namespace spqt::kv;
 // 79.0 for 76.6 us below, since a line of DRAM has several heads of a token.  The first workgroup does the sequence's first and last block, one after the other, since the first
 // reads from the tail what the last one overwrites there.
 // What bounds it: 2 bytes in and 1 out a value, and that a workgroup's loads, largest magnitude and stores follow each other: 25.7k tokens of 8 heads of 128 (6 sequences, 158 MB)
-// 47 us = 3.4 TB/s (a copy: 4.83).  One token of 4 sequences 5.2 us: the chain lengths, table, row, magnitude, codes.
+// 47 us = 3.4 TB/s (a copy: 4.83).  With 79 registers a CU holds six workgroups; eight would take 16 of them to scratch memory.  One token of 4 sequences 5.2 us: the chain lengths, table, row,
+// magnitude, codes.
 template <int D, bool BF16>
 __global__ __launch_bounds__(kTileThreads) void spqt_kv_append_kernel(Cache c, Rows keys, Rows values, int rows, const int32_t *counts) {
     __shared__ Tile<D> tile;

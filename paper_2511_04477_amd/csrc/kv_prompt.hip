@@ -8,9 +8,10 @@
 // would save a third of the products' instructions (4001 rows of 32 / 8 heads of 128 166 us for 208, 1024 rows over 32768 tokens 1042 for 1397), and every output would be off by up to 2^-11
 // of sum p |v|: against 64 bits 2.5e-4 of an fp16 output instead of the 2.1e-4 of its own rounding.
 //
-// What bounds it: matrix and vector instructions of a SIMD side by side; a block takes a SIMD's two wavefronts 96 matrix instructions of 32 cycles and about 620 others, more than
-// half of them for the softmax.  1024 rows of 64 / 8 heads of 128 over 32768 tokens 1397 us = 0.77 PFLOP/s (1.16 of what the instructions multiply; an 8192^3 product: 1.2); 4001 rows of
-// 32 / 8 heads from an empty cache 208 us, since 504 workgroups of uneven length on 256 CUs leave some idle at the end.
+// What bounds it: matrix and vector instructions of a SIMD side by side; a block takes a SIMD's two wavefronts 96 matrix instructions of 32 cycles and about 810 others, most of them for
+// the softmax and its two numbers (the matrix units are busy for 0.56 of the time, the vector units for 0.72).  1024 rows of 64 / 8 heads of 128 over 32768 tokens 1397 to 1520 us, by the
+// card, = 0.72 to 0.77 PFLOP/s (1.08 to 1.16 of what the instructions multiply; an 8192^3 product: 1.2); 4001 rows of 32 / 8 heads from an empty cache 208 to 220 us, since 504 workgroups of
+// uneven length on 256 CUs leave some idle at the end.
 #include "kv_attend.hpp"
 #include "kv_units.hpp"
 

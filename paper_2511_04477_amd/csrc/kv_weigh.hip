@@ -68,7 +68,7 @@ __global__ __launch_bounds__(kThreads) void spqt_kv_weigh_few_kernel(Cache c, Ca
 
 // Many rows: a workgroup per block, whose wavefronts hold its keys as 16-bit numbers of the queries' type (a code is exact in either) and take every eighth (fourth)
 // 32 of the rows that see it.  With S^T = K Q^T a lane has one row and half of each 32 tokens; its tokens' sums meet at the end.
-// What bounds it: 32 exponentials and as many multiply-adds and additions a lane for 16 matrix instructions: 4001 rows of 32 / 8 heads from an empty cache 139 us, 1024 rows of 64 / 8
+// What bounds it: 32 exponentials and as many multiply-adds and additions a lane for 16 matrix instructions: 4001 rows of 32 / 8 heads from an empty cache 116 us (vector units busy for 0.60 of the time, matrix units for 0.30), 1024 rows of 64 / 8
 // heads over 8192 tokens 196 us.
 constexpr int many_threads(int dim) { return dim > 128 ? 256 : 512; }
 
