@@ -84,8 +84,8 @@ int spqt_kv_read(const spqt_kv_cache *cache, const spqt_kv_rows *k_out, const sp
 /* Bytes of the workspace that spqt_kv_attention needs for up to this many rows, at any lengths. */
 int spqt_kv_workspace_bytes(int sequences, int rows, int q_heads, int kv_heads, int head_dim, int max_blocks, size_t *out_bytes);
 
-/* Attention of the call's rows over the cache.  Query head j reads kv head j / (q_heads / kv_heads).  Row i at position p sees
- * the tokens t <= p of its sequence, and with window > 0 only those with t > p - window.
+/* Attention of the call's rows over the cache.  Query head j reads kv head j / (q_heads / kv_heads), a quotient of at most
+ * 2^20.  Row i at position p sees the tokens t <= p of its sequence, and with window > 0 only those with t > p - window.
  *   out  = sum over t of softmax(scale * q . k_t) v_t            16 bit (at most the type's largest number), strided as q
  *   lse  = ln sum over t of exp(scale * q . k_t)                 fp32 [sequences][rows][q_heads], optional
  * Sums and statistics are fp32; for the products with the values a probability has 22 bits, but no finer than about 2^-40 of the row's

@@ -11,7 +11,7 @@ extern "C" int spqt_kv_workspace_bytes(int sequences, int rows, int q_heads, int
         head_dim < 64 || head_dim > SPQT_KV_MAX_DIM || head_dim % 64 != 0 || max_blocks < 1 || max_blocks > 1 << 24)
         return SPQT_ESHAPE;
     const int group = q_heads / kv_heads;
-    if ((int64_t)rows * group > 1 << 28) return SPQT_ESHAPE;
+    if ((int64_t)rows * group > 1 << 28 || group > kMaxGroup) return SPQT_ESHAPE;
     // either kind of call's partial sums, whatever the room of the tables, so that a workspace for more sequences, rows or blocks serves less of them
     size_t bytes = step_bytes(head_dim);
     if ((int64_t)rows * group > kFewRows && prompt_bytes(head_dim) > bytes) bytes = prompt_bytes(head_dim);

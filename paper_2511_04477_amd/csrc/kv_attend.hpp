@@ -13,6 +13,9 @@ constexpr float kNone = -__builtin_inff();
 constexpr int kRoom = 32;
 // Probabilities go to the matrix instructions as two fp16 numbers, 22 bits in all, the largest of them about 2^15 (kv_units.hpp): fp16's smallest number is 2^-39 of that.
 
+// Query heads of a kv head: places of rows are worked out by the fp32 inverse of it (kv_weigh.hip), exactly up to some 2^21.
+constexpr int kMaxGroup = 1 << 20;
+
 struct Call {
     Rows q, out;
     float *lse;

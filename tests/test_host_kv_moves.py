@@ -71,3 +71,21 @@ def test_outputs_over_the_queries_that_the_weights_need():
     assert attention(cache(weights=1 << 20), rows(), rows(), **weighed) == EINVAL
     assert attention(cache(weights=1 << 20), rows(), rows(data=1 << 21), **weighed) == ESIZE
     assert attention(cache(), rows(), rows(), **weighed) == ESIZE
+
+
+def test_so_many_query_heads_of_a_kv_head_are_refused():
+    size = spqt.lib().spqt_kv_workspace_bytes
+    out = ctypes.c_size_t()
+    assert size(1, 1, 1 << 20, 1, 64, 1, ctypes.byref(out)) == 0 and size(1, 1, 4 << 20, 4, 64, 1, ctypes.byref(out)) == 0
+    assert size(1, 1, (1 << 20) + 1, 1, 64, 1, ctypes.byref(out)) == ESHAPE
+    assert attention(cache(kv_heads=1, weights=1 << 20), rows(), rows(data=1 << 21), lse=1 << 22, heads=1 << 23, size=16) == ESHAPE
+
+
+def test_places_by_the_inverse():
+    """The rule of kv_weigh.hip in fp32, at and beside every whole position: 32 rows from any of a kv head's query heads on."""
+    f = lambda x: torch.tensor(x, dtype=torch.float32)  # noqa: E731
+    for group in (1, 2, 3, 5, 7, 8, 40, 641, 4095, 65537, (1 << 20) - 1, 1 << 20):
+        inverse = f(1.0) / f(float(group))
+        n = torch.cat([torch.arange(min(group + 32, 4096)), torch.arange(max(0, group - 64), group + 32), torch.arange(32) + group - 1])
+        n = n[n < group + 31]
+        assert torch.equal(((n.float() + f(0.5)) * inverse).long(), n // group)
