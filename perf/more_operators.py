@@ -150,8 +150,8 @@ EPS = 1e-5
 def _held(x, dtype):
     """(what rows of numbers stand for once they are codes, the rows' scales)."""
     top = x.abs().amax(dim=1, keepdim=True).clamp(min=2.0 ** -100)
-    scale, largest = top / 127.0, torch.finfo(dtype).max
-    values = torch.round(x * (127.0 / top)) * scale
+    scale, inverse, largest = top / 127.0, torch.full_like(top, 127.0) / top, torch.finfo(dtype).max
+    values = torch.round(x * inverse) * scale
     return values.clamp(-largest, largest).to(dtype), scale[:, 0]
 
 
