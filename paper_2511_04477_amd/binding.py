@@ -41,6 +41,7 @@ CB_EXPORTS = ["spqt_cb_packed_bytes", "spqt_cb_quantize", "spqt_cb_dequantize", 
               "spqt_cb8_packed_bytes", "spqt_cb8_quantize", "spqt_cb8_dequantize", "spqt_cb8_gemv", "spqt_cb8_gemv_fused", "spqt_cb8_gemv_rows",
               "spqt_cb2_packed_bytes", "spqt_cb2_quantize", "spqt_cb2_dequantize", "spqt_cb2_gemv", "spqt_cb2_gemv_fused", "spqt_cb2_gemv_rows"]
 KV_EXPORTS = ["spqt_kv_append", "spqt_kv_read", "spqt_kv_workspace_bytes", "spqt_kv_attention", "spqt_kv_evict", "spqt_kv_evict_exact"]
+I8_EXPORTS = ["spqt_i8_quantize", "spqt_i8_read", "spqt_i8_norm", "spqt_i8_gemm", "spqt_i8_workspace_bytes"]
 CB_CHUNK_BYTES = 18432
 CB8_CHUNK_BYTES = 17408
 CB2_CHUNK_BYTES = 20480
@@ -110,11 +111,16 @@ def lib() -> ctypes.CDLL:
         L.spqt_kv_attention.argtypes = [vp, vp, vp, vp, i32, vp, i32, c.c_float, i32, c.c_float, vp, sz, vp]
         L.spqt_kv_evict.argtypes = [vp, i32, i32, vp, i32, vp, vp, vp]
         L.spqt_kv_evict_exact.argtypes = L.spqt_kv_evict.argtypes
-        for name in EXPORTS[1:] + CB_EXPORTS + KV_EXPORTS:
+        L.spqt_i8_quantize.argtypes = [vp, i64, i64, i64, i32, vp, i64, vp, vp]
+        L.spqt_i8_read.argtypes = [vp, i64, vp, i64, i64, i32, vp, i64, vp]
+        L.spqt_i8_norm.argtypes = [vp, vp]
+        L.spqt_i8_workspace_bytes.argtypes = [i64, i64, i64, c.POINTER(sz)]
+        L.spqt_i8_gemm.argtypes = [vp, vp, sz, vp]
+        for name in EXPORTS[1:] + CB_EXPORTS + KV_EXPORTS + I8_EXPORTS:
             getattr(L, name).restype = i32
         # the device functions' addresses, for _fastcall
-        L.at = {name: c.cast(getattr(L, name), vp).value for name in EXPORTS + CB_EXPORTS + KV_EXPORTS
-                if "gemv" in name or "gather" in name or "kv" in name}
+        L.at = {name: c.cast(getattr(L, name), vp).value for name in EXPORTS + CB_EXPORTS + KV_EXPORTS + I8_EXPORTS
+                if "gemv" in name or "gather" in name or "kv" in name or "i8" in name}
         _lib = L
     return _lib
 

@@ -21,6 +21,9 @@ SOURCES = ["pack.cpp", "quant_cb.cpp", "gather.hip", "gemv.hip", "gemv_cb.hip", 
            "gemv_bal.hip"]
 # The key/value cache: one set of objects for all variants of the library, since it has neither their reducers nor their stamps.
 KV_SOURCES = ["kv_append.hip", "kv_attend.hip", "kv_step.hip", "kv_prompt.hip", "kv_weigh.hip", "kv_evict.hip"]
+# The prompt side in 8-bit integers, for which the same holds.
+I8_SOURCES = ["i8_rows.hip", "i8_gemm.hip", "i8_few.hip"]
+SHARED_SOURCES = KV_SOURCES + I8_SOURCES
 CALIB_LIB = os.path.join(PKG, "libspqt_calib.so")       # benchmark-only helper kernels
 CALIB_SOURCES = ["calib.hip", "baseline_rowmajor.hip"]
 # The same kernels with wall-clock stamps per wavefront (python -m paper_2511_04477_amd.timeline).
@@ -96,9 +99,9 @@ def build(verbose: bool = False) -> str:
             _jobs(TIMELINE_LIB, SOURCES, defines=("SPQT_TIMELINE=1",), tag="tl_"),
             _jobs(GIVEUP_LIB, GIVEUP_SOURCES, defines=("SPQT_TEST_GIVE_UP=1",), tag="gu_"),
             _jobs(HANDOVER_LIB, SOURCES, defines=("SPQT_TEST_HAND_OVER=1",), tag="ho_"),
-            _jobs(LIB, SOURCES + KV_SOURCES)]
-    kv = [os.path.join(OBJ, os.path.splitext(s)[0] + ".o") for s in KV_SOURCES]
-    plan = [(cs, (lib, objs + kv if lib in (TIMELINE_LIB, HANDOVER_LIB) else objs)) for cs, (lib, objs) in plan]
+            _jobs(LIB, SOURCES + SHARED_SOURCES)]
+    shared = [os.path.join(OBJ, os.path.splitext(s)[0] + ".o") for s in SHARED_SOURCES]
+    plan = [(cs, (lib, objs + shared if lib in (TIMELINE_LIB, HANDOVER_LIB) else objs)) for cs, (lib, objs) in plan]
     # every object of every library in one pool (longest first), then the links
     compiles = sorted((c for cs, _ in plan for c in cs), key=lambda c: -os.path.getsize(c[-1]))
     fastcall = FASTCALL_LIB + f".tmp{os.getpid()}"

@@ -1,0 +1,48 @@
+// What the kernels of the product in 8-bit integers share: the call, and what becomes of a sum.
+#ifndef SPQT_I8_GEMM_HPP
+#define SPQT_I8_GEMM_HPP
+
+#include "i8_common.hpp"
+
+namespace spqt {
+namespace i8 {
+
+struct Product {
+    const int8_t *codes, *weights;
+    const float *scales, *weight_scales, *bias;
+    void *y;
+    int64_t codes_row, weights_row, y_row;
+    int rows, N, K;
+    int outputs;             // of a row: N, gated N / 2
+    int y_type;
+};
+
+// A sum of channel n and a row with this scale.
+__device__ __forceinline__ float scaled(const Product &p, int sum, float scale, int n) {
+    float v = (float)sum * scale * p.weight_scales[n];
+    if (p.bias) v += p.bias[n];
+    return v;
+}
+__device__ __forceinline__ float gated_by(float gate, float up) { return gate / (1.0f + __expf(-gate)) * up; }
+
+__device__ __forceinline__ void store_one(const Product &p, int64_t row, int n, float v) {
+    const int64_t at = row * p.y_row + n;
+    if (p.y_type == SPQT_I8_FP32) reinterpret_cast<float *>(p.y)[at] = v;
+    else reinterpret_cast<uint16_t *>(p.y)[at] = (uint16_t)(p.y_type == SPQT_I8_BF16 ? narrow2<true>(v, v) : narrow2<false>(v, v));
+}
+
+// Zeros in place of what is behind a row's K-th byte, in the 16 bytes from k on.
+__device__ __forceinline__ i32x4 masked(i32x4 x, int k, int K) {
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        const int left = K - k - 4 * i;
+        x[i] = left >= 4 ? x[i] : left <= 0 ? 0 : x[i] & (int)(0xFFFFFFFFu >> (32 - 8 * left));
+    }
+    return x;
+}
+
+void launch_few(const Product &p, bool gated, hipStream_t stream);
+
+}  // namespace i8
+}  // namespace spqt
+#endif

@@ -1,0 +1,322 @@
+// Rows of numbers to 8-bit codes and back, and the norms before and after a block (spqt_i8.h has the definitions).
+#include "i8_common.hpp"
+
+namespace {
+
+using namespace spqt;
+using namespace spqt::i8;
+
+// T threads hold a row of up to 8 T V numbers, thread t the eights t, t + T, ...; rows of one wavefront share a workgroup of four.
+template <int T>
+struct Shape {
+    static constexpr int kThreads = T == 64 ? 256 : T, kRows = kThreads / T, kWaves = T / 64;
+};
+
+template <int T>
+__device__ __forceinline__ int place(int v) {
+    return ((int)(threadIdx.x % T) + v * T) * 8;
+}
+
+// Eight 16-bit numbers from element k on, as they lie; 0 from element K on.
+__device__ __forceinline__ u32x4 fetch(const uint16_t *row, int k, int K) {
+    if (k + 8 <= K) return *reinterpret_cast<const u32x4_at2 *>(row + k);
+    u32x4 w = {0u, 0u, 0u, 0u};
+#pragma unroll
+    for (int e = 0; e < 7; ++e)
+        if (k + e < K) w[e / 2] |= (uint32_t)row[k + e] << (16 * (e % 2));
+    return w;
+}
+template <bool BF16>
+__device__ __forceinline__ void widen8(u32x4 w, float (&x)[8]) {
+#pragma unroll
+    for (int e = 0; e < 8; ++e) x[e] = widen<BF16>(w[e / 2] >> (16 * (e % 2)) & 0xFFFFu);
+}
+template <bool BF16>
+__device__ __forceinline__ void put(uint16_t *row, int k, int K, const float (&x)[8]) {
+    const u32x4 w = {narrow2<BF16>(x[0], x[1]), narrow2<BF16>(x[2], x[3]), narrow2<BF16>(x[4], x[5]), narrow2<BF16>(x[6], x[7])};
+    if (k + 8 <= K) {
+        *reinterpret_cast<u32x4_at2 *>(row + k) = w;
+        return;
+    }
+#pragma unroll
+    for (int e = 0; e < 7; ++e)
+        if (k + e < K) row[k + e] = (uint16_t)(w[e / 2] >> (16 * (e % 2)));
+}
+
+// A value of every thread of a row together: over the lanes of a wavefront first, then the wavefronts' through shared memory, `slot` being another one than the last time.
+template <int T, class F>
+__device__ __forceinline__ uint32_t over_row(uint32_t v, F f, uint32_t *shared, int slot) {
+#pragma unroll
+    for (int step = 1; step < 64; step *= 2) v = f(v, (uint32_t)__shfl_xor((int)v, step));
+    if (T == 64) return v;
+    constexpr int kWaves = T / 64;
+    if (threadIdx.x % 64 == 0) shared[slot * kWaves + threadIdx.x / 64] = v;
+    __syncthreads();
+    uint32_t all = shared[slot * kWaves];
+#pragma unroll
+    for (int w = 1; w < kWaves; ++w) all = f(all, shared[slot * kWaves + w]);
+    return all;
+}
+template <int T>
+__device__ __forceinline__ float sum_over_row(float v, uint32_t *shared, int slot) {
+    return as_float(over_row<T>(as_u32(v), [](uint32_t a, uint32_t b) { return as_u32(as_float(a) + as_float(b)); }, shared, slot));
+}
+template <int T>
+__device__ __forceinline__ uint32_t most_over_row(uint32_t v, uint32_t *shared, int slot) {
+    return over_row<T>(v, [](uint32_t a, uint32_t b) { return a > b ? a : b; }, shared, slot);
+}
+
+// 1 / sqrt(mean x^2 + eps).  Squares of numbers from 2^64 on leave fp32: such a row is summed in units of 2^70, in which eps is nothing.
+template <int T, int V>
+__device__ __forceinline__ float inverse_rms(const float (&x)[V][8], int K, float eps, uint32_t *shared, int slot) {
+    float sum = 0.0f;
+#pragma unroll
+    for (int v = 0; v < V; ++v)
+#pragma unroll
+        for (int e = 0; e < 8; ++e) sum = __builtin_fmaf(x[v][e], x[v][e], sum);
+    sum = sum_over_row<T>(sum, shared, slot);
+    if (sum < __builtin_inff() || sum != sum) return 1.0f / __builtin_sqrtf(sum / (float)K + eps);
+    sum = 0.0f;
+#pragma unroll
+    for (int v = 0; v < V; ++v)
+#pragma unroll
+        for (int e = 0; e < 8; ++e) {
+            const float y = x[v][e] * 0x1p-70f;
+            sum = __builtin_fmaf(y, y, sum);
+        }
+    sum = sum_over_row<T>(sum, shared, slot + 1);
+    return 0x1p-70f / __builtin_sqrtf(sum / (float)K);
+}
+
+// Codes of a row, with the largest magnitude of this thread's numbers: magnitudes order as their bits do, infinities and NaN above all numbers.
+template <int T, int V>
+__device__ __forceinline__ void quantize_row(const float (&x)[V][8], int K, int8_t *codes, float *scale, uint32_t *shared, int slot) {
+#pragma clang fp contract(off)
+    uint32_t most = 0u;
+#pragma unroll
+    for (int v = 0; v < V; ++v)
+#pragma unroll
+        for (int e = 0; e < 8; ++e) {
+            const uint32_t m = as_u32(x[v][e]) & 0x7FFFFFFFu;
+            most = m > most ? m : most;
+        }
+    most = most_over_row<T>(most, shared, slot);
+    const bool number = most < 0x7F800000u;
+    const float top = __builtin_fmaxf(as_float(most), 0x1p-100f), inverse = 127.0f / top;
+    if (threadIdx.x % T == 0) *scale = number ? top / 127.0f : __builtin_nanf("");
+#pragma unroll
+    for (int v = 0; v < V; ++v) {
+        const int k = place<T>(v);
+        if (k >= K) continue;
+        u32x2 w;
+#pragma unroll
+        for (int i = 0; i < 2; ++i) {
+            // the product rounded, then 1.5 2^23 added, which rounds it to the nearest integer: the code is in the lowest byte
+            uint32_t c[4];
+#pragma unroll
+            for (int j = 0; j < 4; ++j) c[j] = as_u32(x[v][4 * i + j] * inverse + 12582912.0f);
+            w[i] = __builtin_amdgcn_perm(c[1], c[0], 0x0C0C0400u) | __builtin_amdgcn_perm(c[3], c[2], 0x04000C0Cu);
+            if (!number) w[i] = 0u;
+        }
+        if (k + 8 <= K) {
+            *reinterpret_cast<u32x2 *>(codes + k) = w;
+        } else {
+#pragma unroll
+            for (int e = 0; e < 7; ++e)
+                if (k + e < K) codes[k + e] = (int8_t)(w[e / 4] >> (8 * (e % 4)));
+        }
+    }
+}
+
+struct Quantize {
+    const uint16_t *x;
+    int8_t *codes;
+    float *scales;
+    int64_t x_row, codes_row;
+    int rows, K;
+};
+
+template <int T, int V, bool BF16>
+__global__ __launch_bounds__(Shape<T>::kThreads) void spqt_i8_quantize_kernel(Quantize a) {
+    typedef Shape<T> S;
+    __shared__ uint32_t shared[2 * S::kWaves];
+    int slot = 0;
+    for (int64_t row = (int64_t)blockIdx.x * S::kRows + (S::kRows > 1 ? threadIdx.x / T : 0); row < a.rows; row += (int64_t)gridDim.x * S::kRows) {
+        float x[V][8];
+#pragma unroll
+        for (int v = 0; v < V; ++v) widen8<BF16>(fetch(a.x + row * a.x_row, place<T>(v), a.K), x[v]);
+        quantize_row<T, V>(x, a.K, a.codes + row * a.codes_row, a.scales + row, shared, slot);
+        slot ^= 1;
+    }
+}
+
+struct Norm {
+    const uint16_t *h, *block, *block_gain, *gate, *gain;
+    uint16_t *h_out, *out;
+    int8_t *codes;
+    float *scales;
+    int64_t h_row, block_row, gate_row, h_out_row, out_row, codes_row;
+    int rows, K;
+    float residual, eps, offset;
+};
+
+template <int T, int V, bool BF16>
+__global__ __launch_bounds__(Shape<T>::kThreads) void spqt_i8_norm_kernel(Norm a) {
+    typedef Shape<T> S;
+    __shared__ uint32_t shared[5 * S::kWaves];
+    for (int64_t row = (int64_t)blockIdx.x * S::kRows + (S::kRows > 1 ? threadIdx.x / T : 0); row < a.rows; row += (int64_t)gridDim.x * S::kRows) {
+        float s[V][8], other[8];
+        if (a.block) {
+#pragma unroll
+            for (int v = 0; v < V; ++v) widen8<BF16>(fetch(a.block + row * a.block_row, place<T>(v), a.K), s[v]);
+            if (a.block_gain) {
+                const float by = inverse_rms<T, V>(s, a.K, a.eps, shared, 0);
+#pragma unroll
+                for (int v = 0; v < V; ++v) {
+                    widen8<BF16>(fetch(a.block_gain, place<T>(v), a.K), other);
+#pragma unroll
+                    for (int e = 0; e < 8; ++e) s[v][e] = s[v][e] * by * (a.offset + other[e]);
+                }
+            }
+            if (a.gate)
+#pragma unroll
+                for (int v = 0; v < V; ++v) {
+                    widen8<BF16>(fetch(a.gate + row * a.gate_row, place<T>(v), a.K), other);
+#pragma unroll
+                    for (int e = 0; e < 8; ++e) s[v][e] *= other[e];
+                }
+#pragma unroll
+            for (int v = 0; v < V; ++v) {
+                const int k = place<T>(v);
+                widen8<BF16>(fetch(a.h + row * a.h_row, k, a.K), other);
+#pragma unroll
+                for (int e = 0; e < 8; ++e) s[v][e] = k + e < a.K ? __builtin_fmaf(a.residual, other[e], s[v][e]) : 0.0f;
+                if (k < a.K) put<BF16>(a.h_out + row * a.h_out_row, k, a.K, s[v]);
+            }
+        } else {
+#pragma unroll
+            for (int v = 0; v < V; ++v) widen8<BF16>(fetch(a.h + row * a.h_row, place<T>(v), a.K), s[v]);
+        }
+        const float by = inverse_rms<T, V>(s, a.K, a.eps, shared, 2);
+#pragma unroll
+        for (int v = 0; v < V; ++v) {
+            const int k = place<T>(v);
+            widen8<BF16>(fetch(a.gain, k, a.K), other);
+#pragma unroll
+            for (int e = 0; e < 8; ++e) s[v][e] = k + e < a.K ? s[v][e] * by * (a.offset + other[e]) : 0.0f;
+            if (a.out && k < a.K) put<BF16>(a.out + row * a.out_row, k, a.K, s[v]);
+        }
+        if (a.codes) quantize_row<T, V>(s, a.K, a.codes + row * a.codes_row, a.scales + row, shared, 4);
+        if (T > 64) __syncthreads();               // the slots are free again
+    }
+}
+
+// What codes stand for: eight a thread.
+struct Read {
+    const int8_t *codes;
+    const float *scales;
+    uint16_t *out;
+    int64_t codes_row, out_row;
+    int rows, K, per_row;                          // workgroups a row
+};
+template <bool BF16>
+__global__ __launch_bounds__(256) void spqt_i8_read_kernel(Read a) {
+    const float largest = BF16 ? as_float(0x7F7F0000u) : 65504.0f;
+    for (int64_t unit = blockIdx.x; unit < (int64_t)a.rows * a.per_row; unit += gridDim.x) {
+        const int64_t row = unit / a.per_row;
+        const int k = ((int)(unit - row * a.per_row) * 256 + (int)threadIdx.x) * 8;
+        if (k >= a.K) continue;
+        const float scale = a.scales[row];
+        const u32x2 w = *reinterpret_cast<const u32x2 *>(a.codes + row * a.codes_row + k);
+        float x[8];
+#pragma unroll
+        for (int e = 0; e < 8; ++e) {
+            const float v = (float)((int)(w[e / 4] << (24 - 8 * (e % 4))) >> 24) * scale;
+            x[e] = v != v ? v : __builtin_fmaxf(-largest, __builtin_fminf(v, largest));
+        }
+        put<BF16>(a.out + row * a.out_row, k, a.K, x);
+    }
+}
+
+// f(threads, eights a thread, BF16) for rows of K numbers.
+template <class F>
+void dispatch(int64_t K, int type, F f) {
+    auto typed = [&](auto t, auto v) {
+        if (type == SPQT_I8_BF16) f(t, v, std::true_type());
+        else f(t, v, std::false_type());
+    };
+    if (K <= 512) typed(std::integral_constant<int, 64>(), std::integral_constant<int, 1>());
+    else if (K <= 2048) typed(std::integral_constant<int, 256>(), std::integral_constant<int, 1>());
+    else if (K <= 4096) typed(std::integral_constant<int, 256>(), std::integral_constant<int, 2>());
+    else if (K <= 8192) typed(std::integral_constant<int, 256>(), std::integral_constant<int, 4>());
+    else if (K <= 16384) typed(std::integral_constant<int, 512>(), std::integral_constant<int, 4>());
+    else if (K <= 32768) typed(std::integral_constant<int, 1024>(), std::integral_constant<int, 4>());
+    else typed(std::integral_constant<int, 1024>(), std::integral_constant<int, 8>());
+}
+template <class S>
+dim3 grid_of(int64_t rows) {
+    const int64_t n = (rows + S::kRows - 1) / S::kRows;
+    return dim3((unsigned)(n < 1 << 20 ? n : 1 << 20));
+}
+
+}  // namespace
+
+extern "C" int spqt_i8_quantize(const void *x, int64_t x_row, int64_t rows, int64_t K, int type, int8_t *codes, int64_t codes_row, float *scales, void *stream) {
+    if (!sixteen_bits(type)) return SPQT_EINVAL;
+    int rc = check_extents(rows, K, SPQT_I8_MAX_NORM);
+    if (rc == SPQT_OK) rc = check_matrix(x, x_row, rows, K, 2, false);
+    if (rc == SPQT_OK) rc = check_codes(codes, codes_row, rows, K, true);
+    if (rc == SPQT_OK) rc = check_scales(scales);
+    if (rc != SPQT_OK) return rc;
+    const Quantize a = {(const uint16_t *)x, codes, scales, x_row, codes_row, (int)rows, (int)K};
+    dispatch(K, type, [&](auto t, auto v, auto bf16) {
+        typedef Shape<decltype(t)::value> S;
+        hipLaunchKernelGGL((spqt_i8_quantize_kernel<decltype(t)::value, decltype(v)::value, decltype(bf16)::value>), grid_of<S>(rows), dim3(S::kThreads), 0,
+                           (hipStream_t)stream, a);
+    });
+    return launched();
+}
+
+extern "C" int spqt_i8_read(const int8_t *codes, int64_t codes_row, const float *scales, int64_t rows, int64_t K, int type, void *out, int64_t out_row, void *stream) {
+    if (!sixteen_bits(type)) return SPQT_EINVAL;
+    int rc = check_extents(rows, K, SPQT_I8_MAX_K);
+    if (rc == SPQT_OK) rc = check_codes(codes, codes_row, rows, K, false);
+    if (rc == SPQT_OK) rc = check_scales(scales);
+    if (rc == SPQT_OK) rc = check_matrix(out, out_row, rows, K, 2, true);
+    if (rc != SPQT_OK) return rc;
+    const int per_row = (int)((K + 2047) / 2048);
+    const int64_t units = rows * per_row;
+    const Read a = {codes, scales, (uint16_t *)out, codes_row, out_row, (int)rows, (int)K, per_row};
+    const dim3 grid((unsigned)(units < 1 << 22 ? units : 1 << 22));
+    if (type == SPQT_I8_BF16) hipLaunchKernelGGL(spqt_i8_read_kernel<true>, grid, dim3(256), 0, (hipStream_t)stream, a);
+    else hipLaunchKernelGGL(spqt_i8_read_kernel<false>, grid, dim3(256), 0, (hipStream_t)stream, a);
+    return launched();
+}
+
+extern "C" int spqt_i8_norm(const spqt_i8_norm_call *c, void *stream) {
+    if (!c || !sixteen_bits(c->type) || (!c->codes && !c->out && !c->h_out)) return SPQT_EINVAL;
+    if (!c->block != !c->h_out || (!c->block && (c->block_gain || c->gate)) || !c->codes != !c->scales) return SPQT_EINVAL;
+    if (!(c->eps >= 1e-30f) || !__builtin_isfinite(c->eps) || !__builtin_isfinite(c->residual) || !__builtin_isfinite(c->offset)) return SPQT_EINVAL;
+    if (c->h_out && c->h_out == c->out) return SPQT_EINVAL;
+    const int64_t rows = c->rows, K = c->K;
+    int rc = check_extents(rows, K, SPQT_I8_MAX_NORM);
+    if (rc == SPQT_OK) rc = check_matrix(c->h, c->h_row, rows, K, 2, false);
+    if (rc == SPQT_OK) rc = check_matrix(c->gain, 0, 1, K, 2, false);
+    if (rc == SPQT_OK && c->block) rc = check_matrix(c->block, c->block_row, rows, K, 2, false);
+    if (rc == SPQT_OK && c->block_gain) rc = check_matrix(c->block_gain, 0, 1, K, 2, false);
+    if (rc == SPQT_OK && c->gate) rc = check_matrix(c->gate, c->gate_row, rows, K, 2, false);
+    if (rc == SPQT_OK && c->h_out) rc = check_matrix(c->h_out, c->h_out_row, rows, K, 2, true);
+    if (rc == SPQT_OK && c->out) rc = check_matrix(c->out, c->out_row, rows, K, 2, true);
+    if (rc == SPQT_OK && c->codes) rc = check_codes(c->codes, c->codes_row, rows, K, true);
+    if (rc == SPQT_OK && c->codes) rc = check_scales(c->scales);
+    if (rc != SPQT_OK) return rc;
+    const Norm a = {(const uint16_t *)c->h, (const uint16_t *)c->block, (const uint16_t *)c->block_gain, (const uint16_t *)c->gate, (const uint16_t *)c->gain,
+                    (uint16_t *)c->h_out, (uint16_t *)c->out, c->codes, c->scales, c->h_row, c->block_row, c->gate_row, c->h_out_row, c->out_row, c->codes_row,
+                    (int)rows, (int)K, c->residual, c->eps, c->offset};
+    dispatch(K, c->type, [&](auto t, auto v, auto bf16) {
+        typedef Shape<decltype(t)::value> S;
+        hipLaunchKernelGGL((spqt_i8_norm_kernel<decltype(t)::value, decltype(v)::value, decltype(bf16)::value>), grid_of<S>(rows), dim3(S::kThreads), 0,
+                           (hipStream_t)stream, a);
+    });
+    return launched();
+}
