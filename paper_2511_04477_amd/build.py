@@ -22,7 +22,7 @@ SOURCES = ["pack.cpp", "quant_cb.cpp", "gather.hip", "gemv.hip", "gemv_cb.hip", 
 # The key/value cache: one set of objects for all variants of the library, since it has neither their reducers nor their stamps.
 KV_SOURCES = ["kv_append.hip", "kv_attend.hip", "kv_step.hip", "kv_prompt.hip", "kv_weigh.hip", "kv_evict.hip"]
 # The prompt side in 8-bit integers, for which the same holds.
-I8_SOURCES = ["i8_rows.hip", "i8_gemm.hip", "i8_few.hip"]
+I8_SOURCES = ["i8_rows.hip", "i8_gemm.hip", "i8_few.hip", "i8_tiles.hip"]
 SHARED_SOURCES = KV_SOURCES + I8_SOURCES
 CALIB_LIB = os.path.join(PKG, "libspqt_calib.so")       # benchmark-only helper kernels
 CALIB_SOURCES = ["calib.hip", "baseline_rowmajor.hip"]

@@ -12,6 +12,7 @@
 
 #include <ATen/PythonTorchFunctionTLS.h>
 #include <ATen/core/TensorBase.h>
+#include <c10/hip/HIPFunctions.h>
 #include <c10/hip/HIPStream.h>
 #include <torch/csrc/autograd/python_variable.h>
 
@@ -20,6 +21,7 @@
 
 #include "spqt.h"
 #include "spqt_colblock.h"
+#include "spqt_i8.h"
 #include "spqt_kv.h"
 
 namespace {
@@ -356,10 +358,133 @@ PyObject *kv_evict(PyObject *, PyObject *const *a, Py_ssize_t n) {
     });
 }
 
+// The prompt side in 8-bit integers (i8.py): matrices whose rows are dense and any distance apart, on the current device.
+struct I8Device {
+    c10::DeviceIndex index = c10::hip::current_device();
+};
+const at::Tensor &i8_tensor(PyObject *o, I8Device d, int64_t dims) {
+    if (!THPVariable_CheckExact(o)) throw NotPlain();
+    const at::Tensor &t = THPVariable_Unpack(o);
+    const c10::TensorImpl *impl = t.unsafeGetTensorImpl();
+    if (!t.defined() || impl->is_python_dispatch() || !impl->has_storage() || t.layout() != at::kStrided || !t.is_cuda() || t.device().index() != d.index || t.dim() != dims)
+        throw NotPlain();
+    if (t.size(dims - 1) > 1 && t.stride(dims - 1) != 1) throw NotPlain();
+    return t;
+}
+struct I8Matrix {
+    void *p;
+    int64_t row, rows, K;
+    at::ScalarType type;
+};
+I8Matrix i8_matrix(PyObject *o, I8Device d) {
+    const at::Tensor &t = i8_tensor(o, d, 2);
+    return {t.data_ptr(), t.size(0) > 1 ? t.stride(0) : 0, t.size(0), t.size(1), t.scalar_type()};
+}
+I8Matrix i8_matrix(PyObject *o, I8Device d, at::ScalarType type, int64_t rows, int64_t K) {
+    const I8Matrix m = i8_matrix(o, d);
+    if (m.type != type || m.rows != rows || m.K != K) throw NotPlain();
+    return m;
+}
+void *i8_vector(PyObject *o, I8Device d, at::ScalarType type, int64_t n) {
+    const at::Tensor &t = i8_tensor(o, d, 1);
+    if (t.scalar_type() != type || t.size(0) != n) throw NotPlain();
+    return t.data_ptr();
+}
+int i8_type(at::ScalarType t) {
+    if (t != at::kHalf && t != at::kBFloat16) throw NotPlain();
+    return t == at::kBFloat16 ? SPQT_I8_BF16 : SPQT_I8_FP16;
+}
+// i8_quantize(function, x, codes, scales, stream)
+PyObject *i8_quantize(PyObject *, PyObject *const *a, Py_ssize_t n) {
+    return guarded(n, 5, [&]() {
+        const I8Device d;
+        const I8Matrix x = i8_matrix(a[1], d), c = i8_matrix(a[2], d, at::kChar, x.rows, x.K);
+        return call(function<decltype(&spqt_i8_quantize)>(a[0]), x.p, x.row, x.rows, x.K, i8_type(x.type), (int8_t *)c.p, c.row,
+                    (float *)i8_vector(a[3], d, at::kFloat, x.rows), current_stream(a[4]));
+    });
+}
+// i8_read(function, codes, scales, out, stream)
+PyObject *i8_read(PyObject *, PyObject *const *a, Py_ssize_t n) {
+    return guarded(n, 5, [&]() {
+        const I8Device d;
+        const I8Matrix o = i8_matrix(a[3], d), c = i8_matrix(a[1], d, at::kChar, o.rows, o.K);
+        return call(function<decltype(&spqt_i8_read)>(a[0]), (const int8_t *)c.p, c.row, (const float *)i8_vector(a[2], d, at::kFloat, o.rows), o.rows, o.K,
+                    i8_type(o.type), o.p, o.row, current_stream(a[4]));
+    });
+}
+// i8_norm(function, h, gain, out, codes, scales, block, block_gain, gate, residual, eps, offset, h_out, stream)
+PyObject *i8_norm(PyObject *, PyObject *const *a, Py_ssize_t n) {
+    return guarded(n, 14, [&]() {
+        const I8Device d;
+        const I8Matrix h = i8_matrix(a[1], d);
+        spqt_i8_norm_call c = {};
+        auto matrix = [&](PyObject *o, at::ScalarType type, int64_t &row) -> void * {
+            if (o == Py_None) return nullptr;
+            const I8Matrix m = i8_matrix(o, d, type, h.rows, h.K);
+            row = m.row;
+            return m.p;
+        };
+        auto vector = [&](PyObject *o) { return o == Py_None ? nullptr : i8_vector(o, d, h.type, h.K); };
+        c.h = h.p;
+        c.h_row = h.row;
+        c.gain = i8_vector(a[2], d, h.type, h.K);
+        c.out = matrix(a[3], h.type, c.out_row);
+        c.codes = (int8_t *)matrix(a[4], at::kChar, c.codes_row);
+        c.scales = a[5] == Py_None ? nullptr : (float *)i8_vector(a[5], d, at::kFloat, h.rows);
+        if (!c.codes != !c.scales) throw NotPlain();
+        c.block = matrix(a[6], h.type, c.block_row);
+        c.block_gain = vector(a[7]);
+        if (a[8] != Py_None && THPVariable_CheckExact(a[8]) && THPVariable_Unpack(a[8]).dim() == 1) c.gate = vector(a[8]);
+        else c.gate = matrix(a[8], h.type, c.gate_row);
+        c.residual = threshold(a[9]);
+        c.eps = threshold(a[10]);
+        c.offset = threshold(a[11]);
+        c.h_out = matrix(a[12], h.type, c.h_out_row);
+        c.rows = h.rows;
+        c.K = h.K;
+        c.type = i8_type(h.type);
+        return call(function<decltype(&spqt_i8_norm)>(a[0]), &c, current_stream(a[13]));
+    });
+}
+// i8_gemm(function, codes, scales, weights, weight_scales, y, bias, gated, workspace, stream)
+PyObject *i8_gemm(PyObject *, PyObject *const *a, Py_ssize_t n) {
+    return guarded(n, 10, [&]() {
+        const I8Device d;
+        const I8Matrix codes = i8_matrix(a[1], d), w = i8_matrix(a[3], d), y = i8_matrix(a[5], d);
+        if (codes.type != at::kChar || w.type != at::kChar || w.K != codes.K || !PyBool_Check(a[7])) throw NotPlain();
+        spqt_i8_product c = {};
+        c.gated = a[7] == Py_True;
+        if (y.rows != codes.rows || y.K != (c.gated ? w.rows / 2 : w.rows)) throw NotPlain();
+        c.codes = (const int8_t *)codes.p;
+        c.scales = (const float *)i8_vector(a[2], d, at::kFloat, codes.rows);
+        c.weights = (const int8_t *)w.p;
+        c.weight_scales = (const float *)i8_vector(a[4], d, at::kFloat, w.rows);
+        c.bias = a[6] == Py_None ? nullptr : (const float *)i8_vector(a[6], d, at::kFloat, w.rows);
+        c.y = y.p;
+        c.codes_row = codes.row;
+        c.weights_row = w.row;
+        c.y_row = y.row;
+        c.rows = codes.rows;
+        c.N = w.rows;
+        c.K = codes.K;
+        c.y_type = y.type == at::kFloat ? SPQT_I8_FP32 : i8_type(y.type);
+        void *space = nullptr;
+        size_t bytes = 0;
+        if (a[8] != Py_None) {
+            const at::Tensor &t = i8_tensor(a[8], d, 1);
+            if (t.scalar_type() != at::kByte) throw NotPlain();
+            space = t.data_ptr();
+            bytes = (size_t)t.numel();
+        }
+        return call(function<decltype(&spqt_i8_gemm)>(a[0]), &c, space, bytes, current_stream(a[9]));
+    });
+}
+
 #define SPQT_METHOD(name) {#name, (PyCFunction)(void (*)(void))name, METH_FASTCALL, nullptr}
 PyMethodDef methods[] = {SPQT_METHOD(gather),  SPQT_METHOD(gather_rows), SPQT_METHOD(gemv),         SPQT_METHOD(gemv_fused), SPQT_METHOD(gemv_fused_rows),
                          SPQT_METHOD(cb_gemv), SPQT_METHOD(cb_gemv_one), SPQT_METHOD(cb_gemv_fused),
-                         SPQT_METHOD(kv_append), SPQT_METHOD(kv_read), SPQT_METHOD(kv_attention), SPQT_METHOD(kv_evict), {nullptr, nullptr, 0, nullptr}};
+                         SPQT_METHOD(kv_append), SPQT_METHOD(kv_read), SPQT_METHOD(kv_attention), SPQT_METHOD(kv_evict),
+                         SPQT_METHOD(i8_quantize), SPQT_METHOD(i8_read), SPQT_METHOD(i8_norm), SPQT_METHOD(i8_gemm), {nullptr, nullptr, 0, nullptr}};
 PyModuleDef module = {PyModuleDef_HEAD_INIT, "_fastcall", "Device calls of binding.py without the interpreter.", -1, methods, nullptr, nullptr, nullptr, nullptr};
 
 }  // namespace

@@ -24,7 +24,7 @@ typedef int i32x4 __attribute__((ext_vector_type(4)));
 typedef int i32x16 __attribute__((ext_vector_type(16)));
 // Vectors at any element: the memory takes 16 bytes of a lane at any address.
 typedef u32x4 u32x4_at2 __attribute__((aligned(2)));
-typedef u32x2 u32x2_at1 __attribute__((aligned(1)));
+typedef f32x4 f32x4_at4 __attribute__((aligned(4)));
 
 __device__ __forceinline__ float as_float(uint32_t bits) { return __builtin_bit_cast(float, bits); }
 __device__ __forceinline__ uint32_t as_u32(float f) { return __builtin_bit_cast(uint32_t, f); }

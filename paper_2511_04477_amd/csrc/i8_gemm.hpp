@@ -23,7 +23,8 @@ __device__ __forceinline__ float scaled(const Product &p, int sum, float scale, 
     if (p.bias) v += p.bias[n];
     return v;
 }
-__device__ __forceinline__ float gated_by(float gate, float up) { return gate / (1.0f + __expf(-gate)) * up; }
+// (the reciprocal of the hardware is off by a step at most)
+__device__ __forceinline__ float gated_by(float gate, float up) { return gate * __builtin_amdgcn_rcpf(1.0f + __expf(-gate)) * up; }
 
 __device__ __forceinline__ void store_one(const Product &p, int64_t row, int n, float v) {
     const int64_t at = row * p.y_row + n;
@@ -42,6 +43,13 @@ __device__ __forceinline__ i32x4 masked(i32x4 x, int k, int K) {
 }
 
 void launch_few(const Product &p, bool gated, hipStream_t stream);
+
+// A shape of tiles (i8_tiles.hip has them) and the parts that K is divided into.
+struct Plan {
+    int shape, parts;
+};
+Plan plan_tiles(const Product &p, bool gated, size_t room);       // room: bytes for the parts' sums; shape -1: none can
+void launch_tiles_of(const Plan &plan, const Product &p, bool gated, void *workspace, hipStream_t stream);
 
 }  // namespace i8
 }  // namespace spqt

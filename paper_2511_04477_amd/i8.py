@@ -77,6 +77,10 @@ def new_i8_codes(rows: int, K: int, device="cuda"):
 
 def spqt_i8_quantize(x, codes, scales, stream=None) -> None:
     """Codes int8 [rows, K] and scales float32 [rows] of x [rows, K]."""
+    if _b._fast is not None:
+        rc = _b._fast.i8_quantize((_b._lib or lib()).at["spqt_i8_quantize"], x, codes, scales, stream)
+        if rc is not None:
+            return _check(rc)
     torch, halves = _types()
     device = _device()
     x = _tensor(x, halves, (None, None), "x", device)
@@ -86,6 +90,10 @@ def spqt_i8_quantize(x, codes, scales, stream=None) -> None:
 
 def spqt_i8_read(codes, scales, out, stream=None) -> None:
     """out [rows, K] = code * scale."""
+    if _b._fast is not None:
+        rc = _b._fast.i8_read((_b._lib or lib()).at["spqt_i8_read"], codes, scales, out, stream)
+        if rc is not None:
+            return _check(rc)
     torch, halves = _types()
     device = _device()
     o = _tensor(out, halves, (None, None), "out", device)
@@ -98,6 +106,10 @@ def spqt_i8_norm(h, gain, out=None, codes=None, scales=None, block=None, block_g
     """The norms around a block, h [rows, K]: with block, h_out = residual * h + block, the block first normed with block_gain [K] and multiplied by gate ([K] or
     [rows, K]) if they are given; then out and / or codes and scales of that sum (of h, without a block) normed with gain [K].  Gains count from `offset` on.
     h_out may be h or block; out may be h or block."""
+    if _b._fast is not None:
+        rc = _b._fast.i8_norm((_b._lib or lib()).at["spqt_i8_norm"], h, gain, out, codes, scales, block, block_gain, gate, residual, eps, offset, h_out, stream)
+        if rc is not None:
+            return _check(rc)
     torch, halves = _types()
     device = _device()
     h = _tensor(h, halves, (None, None), "h", device)
@@ -138,6 +150,10 @@ def spqt_i8_gemm(codes, scales, weights, weight_scales, y, bias=None, gated: boo
     """y [rows, N] float16, bfloat16 or float32 = (codes [rows, K] times weights int8 [N, K]) * scales [rows] * weight_scales [N] + bias float32 [N].
     gated: weights of N / 2 rows of a gate and, behind them, of an up projection; y [rows, N / 2] = silu(gate) * up.
     workspace (new_i8_workspace): lets K be divided where rows and channels alone do not fill the chip; None: y is the same, and the call may take longer."""
+    if _b._fast is not None:
+        rc = _b._fast.i8_gemm((_b._lib or lib()).at["spqt_i8_gemm"], codes, scales, weights, weight_scales, y, bias, gated, workspace, stream)
+        if rc is not None:
+            return _check(rc)
     torch, halves = _types()
     device = _device()
     c, s = _codes(codes, scales, (None, None), device)

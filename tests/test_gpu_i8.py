@@ -290,7 +290,67 @@ def test_products(gpu, rows, N, K, dtype):
         assert same(check_product(gpu, inputs, dtype, gated=True, space=space, pitch=(8 - N // 2) % 8, at=0), g)
 
 
-@pytest.mark.parametrize("rows,N", [(1, 20), (20, 40), (130, 140), (300, 300)])
+# Sizes that different tiles and numbers of parts are taken for, with edges in every dimension.
+LARGE = [(771, 14331, 4101), (1021, 8183, 28672), (1500, 5118, 5131), (509, 10222, 8192), (1019, 4090, 4109), (250, 4094, 14336), (40, 8190, 28672), (127, 2050, 20000),
+         (4001, 3070, 1000), (8000, 598, 400), (2047, 2050, 130), (65, 128, 131071)]
+
+
+@pytest.mark.parametrize("dtype", ["float16", "bfloat16", "float32"])
+@pytest.mark.parametrize("rows,N,K", LARGE)
+def test_large_products(gpu, rows, N, K, dtype):
+    """Bit for bit what sixteen rows at a time give, and a few rows of that against 64 bits."""
+    dtype = getattr(torch, dtype)
+    codes, scales, weights, weight_scales, _ = product_inputs(rows, N, K, 3)
+    space = gpu.new_i8_workspace(rows, N, K)
+    space.fill_(255)
+    for gated in (False, True):
+        if gated and N % 2:
+            weights, weight_scales, N = weights[:-1], weight_scales[:-1], N - 1
+        outputs = N // 2 if gated else N
+        want = torch.zeros((rows, outputs), dtype=dtype, device="cuda")
+        for r in range(0, rows, 16):
+            gpu.spqt_i8_gemm(codes[r : r + 16], scales[r : r + 16], weights, weight_scales, want[r : r + 16], gated=gated)
+        for given in (None, space):
+            y, whole = guarded(rows, outputs, outputs + 2, dtype, 1)
+            gpu.spqt_i8_gemm(codes, scales, weights, weight_scales, y, gated=gated, workspace=given)
+            assert same(y, want) and untouched(y, whole)
+        some = [0, 1, rows // 2, rows - 1]
+        exact, off = oracle.product(codes[some].cpu(), scales[some].cpu(), weights.cpu(), weight_scales.cpu(), gated=gated)
+        assert rounded_to(want[some], exact, off, dtype)
+
+
+def test_a_workspace_for_more_serves_less(gpu):
+    space = gpu.new_i8_workspace(600, 4096, 9000)
+    for rows, N, K in ((600, 4096, 9000), (17, 40, 300), (250, 4000, 8999), (1, 4096, 9000), (600, 4096, 127)):
+        inputs = product_inputs(rows, N, K)
+        y, z = (torch.zeros((rows, N), device="cuda") for _ in range(2))
+        gpu.spqt_i8_gemm(*inputs[:4], y, workspace=space)
+        gpu.spqt_i8_gemm(*inputs[:4], z)
+        assert same(y, z)
+
+
+def test_a_gemv_on_a_products_workspace_gives_no_numbers(gpu):
+    """A product leaves sums where a GEMV relies on zeros: such a GEMV yields NaN until the workspace is prepared again."""
+    import numpy as np
+    from workloads import make_case, quantile_threshold
+    case = make_case(1, "w")
+    M, K = case["M"], case["K"]
+    packed, x = torch.from_numpy(gpu.spqt_pack(case["q_rowmajor"], case["scales"])).cuda(), torch.from_numpy(case["x"][0]).cuda()
+    space = gpu.new_i8_workspace(250, 4096, 14336)
+    assert space.numel() >= gpu.spqt_workspace_bytes(M, K)
+    gpu.spqt_workspace_init(space)
+    inputs = product_inputs(250, 4096, 14336)
+    y = torch.zeros((250, 4096), device="cuda")
+    gpu.spqt_i8_gemm(*inputs[:4], y, workspace=space)
+    out = torch.zeros(M, device="cuda")
+    gpu.spqt_gemv_fused(packed, M, K, x, quantile_threshold(case["x"], 0.5), out, space)
+    assert bool(out.isnan().any())
+    gpu.spqt_workspace_init(space)
+    gpu.spqt_gemv_fused(packed, M, K, x, quantile_threshold(case["x"], 0.5), out, space)
+    assert bool(torch.isfinite(out).all()) and np.isfinite(float(out.abs().max()))
+
+
+@pytest.mark.parametrize("rows,N", [(1, 20), (20, 40), (130, 140), (300, 300), (513, 1000)])
 def test_the_longest_sums_are_exact(gpu, rows, N):
     K = 131071
     codes = torch.full((rows, 131072), -128, dtype=torch.int8, device="cuda")[:, :K]
