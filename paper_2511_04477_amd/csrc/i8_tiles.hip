@@ -6,12 +6,13 @@ namespace {
 using namespace spqt;
 using namespace spqt::i8;
 
-// What a shape takes, in us: a step of a lone workgroup and of one of 256, and a tile's beginning and end. From 30 sizes of 20 to 8000 rows, 520 to 28672 channels, K of 400 to 28672.
+// What a shape takes, in us: a step of a lone workgroup and of one of 256, and a tile's beginning and end. From 30 sizes of 20 to 8000 rows, 520 to 28672 channels, K of 400 to 28672;
+// a step of 128 is 0.87, 0.43, 0.22 and 0.11 us of matrix instructions at 2.4 GHz. 256 of the large tiles draw so much power that the clock falls to 1.75 GHz.
 struct Cost {
     int rows, channels;
     float step, step_full, fixed;
 };
-constexpr Cost kShapes[] = {{256, 256, 1.0f, 1.7f, 1.0f}, {128, 256, 0.62f, 0.98f, 1.0f}, {128, 128, 0.48f, 0.6f, 2.5f}, {64, 128, 0.42f, 0.43f, 1.5f}};
+constexpr Cost kShapes[] = {{256, 256, 0.95f, 1.62f, 2.5f}, {128, 256, 0.55f, 0.93f, 2.5f}, {128, 128, 0.30f, 0.57f, 2.5f}, {64, 128, 0.22f, 0.36f, 2.0f}};
 constexpr int kCount = sizeof(kShapes) / sizeof(kShapes[0]);
 
 int64_t tiles_of(const Cost &s, const Product &p, bool gated) {
@@ -24,12 +25,12 @@ int64_t tiles_of(const Cost &s, const Product &p, bool gated) {
 namespace spqt {
 namespace i8 {
 
-// The one that is expected to be done first: rounds of 256 workgroups, a tile's steps each; with parts, 4.5 us for the second launch and a us for every 3 MB of sums; and where one
-// tile has all rows, no sooner than 4.7 MB of weights a us.
+// The one that is expected to be done first: rounds of 256 workgroups, a tile's steps each; with parts, 4.5 us for the second launch and a us for every 3 MB of sums. Where one
+// tile has all rows and the weights are more than the caches keep, no sooner than 4.7 MB of weights a us, and 38 KB a us for a workgroup.
 // Rows x channels x K, us of 256 x 256 / 128 x 256 / 128 x 128 / 64 x 128 with the best number of parts each (the one taken is the least, or within 4 % of it):
-//   4001 x 4096 x 14336   191 / 243 / 302 / 459        1500 x 5120 x 5120   56.5 / 44.2 / 58.6 / 87.4      1024 x 4096 x 4096   37.9 / 31.8 / 26.9 / 38.6
-//   1024 x 8192 x 28672   213 (2 parts; one 278) / 240 / 305 / 435       250 x 4096 x 14336   43.4 (7) / 37.7 (7) / 35.4 (4; one 64) / 39.4 (2)
-//   40 x 8192 x 28672     - / - / 55.7 (4) / 53.9 (4; one 110)           20 x 4096 x 4096   - / - / - / 16.8 (3; one 20.5)
+//   4001 x 4096 x 14336   188 / 210 / 268 / 343        1500 x 5120 x 5120   52.0 / 43.1 / 49.4 / 64.0      1024 x 4096 x 4096   38.2 / 28.5 / 24.2 / 31.1
+//   1024 x 8192 x 28672   211 (2 parts; one 287) / 211 / 272 / 385       250 x 4096 x 14336   43.2 (7) / 37.3 (7) / 35.0 (4; two 43.7) / 36.2 (2)
+//   512 x 4096 x 4096     30.6 (3) / 25.1 / 19.4 / 17.2                  40 x 8192 x 28672    - / - / - / 53.5 (4; three 53.6, two 64.9, one 102)
 Plan plan_tiles(const Product &p, bool gated, size_t room) {
     const int64_t line = (int64_t)1 << 31;
     Plan best = {-1, 1};
@@ -43,10 +44,14 @@ Plan plan_tiles(const Product &p, bool gated, size_t room) {
         for (int parts = 1; parts == 1 || (parts <= 16 && parts <= steps && tiles * parts <= kGroups); ++parts) {
             const int64_t units = tiles * parts, sums = units * s.rows * s.channels * 4;
             if (parts > 1 && (size_t)sums > room) break;
-            const double each = (steps + parts - 1) / parts;
-            auto round = [&](int64_t n) { return n == 0 ? 0.0 : each * (s.step + (s.step_full - s.step) * (double)n / kGroups) + s.fixed; };
+            const double each = (steps + parts - 1) / parts, weights = p.N * (double)p.K;
+            const bool streams = p.rows <= s.rows && weights > 32e6;
+            auto round = [&](int64_t n) {
+                const double full = s.step + (s.step_full - s.step) * (double)n / kGroups, least = streams ? s.channels * (128 / 38e3) : 0.0;
+                return n == 0 ? 0.0 : each * (full > least ? full : least) + s.fixed;
+            };
             double us = (double)(units / kGroups) * round(kGroups) + round(units % kGroups);
-            if (p.rows <= s.rows) us = us > p.N * (double)p.K / 4.7e6 ? us : p.N * (double)p.K / 4.7e6;
+            if (streams && us < weights / 4.7e6) us = weights / 4.7e6;
             if (parts > 1) us += 4.5 + (double)sums / 3e6;
             if (best.shape < 0 || us < least) {
                 least = us;
@@ -61,7 +66,7 @@ void launch_tiles_of(const Plan &plan, const Product &p, bool gated, void *works
     switch (plan.shape) {
         case 0: launch_tiles<256, 256, 2, 4, 2, 3>(p, gated, plan.parts, workspace, stream); break;
         case 1: launch_tiles<128, 256, 2, 4, 4, 3>(p, gated, plan.parts, workspace, stream); break;
-        case 2: launch_tiles<128, 128, 2, 2, 5, 5>(p, gated, plan.parts, workspace, stream); break;
+        case 2: launch_tiles<128, 128, 2, 2, 4, 5>(p, gated, plan.parts, workspace, stream); break;
         default: launch_tiles<64, 128, 2, 2, 6, 7>(p, gated, plan.parts, workspace, stream); break;
     }
 }

@@ -59,16 +59,18 @@ struct Shape {
     static constexpr int kRows = TM / WM, kChannels = TN / WN, MI = kRows / 32, NI = kChannels / 32;
     static constexpr int kLoadsA = TM / (8 * kWaves), kLoadsB = TN / (8 * kWaves);
     static constexpr int kRoomA = TM * kStep, kRoomB = TN * kStep, kShared = NA * kRoomA + NB * kRoomB;
+    // A wavefront alone on its SIMD, which has registers enough, reads a whole step ahead; two of them read 32 bytes of K ahead.
+    static constexpr bool kAhead = kWaves == 4 && MI * NI <= 4;
     // Loads that are younger than those of the next step, where a step's wait is (turn() has the order of loads).
-    static constexpr int kYounger = ((NA < NB ? NA : NB) - 2) * (kLoadsA + kLoadsB) + (NB > NA ? kLoadsB : 0);
-    static_assert(NA >= 2 && NB >= 2 && kShared <= 160 * 1024 && kYounger < 64 && kWaves % 2 == 0 && 64 * kChannels <= kLoadsB * 1024);
+    static constexpr int kYounger = ((NA < NB ? NA : NB) - 2) * (kLoadsA + kLoadsB) + (NB > NA && !kAhead ? kLoadsB : 0);
+    static_assert((!kAhead || NB == NA + 1) && NA >= 2 && NB >= 2 && kShared <= 160 * 1024 && kYounger < 64 && kWaves % 2 == 0 && 64 * kChannels <= kLoadsB * 1024);
 };
 
 // What becomes of the sums of 32 rows and a wavefront's channels, from channel n0 on: a lane has fours of channels of one row. They go through shared memory and leave 16 bytes a lane.
 template <class S, int YT, bool GATED>
 struct Finish {
     static constexpr int kOut = GATED ? S::kChannels / 2 : S::kChannels, kBytes = YT == SPQT_I8_FP32 ? 4 : 2;
-    static constexpr int kTimes = kOut * kBytes * 32 > S::kLoadsB * 1024 ? 2 : 1;      // that the channels are divided into, on their way
+    static constexpr int kTimes = kOut * kBytes > 128 ? kOut * kBytes / 128 : 1;       // that the channels are divided into, on their way
     struct Scales {
         f32x4 of[S::NI][4];
     };
@@ -87,20 +89,18 @@ struct Finish {
         for (int e = 0; e < 4; ++e) r[e] = of[(uint32_t)(behind(n) + (channel(n, q) + e < p.outputs ? channel(n, q) + e : p.outputs - 1))];
         return r;
     }
-    __device__ __forceinline__ Scales scales() const {
-        Scales s;
-        if (inside) {
+    // Of all this lane's channels; where not all of them are `inside`, one by one.
+    __device__ __forceinline__ void scales(Scales &s) const {
 #pragma unroll
-            for (int n = 0; n < S::NI; ++n)
+        for (int n = 0; n < S::NI; ++n)
 #pragma unroll
-                for (int q = 0; q < 4; ++q) s.of[n][q] = four(p.weight_scales, n, q);
-        } else {
+            for (int q = 0; q < 4; ++q) s.of[n][q] = four(p.weight_scales, n, q);
+    }
+    __device__ __forceinline__ void scales_at_edge(Scales &s) const {
 #pragma unroll
-            for (int n = 0; n < S::NI; ++n)
+        for (int n = 0; n < S::NI; ++n)
 #pragma unroll
-                for (int q = 0; q < 4; ++q) s.of[n][q] = four_at_edge(p.weight_scales, n, q);
-        }
-        return s;
+            for (int q = 0; q < 4; ++q) s.of[n][q] = four_at_edge(p.weight_scales, n, q);
     }
     __device__ __forceinline__ float scale_of_row(int first) const { return p.scales[first + line < p.rows ? first + line : p.rows - 1]; }
 
@@ -237,9 +237,9 @@ __global__ __launch_bounds__(WM * WN * 64, 1) void spqt_i8_tiles_kernel(Product 
 #pragma unroll
         for (uint32_t &o : offsets) o -= back;
     };
-    auto advance = [&](Cursor &c, auto aim, auto &offsets, int rooms) {
+    auto advance = [&](Cursor &c, auto aim, auto &offsets, int rooms, auto inner) {
         c.room = c.room + 1 < rooms ? c.room + 1 : 0;
-        if (c.step + 1 < c.end) {
+        if (decltype(inner)::value || c.step + 1 < c.end) {
             ++c.step;
             c.from += kStep;
         } else {
@@ -247,35 +247,43 @@ __global__ __launch_bounds__(WM * WN * 64, 1) void spqt_i8_tiles_kernel(Product 
             ++c.round;
             aim();
         }
-        folded(c, offsets);
+        if (!decltype(inner)::value) folded(c, offsets);
     };
-    auto advance_a = [&]() { advance(ca, aim_a, a_off, NA); };
-    auto advance_b = [&]() { advance(cb, aim_b, b_off, NB); };
+    auto advance_a = [&](auto inner) { advance(ca, aim_a, a_off, NA, inner); };
+    auto advance_b = [&](auto inner) { advance(cb, aim_b, b_off, NB, inner); };
+    const std::false_type no;
+    const std::true_type yes;
 
     // Multiplying: of the 32s of K in a step, lanes 0 to 31 have the first 16 of a 32 and the others the second.
     i32x16 acc[S::MI][S::NI];
-    i32x4 x[2][S::MI], w[2][S::NI];
+    constexpr int kSets = S::kAhead ? 8 : 2, kReads = S::MI + S::NI, kProducts = S::MI * S::NI;
+    i32x4 x[kSets][S::MI], w[kSets][S::NI];                       // of 32s of K
     int place[4];
 #pragma unroll
     for (int kk = 0; kk < 4; ++kk) place[kk] = line * kStep + (((kk * 2 + half) ^ swizzle(line)) << 4);
     int room_a = 0, room_b = 0, next_a = 0, next_b = 0;           // of this step and the next one
-    auto read = [&](bool next, int kk, int i) {
-        if (i < S::NI) w[kk & 1][i] = *reinterpret_cast<const i32x4 *>(shared + NA * S::kRoomA + (next ? next_b : room_b) * S::kRoomB + place[kk] + (wn * S::kChannels + i * 32) * kStep);
-        else x[kk & 1][i - S::NI] = *reinterpret_cast<const i32x4 *>(shared + (next ? next_a : room_a) * S::kRoomA + place[kk] + (wm * S::kRows + (i - S::NI) * 32) * kStep);
+    auto read = [&](bool next, int kk, int set, int i) {
+        if (i < S::NI) w[set][i] = *reinterpret_cast<const i32x4 *>(shared + NA * S::kRoomA + (next ? next_b : room_b) * S::kRoomB + place[kk] + (wn * S::kChannels + i * 32) * kStep);
+        else x[set][i - S::NI] = *reinterpret_cast<const i32x4 *>(shared + (next ? next_a : room_a) * S::kRoomA + place[kk] + (wm * S::kRows + (i - S::NI) * 32) * kStep);
     };
-    auto multiply = [&](auto kk_, int step, auto tail) {
-        constexpr int kk = decltype(kk_)::value;
+    auto mask = [&](int kk, int set, int step, auto tail) {
         if (decltype(tail)::value && ragged && step == t.steps - 1)
 #pragma unroll
-            for (int i = 0; i < S::MI; ++i) x[kk & 1][i] = masked(x[kk & 1][i], step * kStep + (kk * 2 + half) * 16, p.K);
-        constexpr int kReads = S::MI + S::NI, kProducts = S::MI * S::NI, kPer = (kReads + kProducts - 1) / kProducts;
+            for (int i = 0; i < S::MI; ++i) x[set][i] = masked(x[set][i], step * kStep + (kk * 2 + half) * 16, p.K);
+    };
+    auto product = [&](int set, int i) {
+        const int m = i / S::NI, n = i % S::NI;
+        acc[m][n] = __builtin_amdgcn_mfma_i32_32x32x32_i8(w[set][n], x[set][m], acc[m][n], 0, 0, 0);
+    };
+    auto multiply = [&](auto kk_, int step, auto tail) {
+        constexpr int kk = decltype(kk_)::value, kPer = (kReads + kProducts - 1) / kProducts;
+        mask(kk, kk & 1, step, tail);
 #pragma unroll
         for (int i = 0; i < kProducts; ++i) {
-            const int m = i / S::NI, n = i % S::NI;
-            acc[m][n] = __builtin_amdgcn_mfma_i32_32x32x32_i8(w[kk & 1][n], x[kk & 1][m], acc[m][n], 0, 0, 0);
+            product(kk & 1, i);
 #pragma unroll
             for (int j = i * kPer; j < (i + 1) * kPer && j < kReads; ++j)
-                if (kk < 3 || !decltype(tail)::value) read(kk == 3, (kk + 1) % 4, j);
+                if (kk < 3 || !decltype(tail)::value) read(kk == 3, (kk + 1) % 4, (kk + 1) & 1, j);
             if (kk == 3) {
 #pragma unroll
                 for (int j = 0; j < S::kLoadsA; ++j)
@@ -289,28 +297,54 @@ __global__ __launch_bounds__(WM * WN * 64, 1) void spqt_i8_tiles_kernel(Product 
         }
     };
     // Until the next step's loads are there, of all wavefronts; younger ones may be on their way.
-    auto meet = [&]() {
-        asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)" : : "n"(S::kYounger) : "memory");
+    auto meet = [&](auto younger) {
+        asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)" : : "n"(decltype(younger)::value) : "memory");
         __builtin_amdgcn_s_barrier();
         asm volatile("" ::: "memory");
         __builtin_amdgcn_sched_barrier(0);
     };
-    // Step t: B(t - 1 + NB) is loaded beside its first three 32s of K, where step t - 1 has left room; then A(t + NA) beside the fourth, for which everyone has read step t.
-    auto turn = [&](int step, auto tail) {
+    typedef std::integral_constant<int, S::kYounger> Younger;
+    // inner: a step in the middle of a unit, from which both cursors move on to the next step and no other; tail: the last one of a unit.
+    auto turn = [&](int step, auto odd_, auto inner, auto tail) {
         next_a = room_a + 1 < NA ? room_a + 1 : 0;
         next_b = room_b + 1 < NB ? room_b + 1 : 0;
-        multiply(std::integral_constant<int, 0>(), step, tail);
-        multiply(std::integral_constant<int, 1>(), step, tail);
-        multiply(std::integral_constant<int, 2>(), step, tail);
-        advance_b();
-        meet();
-        multiply(std::integral_constant<int, 3>(), step, tail);
-        advance_a();
+        if constexpr (S::kAhead) {
+            // Step t is in registers, everyone's; B(t - 1 + NB), A(t + NA) are loaded and step t + 1 read beside its products.
+            constexpr int kOdd = decltype(odd_)::value, kAll = 4 * kProducts, kLoads = S::kLoadsA + S::kLoadsB, kPer = (4 * kReads + kAll - 1) / kAll;
+            meet(Younger());
+#pragma unroll
+            for (int kk = 0; kk < 4; ++kk) mask(kk, 4 * kOdd + kk, step, tail);
+#pragma unroll
+            for (int i = 0; i < kAll; ++i) {
+                product(4 * kOdd + i / kProducts, i % kProducts);
+#pragma unroll
+                for (int j = i * kPer; j < (i + 1) * kPer && j < 4 * kReads; ++j)
+                    if (!decltype(tail)::value) read(true, j / kReads, 4 * (1 - kOdd) + j / kReads, j % kReads);
+#pragma unroll
+                for (int j = 0; j < kLoads; ++j)
+                    if (j * kAll / kLoads == i) {
+                        if (j < S::kLoadsB) load_b(j);
+                        else load_a(j - S::kLoadsB);
+                    }
+                __builtin_amdgcn_sched_barrier(0);
+            }
+            advance_b(inner);
+            advance_a(inner);
+        } else {
+            // Step t: B(t - 1 + NB) is loaded beside its first three 32s of K, where step t - 1 has left room; then A(t + NA) beside the fourth, for which everyone has read step t.
+            multiply(std::integral_constant<int, 0>(), step, tail);
+            multiply(std::integral_constant<int, 1>(), step, tail);
+            multiply(std::integral_constant<int, 2>(), step, tail);
+            advance_b(inner);
+            meet(Younger());
+            multiply(std::integral_constant<int, 3>(), step, tail);
+            advance_a(inner);
+        }
         room_a = next_a;
         room_b = next_b;
     };
 
-    // the loads that turns -NB to -2 would have made, and those of turn -1
+    // the loads that the turns before the first one would have made
     aim_a();
     aim_b();
     folded(ca, a_off);
@@ -318,17 +352,27 @@ __global__ __launch_bounds__(WM * WN * 64, 1) void spqt_i8_tiles_kernel(Product 
     auto all_a = [&]() {
 #pragma unroll
         for (int i = 0; i < S::kLoadsA; ++i) load_a(i);
-        advance_a();
+        advance_a(no);
     };
+    auto all_b = [&]() {
 #pragma unroll
-    for (int j = -(NA > NB ? NA : NB); j <= -1; ++j) {
-        if (j == -1) meet();
-        if (j + NA >= 0) all_a();
-        if (j + NB >= 0 && j < -1) {
-#pragma unroll
-            for (int i = 0; i < S::kLoadsB; ++i) load_b(i);
-            advance_b();
+        for (int i = 0; i < S::kLoadsB; ++i) load_b(i);
+        advance_b(no);
+    };
+    if constexpr (S::kAhead) {
+        for (int j = 0; j < NA; ++j) {
+            all_b();
+            all_a();
         }
+        meet(std::integral_constant<int, (NA - 1) * (S::kLoadsA + S::kLoadsB)>());
+    } else {
+#pragma unroll
+        for (int j = -(NA > NB ? NA : NB); j < -1; ++j) {
+            if (j + NA >= 0) all_a();
+            if (j + NB >= 0) all_b();
+        }
+        meet(Younger());
+        all_a();
     }
 
     for (int round = 0;; ++round) {
@@ -340,18 +384,43 @@ __global__ __launch_bounds__(WM * WN * 64, 1) void spqt_i8_tiles_kernel(Product 
         for (int m = 0; m < S::MI; ++m)
 #pragma unroll
             for (int n = 0; n < S::NI; ++n) acc[m][n] = i32x16{};
-        // (each unit's first 32s of K here, the others beside the products before them: what is read after a unit's outputs needs no registers while these are made)
+        // (a unit's first operands are read here, the others beside the products before them: what is read after a unit's outputs needs no registers while these are made)
+        const std::integral_constant<int, 0> even;
+        const std::integral_constant<int, 1> odd;
 #pragma unroll
-        for (int i = 0; i < S::MI + S::NI; ++i) read(false, 0, i);
-        for (int s = u.begin; s < u.end - 1; ++s) turn(s, std::false_type());
+        for (int kk = 0; kk < kSets / 2; ++kk)
+#pragma unroll
+            for (int i = 0; i < kReads; ++i) read(false, kk, kk, i);
+        int s = u.begin;
+        const int inner = u.end - (NA > NB ? NA : NB) - 2;
+        if constexpr (S::kAhead) {
+            for (; s + 1 < inner; s += 2) {
+                turn(s, even, yes, no);
+                turn(s + 1, odd, yes, no);
+            }
+            for (; s + 2 < u.end; s += 2) {
+                turn(s, even, no, no);
+                turn(s + 1, odd, no, no);
+            }
+        } else {
+            for (; s < inner; ++s) turn(s, even, yes, no);
+            for (; s < u.end - 1; ++s) turn(s, even, no, no);
+        }
         const int here = anew(lane);
         const Finish<S, YT, GATED> finish(p, u.channel_tile * kMade + wn * (S::kChannels / (GATED ? 2 : 1)), here & 31, here >> 5);
-        // (asked for before the last step, used after it)
-        const typename Finish<S, YT, GATED>::Scales by = finish.scales();
+        // Asked for before the last step, used after it. A load that no one waited for would make the compiler wait in the next unit's loop, for the loads that are on their way there.
+        typename Finish<S, YT, GATED>::Scales by;
         float scales[S::MI];
+        if (t.parts == 1 && finish.inside) finish.scales(by);
+        if (t.parts == 1)
 #pragma unroll
-        for (int m = 0; m < S::MI; ++m) scales[m] = finish.scale_of_row(row0 + m * 32);
-        turn(u.end - 1, std::true_type());
+            for (int m = 0; m < S::MI; ++m) scales[m] = finish.scale_of_row(row0 + m * 32);
+        if (S::kAhead && s + 1 < u.end) {
+            turn(s, even, no, no);
+            turn(s + 1, odd, no, yes);
+        } else {
+            turn(s, even, no, yes);
+        }
 
         if (t.parts > 1) {
             i32x4 *to = t.sums + ((size_t)at * S::kWaves + wave) * (S::MI * S::NI * 256);
@@ -366,6 +435,7 @@ __global__ __launch_bounds__(WM * WN * 64, 1) void spqt_i8_tiles_kernel(Product 
                     }
             continue;
         }
+        if (!finish.inside) finish.scales_at_edge(by);
         // The last step's room of the channels is free until the next turn: outputs go through what this wavefront's own loads will write there.
         uint8_t *stage = shared + NA * S::kRoomA + (room_b > 0 ? room_b - 1 : NB - 1) * S::kRoomB + wave * 1024;
 #pragma unroll
@@ -389,7 +459,9 @@ __global__ __launch_bounds__(64) void spqt_i8_join_kernel(Product p, Tiling t) {
     const Finish<S, YT, GATED> finish(p, u.channel_tile * (GATED ? TN / 2 : TN) + wave % WN * (S::kChannels / (GATED ? 2 : 1)), line, half);
     const int first = u.row_tile * TM + wave / WN * S::kRows + m * 32;
     if (first >= p.rows) return;
-    const typename Finish<S, YT, GATED>::Scales by = finish.scales();
+    typename Finish<S, YT, GATED>::Scales by;
+    if (finish.inside) finish.scales(by);
+    else finish.scales_at_edge(by);
     const float scale = finish.scale_of_row(first);
     i32x16 acc[S::NI];
 #pragma unroll
