@@ -1,7 +1,11 @@
 // The product in 8-bit integers, sixteen rows at a time: each weight goes from memory to the matrix instruction of one wavefront.
 //
-// With the weights as its first operand v_mfma_i32_16x16x64_i8 gives a lane four channels of one row. K goes in chunks of 128 bytes, of which a lane has 32:
-// which of them are which is the same for both operands, so any order will do. The wavefronts of a workgroup take the chunks in turn and add their sums up in shared memory.
+// With the weights as its first operand v_mfma_i32_16x16x64_i8 gives a lane four channels of one row. The wavefronts of a workgroup take K in turn, 128 bytes each time, and add their
+// sums up in shared memory: whole numbers, whose order does not matter.
+//
+// What bounds it: reading the weights. 57344 x 8192 with the gate, one row 82 to 86 us = 5.5 to 5.7 TB/s; 28672 x 4096 25.7 us = 4.6; 6144 x 4096 8.5 us (a launch in a graph is 2 to 3 of that).
+// A lane takes the 16 bytes that follow its neighbour's, so that an instruction reads whole halves of lines: with 32 bytes of a lane one after the other the former was 91 us, 28672 x 4096 30.8.
+// Loads that pass the caches by (non-temporal) 93 and 27.0; two chunks on their way for four 81.8 and 26.0, and 6144 x 4096 8.9; 16 wavefronts 81.1 and 25.8.
 #include "i8_gemm.hpp"
 
 namespace {
@@ -9,38 +13,55 @@ namespace {
 using namespace spqt;
 using namespace spqt::i8;
 
-constexpr int kWaves = 8, kChunk = 128;
+constexpr int kChunk = 128;
 
-template <bool GATED>
-__global__ __launch_bounds__(kWaves * 64) void spqt_i8_few_kernel(Product p) {
-    constexpr int C = GATED ? 2 : 1;
-    __shared__ i32x4 sums[kWaves][C][64];
+// W wavefronts, 16 C channels (gated: half of them the gate's, half of them those of the up projection), D chunks of a wavefront on their way together.
+template <int W, int C, int D, bool GATED>
+__global__ __launch_bounds__(W * 64) void spqt_i8_few_kernel(Product p) {
+    constexpr int kMade = GATED ? C / 2 : C;                      // sixteens of outputs
+    __shared__ i32x4 sums[W][C][64];
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, line = lane & 15, quarter = lane >> 4;
-    const int n0 = blockIdx.x * 16, row0 = blockIdx.y * 16;
+    const int n0 = blockIdx.x * (16 * kMade), row0 = blockIdx.y * 16;
     const int row = row0 + line < p.rows ? row0 + line : p.rows - 1;
     const int8_t *a = p.codes + row * p.codes_row, *w[C];
 #pragma unroll
     for (int c = 0; c < C; ++c) {
-        const int n = n0 + line < p.outputs ? n0 + line : p.outputs - 1;
-        w[c] = p.weights + (int64_t)(n + c * p.outputs) * p.weights_row;
+        int n = n0 + c % kMade * 16 + line;
+        n = (n < p.outputs ? n : p.outputs - 1) + c / kMade * p.outputs;
+        w[c] = p.weights + n * p.weights_row;
     }
     i32x4 acc[C];
 #pragma unroll
     for (int c = 0; c < C; ++c) acc[c] = i32x4{0, 0, 0, 0};
     const int whole = p.K / kChunk, chunks = (p.K + kChunk - 1) / kChunk;
-    for (int at = wave; at < whole; at += kWaves) {
+    int at = wave;
+    auto span = [&](auto deep) {
+        constexpr int N = decltype(deep)::value;
+        i32x4 x[N][2], v[N][2][C];
+#pragma unroll
+        for (int d = 0; d < N; ++d)
+#pragma unroll
+            for (int i = 0; i < 2; ++i) {
+                const int k = (at + d * W) * kChunk + i * 64 + quarter * 16;
+#pragma unroll
+                for (int c = 0; c < C; ++c) v[d][i][c] = *reinterpret_cast<const i32x4 *>(w[c] + k);
+                x[d][i] = *reinterpret_cast<const i32x4 *>(a + k);
+            }
+        __builtin_amdgcn_sched_barrier(0);                        // all is asked for before any of it is used
+#pragma unroll
+        for (int d = 0; d < N; ++d)
+#pragma unroll
+            for (int i = 0; i < 2; ++i)
+#pragma unroll
+                for (int c = 0; c < C; ++c) acc[c] = __builtin_amdgcn_mfma_i32_16x16x64_i8(v[d][i][c], x[d][i], acc[c], 0, 0, 0);
+        at += N * W;
+    };
+    while (at + (D - 1) * W < whole) span(std::integral_constant<int, D>());
+    while (at < whole) span(std::integral_constant<int, 1>());
+    if (chunks > whole && whole % W == wave) {
 #pragma unroll
         for (int i = 0; i < 2; ++i) {
-            const int k = at * kChunk + quarter * 32 + i * 16;
-            const i32x4 x = *reinterpret_cast<const i32x4 *>(a + k);
-#pragma unroll
-            for (int c = 0; c < C; ++c) acc[c] = __builtin_amdgcn_mfma_i32_16x16x64_i8(*reinterpret_cast<const i32x4 *>(w[c] + k), x, acc[c], 0, 0, 0);
-        }
-    }
-    if (chunks > whole && whole % kWaves == wave) {
-#pragma unroll
-        for (int i = 0; i < 2; ++i) {
-            const int k = whole * kChunk + quarter * 32 + i * 16, from = k < p.K ? k : 0;       // (behind the row's end nothing is read)
+            const int k = whole * kChunk + i * 64 + quarter * 16, from = k < p.K ? k : 0;       // (behind the row's end nothing is read)
             const i32x4 x = masked(*reinterpret_cast<const i32x4 *>(a + from), k, p.K);
 #pragma unroll
             for (int c = 0; c < C; ++c) acc[c] = __builtin_amdgcn_mfma_i32_16x16x64_i8(*reinterpret_cast<const i32x4 *>(w[c] + from), x, acc[c], 0, 0, 0);
@@ -49,19 +70,30 @@ __global__ __launch_bounds__(kWaves * 64) void spqt_i8_few_kernel(Product p) {
 #pragma unroll
     for (int c = 0; c < C; ++c) sums[wave][c][lane] = acc[c];
     __syncthreads();
-    if (wave > 0 || row0 + line >= p.rows) return;
+    if (wave >= kMade || row0 + line >= p.rows) return;
+    // a wavefront finishes sixteen outputs of a row
+    auto total = [&](int c) {
+        i32x4 t = sums[0][c][lane];
 #pragma unroll
-    for (int c = 0; c < C; ++c)
-        for (int i = 1; i < kWaves; ++i) acc[c] += sums[i][c][lane];
+        for (int i = 1; i < W; ++i) t += sums[i][c][lane];
+        return t;
+    };
+    const i32x4 first = total(wave), second = total(GATED ? wave + kMade : wave);
     const float scale = p.scales[row];
 #pragma unroll
     for (int e = 0; e < 4; ++e) {
-        const int n = n0 + 4 * quarter + e;
+        const int n = n0 + wave * 16 + 4 * quarter + e;
         if (n >= p.outputs) break;
-        float v = scaled(p, acc[0][e], scale, n);
-        if (GATED) v = gated_by(v, scaled(p, acc[C - 1][e], scale, n + p.outputs));
+        float v = scaled(p, first[e], scale, n);
+        if (GATED) v = gated_by(v, scaled(p, second[e], scale, n + p.outputs));
         store_one(p, row, n, v);
     }
+}
+
+template <int W, int C, int D, bool GATED>
+void launch(const Product &p, hipStream_t stream) {
+    const int made = 16 * (GATED ? C / 2 : C);
+    hipLaunchKernelGGL((spqt_i8_few_kernel<W, C, D, GATED>), dim3((p.outputs + made - 1) / made, (p.rows + 15) / 16), dim3(W * 64), 0, stream, p);
 }
 
 }  // namespace
@@ -69,10 +101,14 @@ __global__ __launch_bounds__(kWaves * 64) void spqt_i8_few_kernel(Product p) {
 namespace spqt {
 namespace i8 {
 
+// Sixteen channels a workgroup, thirty-two where the codes are so many that reading them for every sixteen channels counts, and there are workgroups enough all the same: rows x channels x K,
+// us of 16 / 32 channels: 16 x 8192 x 28672 65.3 / 51.0, 4 x 8192 x 28672 50.0 / 47.8, 16 x 57344 x 8192 with the gate 105 / 96; the other way round 1 x 28672 x 4096 25.7 / 27.4,
+// 16 x 4096 x 14336 (few workgroups) 19.7 / 24.1, 1 x 22016 x 4096 22.6 / 27.4.
 void launch_few(const Product &p, bool gated, hipStream_t stream) {
-    const dim3 grid((p.outputs + 15) / 16, (p.rows + 15) / 16);
-    if (gated) hipLaunchKernelGGL(spqt_i8_few_kernel<true>, grid, dim3(kWaves * 64), 0, stream, p);
-    else hipLaunchKernelGGL(spqt_i8_few_kernel<false>, grid, dim3(kWaves * 64), 0, stream, p);
+    const int64_t rows = p.rows < 16 ? p.rows : 16;
+    const bool wide = rows * p.K >= 112 << 10 && p.outputs >= 256 * 32;
+    if (gated) wide ? launch<8, 4, 2, true>(p, stream) : launch<8, 2, 4, true>(p, stream);
+    else wide ? launch<8, 2, 2, false>(p, stream) : launch<8, 1, 4, false>(p, stream);
 }
 
 }  // namespace i8

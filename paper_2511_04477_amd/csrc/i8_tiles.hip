@@ -26,7 +26,7 @@ namespace spqt {
 namespace i8 {
 
 // The one that is expected to be done first: rounds of 256 workgroups, a tile's steps each; with parts, 4.5 us for the second launch and a us for every 3 MB of sums. Where one
-// tile has all rows and the weights are more than the caches keep, no sooner than 4.7 MB of weights a us, and 38 KB a us for a workgroup.
+// tile has all rows and the weights are more than the caches keep, no sooner than 4.7 MB of weights a us, and 33 KB a us for a workgroup.
 // Rows x channels x K, us of 256 x 256 / 128 x 256 / 128 x 128 / 64 x 128 with the best number of parts each (the one taken is the least, or within 4 % of it):
 //   4001 x 4096 x 14336   188 / 210 / 268 / 343        1500 x 5120 x 5120   52.0 / 43.1 / 49.4 / 64.0      1024 x 4096 x 4096   38.2 / 28.5 / 24.2 / 31.1
 //   1024 x 8192 x 28672   211 (2 parts; one 287) / 211 / 272 / 385       250 x 4096 x 14336   43.2 (7) / 37.3 (7) / 35.0 (4; two 43.7) / 36.2 (2)
@@ -47,7 +47,7 @@ Plan plan_tiles(const Product &p, bool gated, size_t room) {
             const double each = (steps + parts - 1) / parts, weights = p.N * (double)p.K;
             const bool streams = p.rows <= s.rows && weights > 32e6;
             auto round = [&](int64_t n) {
-                const double full = s.step + (s.step_full - s.step) * (double)n / kGroups, least = streams ? s.channels * (128 / 38e3) : 0.0;
+                const double full = s.step + (s.step_full - s.step) * (double)n / kGroups, least = streams ? s.channels * (128 / 33e3) : 0.0;
                 return n == 0 ? 0.0 : each * (full > least ? full : least) + s.fixed;
             };
             double us = (double)(units / kGroups) * round(kGroups) + round(units % kGroups);

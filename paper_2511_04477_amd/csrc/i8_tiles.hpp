@@ -466,7 +466,7 @@ __global__ __launch_bounds__(64) void spqt_i8_join_kernel(Product p, Tiling t) {
     i32x16 acc[S::NI];
 #pragma unroll
     for (int n = 0; n < S::NI; ++n) acc[n] = i32x16{};
-#pragma unroll 2
+#pragma unroll 4
     for (int part = 0; part < t.parts; ++part) {
         const i32x4 *from = t.sums + ((((size_t)part * t.tiles + tile) * S::kWaves + wave) * S::MI + m) * S::NI * 256 + lane;
 #pragma unroll
