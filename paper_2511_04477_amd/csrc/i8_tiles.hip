@@ -32,9 +32,10 @@ namespace i8 {
 //   1024 x 8192 x 28672   211 (2 parts; one 287) / 211 / 272 / 385       250 x 4096 x 14336   43.2 (7) / 37.3 (7) / 35.0 (4; two 43.7) / 36.2 (2)
 //   512 x 4096 x 4096     30.6 (3) / 25.1 / 19.4 / 17.2                  40 x 8192 x 28672    - / - / - / 53.5 (4; three 53.6, two 64.9, one 102)
 Plan plan_tiles(const Product &p, bool gated, size_t room) {
-    const int64_t line = (int64_t)1 << 31;
+    // places within a tile, with the gate's and the up projection's channels in one, are 32 bits
+    const int64_t widest = (int64_t)1 << 23;
     Plan best = {-1, 1};
-    if (p.codes_row >= line / 256 || (gated ? p.N + 256 : 256) * p.weights_row >= line || p.y_row >= line / 256) return best;
+    if (p.codes_row >= widest || p.weights_row >= widest || p.y_row >= widest || (gated && (p.N + 256) * p.weights_row >= (int64_t)1 << 32)) return best;
     const int steps = (p.K + kStep - 1) / kStep;
     double least = 0.0;
     for (int i = 0; i < kCount; ++i) {

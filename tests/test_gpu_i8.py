@@ -508,7 +508,11 @@ def test_replays_of_a_graph_and_other_streams(gpu):
     assert same(y, z)
 
 
-def test_calls_that_are_refused(gpu):
+@pytest.mark.parametrize("quick", [True, False])
+def test_calls_that_are_refused(gpu, monkeypatch, quick):
+    from paper_2511_04477_amd import binding
+    if not quick:
+        monkeypatch.setattr(binding, "_fast", None)
     x, codes, scales = torch.zeros((4, 64), dtype=torch.float16, device="cuda"), gpu.new_i8_codes(4, 64), torch.zeros(4, device="cuda")
     w, ws, y = gpu.new_i8_codes(6, 64), torch.zeros(6, device="cuda"), torch.zeros((4, 6), device="cuda")
     gain = x[0].clone()
@@ -531,3 +535,48 @@ def test_calls_that_are_refused(gpu):
         with pytest.raises(gpu.SpqtError):
             call()
             print("not refused:", i)
+
+
+def test_the_extension_module_gives_the_same(gpu, monkeypatch):
+    """Calls through _fastcall and through the Python code: the same bits, and the module takes the plain ones itself, slices and all."""
+    from paper_2511_04477_amd import binding
+    fast, left = binding._fast, []
+    assert fast is not None
+
+    class Watched:
+        def __getattr__(self, name):
+            def go(*a):
+                rc = getattr(fast, name)(*a)
+                left.extend([name] if rc is None else [])
+                return rc
+            return go
+
+    x = torch.randn((9, 700), generator=torch.Generator().manual_seed(1)).half().cuda()
+    w, weight_scales = codes_like(50, 690, 2), torch.rand(50, device="cuda")
+
+    def calls():
+        codes, scales, back = gpu.new_i8_codes(9, 690), torch.zeros(9, device="cuda"), torch.zeros((9, 690), dtype=torch.float16, device="cuda")
+        gpu.spqt_i8_quantize(x[:, 10:], codes, scales)
+        gpu.spqt_i8_read(codes, scales, back)
+        h_out, out = torch.zeros_like(back), torch.zeros_like(back)
+        gpu.spqt_i8_norm(x[:, 5:695], x[0, :690], block=x[:, 10:], block_gain=x[1, 3:693], gate=x[:, 1:691], residual=0.5, offset=1.0, h_out=h_out, out=out, codes=codes, scales=scales)
+        one = torch.zeros_like(back)
+        gpu.spqt_i8_norm(x[:, 5:695], x[0, :690], block=x[:, 10:], gate=x[3, :690], h_out=h_out, out=one)
+        found = [codes, scales, back, h_out, out, one]
+        for dtype in (torch.float16, torch.bfloat16, torch.float32):
+            for gated in (False, True):
+                y = torch.zeros((9, 60), dtype=dtype, device="cuda")[:, : 25 if gated else 50]
+                gpu.spqt_i8_gemm(codes, scales, w, weight_scales, y, bias=weight_scales, gated=gated, workspace=gpu.new_i8_workspace(9, 50, 690) if gated else None)
+                found.append(y)
+        return [t.clone() for t in found]
+
+    monkeypatch.setattr(binding, "_fast", None)
+    want = calls()
+    monkeypatch.setattr(binding, "_fast", Watched())
+    assert all(same(a, b) for a, b in zip(calls(), want)) and not left
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(side):
+        again = calls()
+    side.synchronize()
+    assert all(same(a, b) for a, b in zip(again, want)) and not left

@@ -114,7 +114,7 @@ def test_binding_refuses_what_is_not_on_the_gpu():
             call()
 
 
-def test_codes_that_the_binding_makes_begin_at_multiples_of_16_bytes():
-    for rows, K in ((1, 1), (3, 16), (5, 17), (4, 4096), (2, 5003), (2, 8192)):
+def test_codes_that_the_binding_makes_begin_at_multiples_of_128_bytes():
+    for rows, K in ((2, 1), (3, 16), (5, 17), (4, 4096), (2, 5003), (2, 8192)):
         c = spqt.new_i8_codes(rows, K, device="cpu")
-        assert tuple(c.shape) == (rows, K) and c.stride(1) == 1 and c.stride(0) % 16 == 0 and c.stride(0) >= K and c.stride(0) % 4096 != 0
+        assert tuple(c.shape) == (rows, K) and c.stride(1) == 1 and c.stride(0) % 128 == 0 and c.stride(0) >= K
