@@ -1,4 +1,4 @@
-// The product in 8-bit integers, sixteen rows at a time: each weight goes from memory to the matrix instruction of one wavefront.
+// The product in 8-bit integers, few rows or little of everything: each weight goes from memory to the matrix instruction of one wavefront.
 //
 // With the weights as its first operand v_mfma_i32_16x16x64_i8 gives a lane four channels of one row. The wavefronts of a workgroup take K in turn, 128 bytes each time, and add their
 // sums up in shared memory: whole numbers, whose order does not matter.
@@ -15,29 +15,35 @@ using namespace spqt::i8;
 
 constexpr int kChunk = 128;
 
-// W wavefronts, 16 C channels (gated: half of them the gate's, half of them those of the up projection), D chunks of a wavefront on their way together.
-template <int W, int C, int D, bool GATED>
+// W wavefronts, 16 R rows, 16 C channels (gated: half of them the gate's, half of them those of the up projection), D chunks of a wavefront on their way together.
+template <int W, int R, int C, int D, bool GATED>
 __global__ __launch_bounds__(W * 64) void spqt_i8_few_kernel(Product p) {
     constexpr int kMade = GATED ? C / 2 : C;                      // sixteens of outputs
-    __shared__ i32x4 sums[W][C][64];
+    __shared__ i32x4 sums[W][C * R][64];
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, line = lane & 15, quarter = lane >> 4;
-    const int n0 = blockIdx.x * (16 * kMade), row0 = blockIdx.y * 16;
-    const int row = row0 + line < p.rows ? row0 + line : p.rows - 1;
-    const int8_t *a = p.codes + row * p.codes_row, *w[C];
+    const int n0 = blockIdx.x * (16 * kMade), row0 = blockIdx.y * (16 * R);
+    const int8_t *a[R], *w[C];
+#pragma unroll
+    for (int r = 0; r < R; ++r) {
+        const int row = row0 + r * 16 + line;
+        a[r] = p.codes + (row < p.rows ? row : p.rows - 1) * p.codes_row;
+    }
 #pragma unroll
     for (int c = 0; c < C; ++c) {
         int n = n0 + c % kMade * 16 + line;
         n = (n < p.outputs ? n : p.outputs - 1) + c / kMade * p.outputs;
         w[c] = p.weights + n * p.weights_row;
     }
-    i32x4 acc[C];
+    i32x4 acc[C][R];
 #pragma unroll
-    for (int c = 0; c < C; ++c) acc[c] = i32x4{0, 0, 0, 0};
+    for (int c = 0; c < C; ++c)
+#pragma unroll
+        for (int r = 0; r < R; ++r) acc[c][r] = i32x4{0, 0, 0, 0};
     const int whole = p.K / kChunk, chunks = (p.K + kChunk - 1) / kChunk;
     int at = wave;
     auto span = [&](auto deep) {
         constexpr int N = decltype(deep)::value;
-        i32x4 x[N][2], v[N][2][C];
+        i32x4 x[N][2][R], v[N][2][C];
 #pragma unroll
         for (int d = 0; d < N; ++d)
 #pragma unroll
@@ -45,7 +51,8 @@ __global__ __launch_bounds__(W * 64) void spqt_i8_few_kernel(Product p) {
                 const int k = (at + d * W) * kChunk + i * 64 + quarter * 16;
 #pragma unroll
                 for (int c = 0; c < C; ++c) v[d][i][c] = *reinterpret_cast<const i32x4 *>(w[c] + k);
-                x[d][i] = *reinterpret_cast<const i32x4 *>(a + k);
+#pragma unroll
+                for (int r = 0; r < R; ++r) x[d][i][r] = *reinterpret_cast<const i32x4 *>(a[r] + k);
             }
         __builtin_amdgcn_sched_barrier(0);                        // all is asked for before any of it is used
 #pragma unroll
@@ -53,7 +60,9 @@ __global__ __launch_bounds__(W * 64) void spqt_i8_few_kernel(Product p) {
 #pragma unroll
             for (int i = 0; i < 2; ++i)
 #pragma unroll
-                for (int c = 0; c < C; ++c) acc[c] = __builtin_amdgcn_mfma_i32_16x16x64_i8(v[d][i][c], x[d][i], acc[c], 0, 0, 0);
+                for (int c = 0; c < C; ++c)
+#pragma unroll
+                    for (int r = 0; r < R; ++r) acc[c][r] = __builtin_amdgcn_mfma_i32_16x16x64_i8(v[d][i][c], x[d][i][r], acc[c][r], 0, 0, 0);
         at += N * W;
     };
     while (at + (D - 1) * W < whole) span(std::integral_constant<int, D>());
@@ -62,27 +71,34 @@ __global__ __launch_bounds__(W * 64) void spqt_i8_few_kernel(Product p) {
 #pragma unroll
         for (int i = 0; i < 2; ++i) {
             const int k = whole * kChunk + i * 64 + quarter * 16, from = k < p.K ? k : 0;       // (behind the row's end nothing is read)
-            const i32x4 x = masked(*reinterpret_cast<const i32x4 *>(a + from), k, p.K);
 #pragma unroll
-            for (int c = 0; c < C; ++c) acc[c] = __builtin_amdgcn_mfma_i32_16x16x64_i8(*reinterpret_cast<const i32x4 *>(w[c] + from), x, acc[c], 0, 0, 0);
+            for (int r = 0; r < R; ++r) {
+                const i32x4 x = masked(*reinterpret_cast<const i32x4 *>(a[r] + from), k, p.K);
+#pragma unroll
+                for (int c = 0; c < C; ++c) acc[c][r] = __builtin_amdgcn_mfma_i32_16x16x64_i8(*reinterpret_cast<const i32x4 *>(w[c] + from), x, acc[c][r], 0, 0, 0);
+            }
         }
     }
 #pragma unroll
-    for (int c = 0; c < C; ++c) sums[wave][c][lane] = acc[c];
+    for (int c = 0; c < C; ++c)
+#pragma unroll
+        for (int r = 0; r < R; ++r) sums[wave][c * R + r][lane] = acc[c][r];
     __syncthreads();
-    if (wave >= kMade || row0 + line >= p.rows) return;
-    // a wavefront finishes sixteen outputs of a row
+    // a wavefront finishes sixteen outputs of sixteen rows
+    static_assert(kMade * R <= W);
+    const int row = row0 + wave % R * 16 + line, made = wave / R;
+    if (made >= kMade || row >= p.rows) return;
     auto total = [&](int c) {
         i32x4 t = sums[0][c][lane];
 #pragma unroll
         for (int i = 1; i < W; ++i) t += sums[i][c][lane];
         return t;
     };
-    const i32x4 first = total(wave), second = total(GATED ? wave + kMade : wave);
+    const i32x4 first = total(wave), second = total(GATED ? wave + kMade * R : wave);
     const float scale = p.scales[row];
 #pragma unroll
     for (int e = 0; e < 4; ++e) {
-        const int n = n0 + wave * 16 + 4 * quarter + e;
+        const int n = n0 + made * 16 + 4 * quarter + e;
         if (n >= p.outputs) break;
         float v = scaled(p, first[e], scale, n);
         if (GATED) v = gated_by(v, scaled(p, second[e], scale, n + p.outputs));
@@ -90,7 +106,7 @@ __global__ __launch_bounds__(W * 64) void spqt_i8_few_kernel(Product p) {
     }
 }
 
-template <int W, int C, int D, bool GATED>
+template <int W, int R, int C, int D, bool GATED>
 void launch(const Product &p, hipStream_t stream) {
     const int made = 16 * (GATED ? C / 2 : C), most = 65535 * 16;                               // rows of a grid
     for (int64_t first = 0; first < p.rows; first += most) {
@@ -99,7 +115,7 @@ void launch(const Product &p, hipStream_t stream) {
         part.codes += first * p.codes_row;
         part.scales += first;
         part.y = (uint8_t *)p.y + first * p.y_row * (p.y_type == SPQT_I8_FP32 ? 4 : 2);
-        hipLaunchKernelGGL((spqt_i8_few_kernel<W, C, D, GATED>), dim3((p.outputs + made - 1) / made, (part.rows + 15) / 16), dim3(W * 64), 0, stream, part);
+        hipLaunchKernelGGL((spqt_i8_few_kernel<W, R, C, D, GATED>), dim3((p.outputs + made - 1) / made, (part.rows + 16 * R - 1) / (16 * R)), dim3(W * 64), 0, stream, part);
     }
 }
 
@@ -108,14 +124,24 @@ void launch(const Product &p, hipStream_t stream) {
 namespace spqt {
 namespace i8 {
 
-// Sixteen channels a workgroup, thirty-two where the codes are so many that reading them for every sixteen channels counts, and there are workgroups enough all the same: rows x channels x K,
-// us of 16 / 32 channels: 16 x 8192 x 28672 65.3 / 51.0, 4 x 8192 x 28672 50.0 / 47.8, 16 x 57344 x 8192 with the gate 105 / 96; the other way round 1 x 28672 x 4096 25.7 / 27.4,
+// Of more than sixteen rows, in us: an instruction reads 16 rows, each a line of its own, which takes a CU as many cycles: 35 KB a us, of codes and weights alike; not before the weights are
+// read, and 3 for the launch. Measured / this: 64 x 4096 x 4096 12.7 / 12.4, 128 x 4096 x 4096 21.7 / 21.7, 32 x 12288 x 4096 21.2 / 19.9, 300 x 520 x 2000 6.9 / 7.6.
+double few_us(const Product &p, bool gated) {
+    const int R = p.rows <= 32 ? 2 : 4;
+    const int64_t groups = (int64_t)((p.outputs + 15) / 16) * ((p.rows + 16 * R - 1) / (16 * R));
+    const double turns = (double)((groups + 255) / 256), read = turns * (16 * R + (gated ? 32 : 16)) * p.K / 35e3, weights = p.N * (double)p.K / 4.7e6;
+    return 3.0 + (read > weights ? read : weights);
+}
+
+// Sixteen channels a workgroup, thirty-two where sixteen rows' codes are so many that reading them for every sixteen channels counts, and there are workgroups enough all the same: rows x
+// channels x K, us of 16 / 32 channels: 16 x 8192 x 28672 65.3 / 51.0, 4 x 8192 x 28672 50.0 / 47.8, 16 x 57344 x 8192 with the gate 105 / 96; the other way round 1 x 28672 x 4096 25.7 / 27.4,
 // 16 x 4096 x 14336 (few workgroups) 19.7 / 24.1, 1 x 22016 x 4096 22.6 / 27.4.
 void launch_few(const Product &p, bool gated, hipStream_t stream) {
-    const int64_t rows = p.rows < 16 ? p.rows : 16;
-    const bool wide = rows * p.K >= 112 << 10 && p.outputs >= 256 * 32;
-    if (gated) wide ? launch<8, 4, 2, true>(p, stream) : launch<8, 2, 4, true>(p, stream);
-    else wide ? launch<8, 2, 2, false>(p, stream) : launch<8, 1, 4, false>(p, stream);
+    if (p.rows > 32) return gated ? launch<8, 4, 2, 1, true>(p, stream) : launch<8, 4, 1, 1, false>(p, stream);
+    if (p.rows > 16) return gated ? launch<8, 2, 2, 2, true>(p, stream) : launch<8, 2, 1, 2, false>(p, stream);
+    const bool wide = (int64_t)p.rows * p.K >= 112 << 10 && p.outputs >= 256 * 32;
+    if (gated) wide ? launch<8, 1, 4, 2, true>(p, stream) : launch<8, 1, 2, 4, true>(p, stream);
+    else wide ? launch<8, 1, 2, 2, false>(p, stream) : launch<8, 1, 1, 4, false>(p, stream);
 }
 
 }  // namespace i8

@@ -5,7 +5,7 @@ using namespace spqt;
 using namespace spqt::i8;
 
 namespace {
-constexpr int kFewRows = 16;         // that go through i8_few.hip; more than these where strides are too wide for tiles
+constexpr int kFewRows = 16;         // that always go through i8_few.hip
 }
 
 extern "C" int spqt_i8_workspace_bytes(int64_t rows, int64_t N, int64_t K, size_t *out_bytes) {
@@ -42,7 +42,7 @@ extern "C" int spqt_i8_gemm(const spqt_i8_product *c, void *workspace, size_t wo
                        (int)c->rows, (int)c->N, (int)c->K, (int)outputs, c->y_type};
     if (p.rows > kFewRows) {
         const Plan plan = plan_tiles(p, c->gated != 0, workspace && need > kWorkspaceHead ? need - kWorkspaceHead : 0);
-        if (plan.shape >= 0) {
+        if (plan.shape >= 0 && plan.us < few_us(p, c->gated != 0)) {
             launch_tiles_of(plan, p, c->gated != 0, workspace, (hipStream_t)stream);
             return launched();
         }

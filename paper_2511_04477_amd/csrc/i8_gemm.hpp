@@ -44,9 +44,13 @@ __device__ __forceinline__ i32x4 masked(i32x4 x, int k, int K) {
 
 void launch_few(const Product &p, bool gated, hipStream_t stream);
 
-// A shape of tiles (i8_tiles.hip has them) and the parts that K is divided into.
+// What launch_few is expected to take.
+double few_us(const Product &p, bool gated);
+
+// A shape of tiles (i8_tiles.hip has them) and the parts that K is divided into, and what that is expected to take.
 struct Plan {
     int shape, parts;
+    double us;
 };
 Plan plan_tiles(const Product &p, bool gated, size_t room);       // room: bytes for the parts' sums; shape -1: none can
 void launch_tiles_of(const Plan &plan, const Product &p, bool gated, void *workspace, hipStream_t stream);

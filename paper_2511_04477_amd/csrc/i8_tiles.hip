@@ -34,10 +34,9 @@ namespace i8 {
 Plan plan_tiles(const Product &p, bool gated, size_t room) {
     // places within a tile, with the gate's and the up projection's channels in one, are 32 bits
     const int64_t widest = (int64_t)1 << 23;
-    Plan best = {-1, 1};
+    Plan best = {-1, 1, 0.0};
     if (p.codes_row >= widest || p.weights_row >= widest || p.y_row >= widest || (gated && (p.N + 256) * p.weights_row >= (int64_t)1 << 32)) return best;
     const int steps = (p.K + kStep - 1) / kStep;
-    double least = 0.0;
     for (int i = 0; i < kCount; ++i) {
         const Cost &s = kShapes[i];
         const int64_t tiles = tiles_of(s, p, gated);
@@ -48,16 +47,14 @@ Plan plan_tiles(const Product &p, bool gated, size_t room) {
             const double each = (steps + parts - 1) / parts, weights = p.N * (double)p.K;
             const bool streams = p.rows <= s.rows && weights > 32e6;
             auto round = [&](int64_t n) {
-                const double full = s.step + (s.step_full - s.step) * (double)n / kGroups, least = streams ? s.channels * (128 / 33e3) : 0.0;
-                return n == 0 ? 0.0 : each * (full > least ? full : least) + s.fixed;
+                const double full = s.step + (s.step_full - s.step) * (double)n / kGroups, slowest = streams ? s.channels * (128 / 33e3) : 0.0;
+                return n == 0 ? 0.0 : each * (full > slowest ? full : slowest) + s.fixed;
             };
             double us = (double)(units / kGroups) * round(kGroups) + round(units % kGroups);
             if (streams && us < weights / 4.7e6) us = weights / 4.7e6;
             if (parts > 1) us += 4.5 + (double)sums / 3e6;
-            if (best.shape < 0 || us < least) {
-                least = us;
-                best = {i, parts};
-            }
+            us += 5.0;                               // the launch, and a first tile's first operands
+            if (best.shape < 0 || us < best.us) best = {i, parts, us};
         }
     }
     return best;

@@ -291,7 +291,7 @@ def test_products(gpu, rows, N, K, dtype):
 
 
 # Sizes that different tiles and numbers of parts are taken for, with edges in every dimension.
-LARGE = [(771, 14331, 4101), (1021, 8183, 28672), (1500, 5118, 5131), (16, 8191, 28672), (7, 16390, 17000), (509, 10222, 8192), (1019, 4090, 4109), (250, 4094, 14336), (40, 8190, 28672), (127, 2050, 20000),
+LARGE = [(771, 14331, 4101), (1021, 8183, 28672), (1500, 5118, 5131), (16, 8191, 28672), (7, 16390, 17000), (26, 1682, 7051), (61, 4090, 4100), (300, 521, 2000), (509, 10222, 8192), (1019, 4090, 4109), (250, 4094, 14336), (40, 8190, 28672), (127, 2050, 20000),
          (4001, 3070, 1000), (8000, 598, 400), (2047, 2050, 130), (65, 128, 131071)]
 
 
