@@ -129,7 +129,7 @@ namespace i8 {
 double few_us(const Product &p, bool gated) {
     const int R = p.rows <= 32 ? 2 : 4;
     const int64_t groups = (int64_t)((p.outputs + 15) / 16) * ((p.rows + 16 * R - 1) / (16 * R));
-    const double turns = (double)((groups + 255) / 256), read = turns * (16 * R + (gated ? 32 : 16)) * p.K / 35e3, weights = p.N * (double)p.K / 4.7e6;
+    const double turns = (double)((groups + 255) / 256), read = turns * ((p.rows < 16 * R ? p.rows : 16 * R) + (gated ? 32 : 16)) * p.K / 35e3, weights = p.N * (double)p.K / 4.7e6;
     return 3.0 + (read > weights ? read : weights);
 }
 

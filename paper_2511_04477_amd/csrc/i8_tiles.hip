@@ -45,7 +45,7 @@ Plan plan_tiles(const Product &p, bool gated, size_t room) {
             const int64_t units = tiles * parts, sums = units * s.rows * s.channels * 4;
             if (parts > 1 && (size_t)sums > room) break;
             const double each = (steps + parts - 1) / parts, weights = p.N * (double)p.K;
-            const bool streams = p.rows <= s.rows && weights > 32e6;
+            const bool streams = p.rows <= s.rows && weights > 20e6;
             auto round = [&](int64_t n) {
                 const double full = s.step + (s.step_full - s.step) * (double)n / kGroups, slowest = streams ? s.channels * (128 / 33e3) : 0.0;
                 return n == 0 ? 0.0 : each * (full > slowest ? full : slowest) + s.fixed;

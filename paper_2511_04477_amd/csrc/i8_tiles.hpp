@@ -447,28 +447,23 @@ __global__ __launch_bounds__(WM * WN * 64, 1) void spqt_i8_tiles_kernel(Product 
     asm volatile("s_waitcnt vmcnt(0)" ::: "memory");              // no load may arrive after the workgroup has left its shared memory
 }
 
-// The parts' sums together, and what becomes of them: a wavefront takes 32 rows of what a wavefront of the other kernel had.
+// The parts' sums together, and what becomes of them: a workgroup takes 32 rows of what a wavefront of the other kernel had, each of its four wavefronts every fourth part.
 template <int TM, int TN, int WM, int WN, int NA, int NB, int YT, bool GATED>
-__global__ __launch_bounds__(64) void spqt_i8_join_kernel(Product p, Tiling t) {
+__global__ __launch_bounds__(256) void spqt_i8_join_kernel(Product p, Tiling t) {
     typedef Shape<TM, TN, WM, WN, NA, NB> S;
     __shared__ __attribute__((aligned(1024))) uint8_t stage[S::kLoadsB * 1024];
-    const int lane = threadIdx.x, line = lane & 31, half = lane >> 5;
+    __shared__ i32x4 sums[3][S::NI * 4][64];
+    const int lane = threadIdx.x & 63, own = threadIdx.x >> 6, line = lane & 31, half = lane >> 5;
     const int m = blockIdx.x % S::MI, wave = blockIdx.x / S::MI % S::kWaves, tile = blockIdx.x / (S::MI * S::kWaves);
-    if (blockIdx.x == 0 && lane == 0) *t.head = 1u;                // (a GEMV on this workspace is to yield NaN)
+    if (blockIdx.x == 0 && threadIdx.x == 0) *t.head = 1u;         // (a GEMV on this workspace is to yield NaN)
     const Unit u = unit_at(t, tile);
     const Finish<S, YT, GATED> finish(p, u.channel_tile * (GATED ? TN / 2 : TN) + wave % WN * (S::kChannels / (GATED ? 2 : 1)), line, half);
     const int first = u.row_tile * TM + wave / WN * S::kRows + m * 32;
     if (first >= p.rows) return;
-    typename Finish<S, YT, GATED>::Scales by;
-    if (finish.inside) finish.scales(by);
-    else finish.scales_at_edge(by);
-    const float scale = finish.scale_of_row(first);
     i32x16 acc[S::NI];
 #pragma unroll
     for (int n = 0; n < S::NI; ++n) acc[n] = i32x16{};
-#pragma unroll 4
-    for (int part = 0; part < t.parts; ++part) {
-        const i32x4 *from = t.sums + ((((size_t)part * t.tiles + tile) * S::kWaves + wave) * S::MI + m) * S::NI * 256 + lane;
+    auto add = [&](const i32x4 *from) {
 #pragma unroll
         for (int n = 0; n < S::NI; ++n)
 #pragma unroll
@@ -477,7 +472,22 @@ __global__ __launch_bounds__(64) void spqt_i8_join_kernel(Product p, Tiling t) {
 #pragma unroll
                 for (int e = 0; e < 4; ++e) acc[n][4 * q + e] += v[e];
             }
-    }
+    };
+#pragma unroll 2
+    for (int part = own; part < t.parts; part += 4) add(t.sums + ((((size_t)part * t.tiles + tile) * S::kWaves + wave) * S::MI + m) * S::NI * 256 + lane);
+    if (own > 0)
+#pragma unroll
+        for (int n = 0; n < S::NI; ++n)
+#pragma unroll
+            for (int q = 0; q < 4; ++q) sums[own - 1][n * 4 + q][lane] = i32x4{acc[n][4 * q], acc[n][4 * q + 1], acc[n][4 * q + 2], acc[n][4 * q + 3]};
+    __syncthreads();
+    if (own > 0) return;
+    typename Finish<S, YT, GATED>::Scales by;
+    if (finish.inside) finish.scales(by);
+    else finish.scales_at_edge(by);
+    const float scale = finish.scale_of_row(first);
+#pragma unroll
+    for (int i = 0; i < 3; ++i) add(&sums[i][0][lane]);
     finish.rows(acc, first, scale, by, stage, 1024, lane);
 }
 
@@ -487,7 +497,7 @@ void launch_tiles_as(const Product &p, const Tiling &t, hipStream_t stream) {
     const int grid = t.units < kGroups ? (t.units + 7) / 8 * 8 : kGroups;
     hipLaunchKernelGGL((spqt_i8_tiles_kernel<TM, TN, WM, WN, NA, NB, YT, GATED>), dim3(grid), dim3(S::kThreads), 0, stream, p, t);
     if (t.parts > 1)
-        hipLaunchKernelGGL((spqt_i8_join_kernel<TM, TN, WM, WN, NA, NB, YT, GATED>), dim3(t.tiles * S::kWaves * S::MI), dim3(64), 0, stream, p, t);
+        hipLaunchKernelGGL((spqt_i8_join_kernel<TM, TN, WM, WN, NA, NB, YT, GATED>), dim3(t.tiles * S::kWaves * S::MI), dim3(256), 0, stream, p, t);
 }
 
 // In `parts` parts of K, whose sums take parts * tiles * TM * TN * 4 bytes from 256 bytes behind the workspace's beginning on.
