@@ -25,18 +25,20 @@ int64_t tiles_of(const Cost &s, const Product &p, bool gated) {
 namespace spqt {
 namespace i8 {
 
-// The one that is expected to be done first: rounds of 256 workgroups, a tile's steps each; with parts, 4.5 us for the second launch and a us for every 3 MB of sums. Where one
-// tile has all rows and the weights are more than the caches keep, no sooner than 4.7 MB of weights a us, and 33 KB a us for a workgroup.
-// Rows x channels x K, us of 256 x 256 / 128 x 256 / 128 x 128 / 64 x 128 with the best number of parts each (the one taken is the least, or within 4 % of it):
+// The one that is expected to be done first: rounds of 256 workgroups, a tile's steps each; with parts, 3 us for the second launch and a us for every 3.5 MB of sums. Where one
+// tile has all rows and the weights are more than the caches keep, no sooner than 4.7 MB of weights a us, and 33 KB a us for a workgroup. Rows that begin within
+// a line take a quarter longer: each of their steps is in two lines (777 x 1111 x 5003 in rows of 5120 and 5008 bytes, one part: 20.0 and 24.6 us).
+// Rows x channels x K, us of 256 x 256 / 128 x 256 / 128 x 128 / 64 x 128 with the best number of parts each (the one taken is the least, or within 7 % of it):
 //   4001 x 4096 x 14336   188 / 210 / 268 / 343        1500 x 5120 x 5120   52.0 / 43.1 / 49.4 / 64.0      1024 x 4096 x 4096   38.2 / 28.5 / 24.2 / 31.1
-//   1024 x 8192 x 28672   211 (2 parts; one 287) / 211 / 272 / 385       250 x 4096 x 14336   43.2 (7) / 37.3 (7) / 35.0 (4; two 43.7) / 36.2 (2)
-//   512 x 4096 x 4096     30.6 (3) / 25.1 / 19.4 / 17.2                  40 x 8192 x 28672    - / - / - / 53.5 (4; three 53.6, two 64.9, one 102)
+//   1024 x 8192 x 28672   207 (2 parts; one 283) / 211 / 276 / 386       250 x 4096 x 14336    36.8 (10) / 33.2 (7) / 32.3 (4; two 42.5) / 35.5 (2)
+//   512 x 4096 x 4096     29.4 (3) / 25.3 / 19.3 / 17.1                  40 x 8192 x 28672    - / - / - / 50.4 (4; three 52.0, two 63.6, one 103)
 Plan plan_tiles(const Product &p, bool gated, size_t room) {
     // places within a tile, with the gate's and the up projection's channels in one, are 32 bits
     const int64_t widest = (int64_t)1 << 23;
     Plan best = {-1, 1, 0.0};
     if (p.codes_row >= widest || p.weights_row >= widest || p.y_row >= widest || (gated && (p.N + 256) * p.weights_row >= (int64_t)1 << 32)) return best;
     const int steps = (p.K + kStep - 1) / kStep;
+    const double longer = p.codes_row % kStep == 0 && p.weights_row % kStep == 0 ? 1.0 : 1.25;
     for (int i = 0; i < kCount; ++i) {
         const Cost &s = kShapes[i];
         const int64_t tiles = tiles_of(s, p, gated);
@@ -44,7 +46,7 @@ Plan plan_tiles(const Product &p, bool gated, size_t room) {
         for (int parts = 1; parts == 1 || (parts <= 16 && parts <= steps && tiles * parts <= kGroups); ++parts) {
             const int64_t units = tiles * parts, sums = units * s.rows * s.channels * 4;
             if (parts > 1 && (size_t)sums > room) break;
-            const double each = (steps + parts - 1) / parts, weights = p.N * (double)p.K;
+            const double each = (steps + parts - 1) / parts * longer, weights = p.N * (double)p.K;
             const bool streams = p.rows <= s.rows && weights > 20e6;
             auto round = [&](int64_t n) {
                 const double full = s.step + (s.step_full - s.step) * (double)n / kGroups, slowest = streams ? s.channels * (128 / 33e3) : 0.0;
@@ -52,7 +54,7 @@ Plan plan_tiles(const Product &p, bool gated, size_t room) {
             };
             double us = (double)(units / kGroups) * round(kGroups) + round(units % kGroups);
             if (streams && us < weights / 4.7e6) us = weights / 4.7e6;
-            if (parts > 1) us += 4.5 + (double)sums / 3e6;
+            if (parts > 1) us += 3.0 + (double)sums / 3.5e6;
             us += 5.0;                               // the launch, and a first tile's first operands
             if (best.shape < 0 || us < best.us) best = {i, parts, us};
         }
