@@ -453,13 +453,20 @@ __global__ __launch_bounds__(256) void spqt_i8_join_kernel(Product p, Tiling t) 
     typedef Shape<TM, TN, WM, WN, NA, NB> S;
     __shared__ __attribute__((aligned(1024))) uint8_t stage[S::kLoadsB * 1024];
     __shared__ i32x4 sums[3][S::NI * 4][64];
-    const int lane = threadIdx.x & 63, own = threadIdx.x >> 6, line = lane & 31, half = lane >> 5;
+    const int lane = threadIdx.x & 63, own = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), line = lane & 31, half = lane >> 5;
     const int m = blockIdx.x % S::MI, wave = blockIdx.x / S::MI % S::kWaves, tile = blockIdx.x / (S::MI * S::kWaves);
     if (blockIdx.x == 0 && threadIdx.x == 0) *t.head = 1u;         // (a GEMV on this workspace is to yield NaN)
     const Unit u = unit_at(t, tile);
     const Finish<S, YT, GATED> finish(p, u.channel_tile * (GATED ? TN / 2 : TN) + wave % WN * (S::kChannels / (GATED ? 2 : 1)), line, half);
     const int first = u.row_tile * TM + wave / WN * S::kRows + m * 32;
     if (first >= p.rows) return;
+    typename Finish<S, YT, GATED>::Scales by;                     // asked for beside the sums
+    float scale = 0.0f;
+    if (own == 0) {
+        if (finish.inside) finish.scales(by);
+        else finish.scales_at_edge(by);
+        scale = finish.scale_of_row(first);
+    }
     i32x16 acc[S::NI];
 #pragma unroll
     for (int n = 0; n < S::NI; ++n) acc[n] = i32x16{};
@@ -482,10 +489,6 @@ __global__ __launch_bounds__(256) void spqt_i8_join_kernel(Product p, Tiling t) 
             for (int q = 0; q < 4; ++q) sums[own - 1][n * 4 + q][lane] = i32x4{acc[n][4 * q], acc[n][4 * q + 1], acc[n][4 * q + 2], acc[n][4 * q + 3]};
     __syncthreads();
     if (own > 0) return;
-    typename Finish<S, YT, GATED>::Scales by;
-    if (finish.inside) finish.scales(by);
-    else finish.scales_at_edge(by);
-    const float scale = finish.scale_of_row(first);
 #pragma unroll
     for (int i = 0; i < 3; ++i) add(&sums[i][0][lane]);
     finish.rows(acc, first, scale, by, stage, 1024, lane);
