@@ -90,7 +90,8 @@ __device__ __forceinline__ uint32_t most_over_row(uint32_t v, uint32_t *shared, 
     return over_row<T>(v, [](uint32_t a, uint32_t b) { return a > b ? a : b; }, shared, slot);
 }
 
-// 1 / sqrt(mean x^2 + eps).  Squares of numbers from 2^64 on leave fp32: such a row is summed in units of 2^70, in which eps is nothing.
+// 1 / sqrt(mean x^2 + eps).  Squares of numbers from 2^64 on, and sums of 2^16 of them from 2^56 on, leave fp32: such a row is summed in units of 2^80, in which eps is nothing,
+// its largest number is from 2^-24 to 2^48.
 template <int T, int V>
 __device__ __forceinline__ float inverse_rms(const float (&x)[V][8], int K, float eps, uint32_t *shared, int slot) {
     float sum = 0.0f;
@@ -105,11 +106,11 @@ __device__ __forceinline__ float inverse_rms(const float (&x)[V][8], int K, floa
     for (int v = 0; v < V; ++v)
 #pragma unroll
         for (int e = 0; e < 8; ++e) {
-            const float y = x[v][e] * 0x1p-70f;
+            const float y = x[v][e] * 0x1p-80f;
             sum = __builtin_fmaf(y, y, sum);
         }
     sum = sum_over_row<T>(sum, shared, slot + 1);
-    return 0x1p-70f / __builtin_sqrtf(sum / (float)K);
+    return 0x1p-80f / __builtin_sqrtf(sum / (float)K);
 }
 
 // Codes of a row, from the largest magnitude of this thread's numbers: magnitudes order as their bits do, infinities and NaN above all numbers.

@@ -236,6 +236,23 @@ def test_norm_of_rows_that_are_no_ordinary_numbers(gpu, K):
     assert bool((codes[0] == 0).all()) and torch.isfinite(scales[keep]).all()
 
 
+@pytest.mark.parametrize("K", [7, 4096, 20000, 65536])
+def test_norm_of_the_largest_numbers(gpu, K):
+    dtype = torch.bfloat16
+    h = torch.full((3, K), torch.finfo(dtype).max, dtype=dtype)
+    h[0, 1::2] *= -1
+    h[1] *= 2.0**-71                                 # whose squares are numbers of fp32 and whose sum is one or not, by K
+    h[2, K // 2 :] = 1.0
+    gain = torch.randn(K, generator=torch.Generator().manual_seed(K)).to(dtype)
+    out, codes, scales = torch.zeros((3, K), dtype=dtype, device="cuda"), gpu.new_i8_codes(3, K), torch.zeros(3, device="cuda")
+    gpu.spqt_i8_norm(h.cuda(), gain.cuda(), out=out, codes=codes, scales=scales)
+    _, x, _, far = oracle.norm(h.double(), gain.double())
+    far = far + x.abs() * 2.0**-21                   # 1 / 2^128 is a subnormal number of 22 bits
+    assert rounded_to(out, x, far + 1e-38, dtype)
+    top = x.abs().max(dim=1)[0]
+    assert bool(((scales.double().cpu() * 127 - top).abs() <= far.max(dim=1)[0] + 2 * oracle.U * top).all())
+
+
 @pytest.mark.parametrize("rows,K", [(5001, 24), (3001, 1000), (1500, 4096)])
 def test_norm_of_many_rows(gpu, rows, K):
     given, more = norm_inputs(rows, K, torch.float16, dict(block_gain=True, gate="channel"))
