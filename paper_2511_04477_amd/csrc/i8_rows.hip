@@ -294,8 +294,8 @@ __global__ __launch_bounds__(256) void spqt_i8_read_kernel(Read a) {
 
 // f(threads, eights a thread, BF16) for rows of K numbers: a norm's threads hold two eights up to where a workgroup ends, since they have five tensors to ask for. Codes of 4001 rows of 14336
 // with 512 x 4 / 1024 x 2 / 256 x 8 34.4 / 40.3 / 35.9 us, of 8192 with 256 x 4 / 512 x 2 / 1024 x 1 20.5 / 21.2 / 24.2; norms of 4001 rows of 4096 with 256 x 2 / 512 x 1 27.8 / 34.5.
-template <class F>
-void dispatch(int64_t K, int type, bool norm, F f) {
+template <bool NORM, class F>
+void dispatch(int64_t K, int type, F f) {
     auto typed = [&](auto t, auto v) {
         if (type == SPQT_I8_BF16) f(t, v, std::true_type());
         else f(t, v, std::false_type());
@@ -303,13 +303,9 @@ void dispatch(int64_t K, int type, bool norm, F f) {
     if (K <= 512) typed(std::integral_constant<int, 64>(), std::integral_constant<int, 1>());
     else if (K <= 2048) typed(std::integral_constant<int, 256>(), std::integral_constant<int, 1>());
     else if (K <= 4096) typed(std::integral_constant<int, 256>(), std::integral_constant<int, 2>());
-    else if (K <= 8192) {
-        if (norm) typed(std::integral_constant<int, 512>(), std::integral_constant<int, 2>());
-        else typed(std::integral_constant<int, 256>(), std::integral_constant<int, 4>());
-    } else if (K <= 16384) {
-        if (norm) typed(std::integral_constant<int, 1024>(), std::integral_constant<int, 2>());
-        else typed(std::integral_constant<int, 512>(), std::integral_constant<int, 4>());
-    } else if (K <= 32768) typed(std::integral_constant<int, 1024>(), std::integral_constant<int, 4>());
+    else if (K <= 8192) typed(std::integral_constant<int, NORM ? 512 : 256>(), std::integral_constant<int, NORM ? 2 : 4>());
+    else if (K <= 16384) typed(std::integral_constant<int, NORM ? 1024 : 512>(), std::integral_constant<int, NORM ? 2 : 4>());
+    else if (K <= 32768) typed(std::integral_constant<int, 1024>(), std::integral_constant<int, 4>());
     else typed(std::integral_constant<int, 1024>(), std::integral_constant<int, 8>());
 }
 template <class S>
@@ -328,7 +324,7 @@ extern "C" int spqt_i8_quantize(const void *x, int64_t x_row, int64_t rows, int6
     if (rc == SPQT_OK) rc = check_scales(scales);
     if (rc != SPQT_OK) return rc;
     const Quantize a = {(const uint16_t *)x, codes, scales, x_row, codes_row, (int)rows, (int)K};
-    dispatch(K, type, false, [&](auto t, auto v, auto bf16) {
+    dispatch<false>(K, type, [&](auto t, auto v, auto bf16) {
         typedef Shape<decltype(t)::value> S;
         hipLaunchKernelGGL((spqt_i8_quantize_kernel<decltype(t)::value, decltype(v)::value, decltype(bf16)::value>), grid_of<S>(rows), dim3(S::kThreads), 0,
                            (hipStream_t)stream, a);
@@ -372,7 +368,7 @@ extern "C" int spqt_i8_norm(const spqt_i8_norm_call *c, void *stream) {
     const Norm a = {(const uint16_t *)c->h, (const uint16_t *)c->block, (const uint16_t *)c->block_gain, (const uint16_t *)c->gate, (const uint16_t *)c->gain,
                     (uint16_t *)c->h_out, (uint16_t *)c->out, c->codes, c->scales, c->h_row, c->block_row, c->gate_row, c->h_out_row, c->out_row, c->codes_row,
                     (int)rows, (int)K, c->residual, c->eps, c->offset};
-    dispatch(K, c->type, true, [&](auto t, auto v, auto bf16) {
+    dispatch<true>(K, c->type, [&](auto t, auto v, auto bf16) {
         typedef Shape<decltype(t)::value> S;
         hipLaunchKernelGGL((spqt_i8_norm_kernel<decltype(t)::value, decltype(v)::value, decltype(bf16)::value>), grid_of<S>(rows), dim3(S::kThreads), 0,
                            (hipStream_t)stream, a);
