@@ -17,10 +17,20 @@ __device__ __forceinline__ int place(int v) {
     return ((int)(threadIdx.x % T) + v * T) * 8;
 }
 
+// Rows of whole 512s (WHOLE) end between two wavefronts' eights: whether a wavefront has its v-th ones is one question for all its lanes, and nothing needs to be moved or
+// masked. With that question asked lane by lane a norm of 4001 rows of 8192 took 57 us.
+template <int T, bool WHOLE>
+__device__ __forceinline__ bool has(int v, int K) {
+    if (!WHOLE) return place<T>(v) < K;
+    return (__builtin_amdgcn_readfirstlane((int)(threadIdx.x % T) / 64) * 64 + v * T) * 8 < K;
+}
+
 // Eight 16-bit numbers from element k on, as they lie. At a row's end the row's last eight, which settle() moves to their places, with 0 from element K on; rows of less than eight
 // are put together from single ones.
-template <int T>
-__device__ __forceinline__ u32x4 fetch(const uint16_t *row, int k, int K) {
+template <int T, bool WHOLE>
+__device__ __forceinline__ u32x4 fetch(const uint16_t *row, int v, int K) {
+    const int k = place<T>(v);
+    if (WHOLE) return *reinterpret_cast<const u32x4_at2 *>(row + (has<T, WHOLE>(v, K) ? k : k % 512));
     if (T == 64 && K < 8) {
         u32x4 w = {0u, 0u, 0u, 0u};
 #pragma unroll
@@ -30,8 +40,10 @@ __device__ __forceinline__ u32x4 fetch(const uint16_t *row, int k, int K) {
     }
     return *reinterpret_cast<const u32x4_at2 *>(row + (k + 8 <= K ? k : K - 8));
 }
-template <int T>
-__device__ __forceinline__ u32x4 settle(u32x4 w, int k, int K) {
+template <int T, bool WHOLE>
+__device__ __forceinline__ u32x4 settle(u32x4 w, int v, int K) {
+    if (WHOLE) return has<T, WHOLE>(v, K) ? w : u32x4{0u, 0u, 0u, 0u};
+    const int k = place<T>(v);
     if (k + 8 <= K || (T == 64 && K < 8)) return w;
     const int by = k + 8 - K < 8 ? k + 8 - K : 8;                 // elements that are not this thread's, in front
     const uint32_t odd = by & 1;
@@ -49,10 +61,10 @@ __device__ __forceinline__ void widen8(u32x4 w, float (&x)[8]) {
 #pragma unroll
     for (int e = 0; e < 8; ++e) x[e] = widen<BF16>(w[e / 2] >> (16 * (e % 2)) & 0xFFFFu);
 }
-template <bool BF16>
+template <bool BF16, bool WHOLE>
 __device__ __forceinline__ void put(uint16_t *row, int k, int K, const float (&x)[8]) {
     const u32x4 w = {narrow2<BF16>(x[0], x[1]), narrow2<BF16>(x[2], x[3]), narrow2<BF16>(x[4], x[5]), narrow2<BF16>(x[6], x[7])};
-    if (k + 8 <= K) {
+    if (WHOLE || k + 8 <= K) {
         *reinterpret_cast<u32x4_at2 *>(row + k) = w;
         return;
     }
@@ -90,17 +102,17 @@ __device__ __forceinline__ uint32_t most_over_row(uint32_t v, uint32_t *shared, 
     return over_row<T>(v, [](uint32_t a, uint32_t b) { return a > b ? a : b; }, shared, slot);
 }
 
-// 1 / sqrt(mean x^2 + eps).  Squares of numbers from 2^64 on, and sums of 2^16 of them from 2^56 on, leave fp32: such a row is summed in units of 2^80, in which eps is nothing,
+// 1 / sqrt(mean x^2 + eps), within 3.5 halves of fp32's steps behind the sum: 1 / K and its product, the sum with eps, these by the root's half, and two of the hardware's reciprocal root.  Squares of numbers from 2^64 on, and sums of 2^16 of them from 2^56 on, leave fp32: such a row is summed in units of 2^80, in which eps is nothing,
 // its largest number is from 2^-24 to 2^48.
 template <int T, int V>
-__device__ __forceinline__ float inverse_rms(const float (&x)[V][8], int K, float eps, uint32_t *shared, int slot) {
+__device__ __forceinline__ float inverse_rms(const float (&x)[V][8], float per, float eps, uint32_t *shared, int slot) {
     float sum = 0.0f;
 #pragma unroll
     for (int v = 0; v < V; ++v)
 #pragma unroll
         for (int e = 0; e < 8; ++e) sum = __builtin_fmaf(x[v][e], x[v][e], sum);
     sum = sum_over_row<T>(sum, shared, slot);
-    if (sum < __builtin_inff() || sum != sum) return 1.0f / __builtin_sqrtf(sum / (float)K + eps);
+    if (sum < __builtin_inff() || sum != sum) return __builtin_amdgcn_rsqf(sum * per + eps);
     sum = 0.0f;
 #pragma unroll
     for (int v = 0; v < V; ++v)
@@ -110,11 +122,11 @@ __device__ __forceinline__ float inverse_rms(const float (&x)[V][8], int K, floa
             sum = __builtin_fmaf(y, y, sum);
         }
     sum = sum_over_row<T>(sum, shared, slot + 1);
-    return 0x1p-80f / __builtin_sqrtf(sum / (float)K);
+    return 0x1p-80f * __builtin_amdgcn_rsqf(sum * per);
 }
 
 // Codes of a row, from the largest magnitude of this thread's numbers: magnitudes order as their bits do, infinities and NaN above all numbers.
-template <int T, int V>
+template <int T, int V, bool WHOLE>
 __device__ __forceinline__ void quantize_row(const float (&x)[V][8], int K, int8_t *codes, float *scale, uint32_t *shared, int slot) {
 #pragma clang fp contract(off)
     uint32_t most = 0u;
@@ -131,8 +143,8 @@ __device__ __forceinline__ void quantize_row(const float (&x)[V][8], int K, int8
     if (threadIdx.x % T == 0) *scale = number ? top / 127.0f : __builtin_nanf("");
 #pragma unroll
     for (int v = 0; v < V; ++v) {
+        if (!has<T, WHOLE>(v, K)) continue;
         const int k = place<T>(v);
-        if (k >= K) continue;
         u32x2 w;
 #pragma unroll
         for (int i = 0; i < 2; ++i) {
@@ -143,7 +155,7 @@ __device__ __forceinline__ void quantize_row(const float (&x)[V][8], int K, int8
             w[i] = __builtin_amdgcn_perm(c[1], c[0], 0x0C0C0400u) | __builtin_amdgcn_perm(c[3], c[2], 0x04000C0Cu);
             if (!number) w[i] = 0u;
         }
-        if (k + 8 <= K) {
+        if (WHOLE || k + 8 <= K) {
             *reinterpret_cast<u32x2 *>(codes + k) = w;
         } else {
 #pragma unroll
@@ -163,7 +175,7 @@ struct Quantize {
 
 // A row is in the registers of its threads: read once, its largest magnitude found, its codes written.
 // What bounds it: 2 bytes in and 1 out a number: 4001 rows of 14336 34.4 us = 5.0 TB/s, of 8192 20.5 = 4.8 (a copy: 4.83); 40 of 28672 4.4 us; one of 4096 2.2.
-template <int T, int V, bool BF16>
+template <int T, int V, bool BF16, bool WHOLE>
 __global__ __launch_bounds__(Shape<T>::kThreads) void spqt_i8_quantize_kernel(Quantize a) {
     typedef Shape<T> S;
     __shared__ uint32_t shared[2 * S::kWaves];
@@ -172,11 +184,11 @@ __global__ __launch_bounds__(Shape<T>::kThreads) void spqt_i8_quantize_kernel(Qu
         float x[V][8];
         u32x4 w[V];
 #pragma unroll
-        for (int v = 0; v < V; ++v) w[v] = fetch<T>(a.x + row * a.x_row, place<T>(v), a.K);
+        for (int v = 0; v < V; ++v) w[v] = fetch<T, WHOLE>(a.x + row * a.x_row, v, a.K);
         __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
-        for (int v = 0; v < V; ++v) widen8<BF16>(settle<T>(w[v], place<T>(v), a.K), x[v]);
-        quantize_row<T, V>(x, a.K, a.codes + row * a.codes_row, a.scales + row, shared, slot);
+        for (int v = 0; v < V; ++v) widen8<BF16>(settle<T, WHOLE>(w[v], v, a.K), x[v]);
+        quantize_row<T, V, WHOLE>(x, a.K, a.codes + row * a.codes_row, a.scales + row, shared, slot);
         slot ^= 1;
     }
 }
@@ -188,13 +200,13 @@ struct Norm {
     float *scales;
     int64_t h_row, block_row, gate_row, h_out_row, out_row, codes_row;
     int rows, K;
-    float residual, eps, offset;
+    float residual, eps, offset, per;              // per: 1 / K
 };
 
 // One pass: what a block has made, the stream and the vectors are read once, and the sum stays in registers, in 32 bits, from the join over both norms to the codes.
 // What bounds it: 4 bytes in and 3 out a number, and three sums over a row that follow each other: 4001 rows of 8192 with both norms and a gate 56 us = 4.1 TB/s; with loads where they are
 // used and sums over lanes by way of shared memory 82. One row of 4096 4.0 us: loads, three sums, stores.
-template <int T, int V, bool BF16>
+template <int T, int V, bool BF16, bool WHOLE>
 __global__ __launch_bounds__(Shape<T>::kThreads) void spqt_i8_norm_kernel(Norm a) {
     typedef Shape<T> S;
     constexpr bool kTogether = V <= 2;
@@ -205,7 +217,7 @@ __global__ __launch_bounds__(Shape<T>::kThreads) void spqt_i8_norm_kernel(Norm a
         const uint16_t *const h_at = a.h + row * a.h_row, *const gate_at = a.gate + row * a.gate_row;
         auto fetch_row = [&](u32x4 (&w)[V], const uint16_t *from) {
 #pragma unroll
-            for (int v = 0; v < V; ++v) w[v] = fetch<T>(from, place<T>(v), a.K);
+            for (int v = 0; v < V; ++v) w[v] = fetch<T, WHOLE>(from, v, a.K);
         };
         if (a.block) fetch_row(block, a.block + row * a.block_row);
         if (kTogether) {
@@ -216,20 +228,25 @@ __global__ __launch_bounds__(Shape<T>::kThreads) void spqt_i8_norm_kernel(Norm a
             __builtin_amdgcn_sched_barrier(0);
         }
         auto numbers = [&](const u32x4 (&w)[V], const uint16_t *from, int v, float (&x)[8]) {
-            const int k = place<T>(v);
-            widen8<BF16>(settle<T>(kTogether ? w[v] : fetch<T>(from, k, a.K), k, a.K), x);
+            widen8<BF16>(settle<T, WHOLE>(kTogether ? w[v] : fetch<T, WHOLE>(from, v, a.K), v, a.K), x);
+        };
+        auto gains = [&](const u32x4 (&w)[V], const uint16_t *from, int v, float (&x)[8]) {
+            numbers(w, from, v, x);
+            if (a.offset != 0.0f)
+#pragma unroll
+                for (int e = 0; e < 8; ++e) x[e] += a.offset;
         };
         float s[V][8], other[8];
         if (a.block) {
 #pragma unroll
-            for (int v = 0; v < V; ++v) widen8<BF16>(settle<T>(block[v], place<T>(v), a.K), s[v]);
+            for (int v = 0; v < V; ++v) widen8<BF16>(settle<T, WHOLE>(block[v], v, a.K), s[v]);
             if (a.block_gain) {
-                const float by = inverse_rms<T, V>(s, a.K, a.eps, shared, 0);
+                const float by = inverse_rms<T, V>(s, a.per, a.eps, shared, 0);
 #pragma unroll
                 for (int v = 0; v < V; ++v) {
-                    numbers(block_gain, a.block_gain, v, other);
+                    gains(block_gain, a.block_gain, v, other);
 #pragma unroll
-                    for (int e = 0; e < 8; ++e) s[v][e] = s[v][e] * by * (a.offset + other[e]);
+                    for (int e = 0; e < 8; ++e) s[v][e] = s[v][e] * by * other[e];
                 }
             }
             if (a.gate)
@@ -241,26 +258,24 @@ __global__ __launch_bounds__(Shape<T>::kThreads) void spqt_i8_norm_kernel(Norm a
                 }
 #pragma unroll
             for (int v = 0; v < V; ++v) {
-                const int k = place<T>(v);
                 numbers(h, h_at, v, other);
 #pragma unroll
                 for (int e = 0; e < 8; ++e) s[v][e] = __builtin_fmaf(a.residual, other[e], s[v][e]);
-                if (k < a.K) put<BF16>(a.h_out + row * a.h_out_row, k, a.K, s[v]);
+                if (has<T, WHOLE>(v, a.K)) put<BF16, WHOLE>(a.h_out + row * a.h_out_row, place<T>(v), a.K, s[v]);
             }
         } else {
 #pragma unroll
             for (int v = 0; v < V; ++v) numbers(h, h_at, v, s[v]);
         }
-        const float by = inverse_rms<T, V>(s, a.K, a.eps, shared, 2);
+        const float by = inverse_rms<T, V>(s, a.per, a.eps, shared, 2);
 #pragma unroll
         for (int v = 0; v < V; ++v) {
-            const int k = place<T>(v);
-            numbers(gain, a.gain, v, other);
+            gains(gain, a.gain, v, other);
 #pragma unroll
-            for (int e = 0; e < 8; ++e) s[v][e] = s[v][e] * by * (a.offset + other[e]);
-            if (a.out && k < a.K) put<BF16>(a.out + row * a.out_row, k, a.K, s[v]);
+            for (int e = 0; e < 8; ++e) s[v][e] = s[v][e] * by * other[e];
+            if (a.out && has<T, WHOLE>(v, a.K)) put<BF16, WHOLE>(a.out + row * a.out_row, place<T>(v), a.K, s[v]);
         }
-        if (a.codes) quantize_row<T, V>(s, a.K, a.codes + row * a.codes_row, a.scales + row, shared, 4);
+        if (a.codes) quantize_row<T, V, WHOLE>(s, a.K, a.codes + row * a.codes_row, a.scales + row, shared, 4);
         if (T > 64) __syncthreads();               // the slots are free again
     }
 }
@@ -288,17 +303,21 @@ __global__ __launch_bounds__(256) void spqt_i8_read_kernel(Read a) {
             const float v = (float)((int)(w[e / 4] << (24 - 8 * (e % 4))) >> 24) * scale;
             x[e] = v != v ? v : __builtin_fmaxf(-largest, __builtin_fminf(v, largest));
         }
-        put<BF16>(a.out + row * a.out_row, k, a.K, x);
+        put<BF16, false>(a.out + row * a.out_row, k, a.K, x);
     }
 }
 
-// f(threads, eights a thread, BF16) for rows of K numbers: a norm's threads hold two eights up to where a workgroup ends, since they have five tensors to ask for. Codes of 4001 rows of 14336
+// f(threads, eights a thread, BF16, whole 512s) for rows of K numbers: a norm's threads hold two eights up to where a workgroup ends, since they have five tensors to ask for. Codes of 4001 rows of 14336
 // with 512 x 4 / 1024 x 2 / 256 x 8 34.4 / 40.3 / 35.9 us, of 8192 with 256 x 4 / 512 x 2 / 1024 x 1 20.5 / 21.2 / 24.2; norms of 4001 rows of 4096 with 256 x 2 / 512 x 1 27.8 / 34.5.
 template <bool NORM, class F>
 void dispatch(int64_t K, int type, F f) {
     auto typed = [&](auto t, auto v) {
-        if (type == SPQT_I8_BF16) f(t, v, std::true_type());
-        else f(t, v, std::false_type());
+        auto whole = [&](auto bf16) {
+            if (K % 512 == 0) f(t, v, bf16, std::true_type());
+            else f(t, v, bf16, std::false_type());
+        };
+        if (type == SPQT_I8_BF16) whole(std::true_type());
+        else whole(std::false_type());
     };
     if (K <= 512) typed(std::integral_constant<int, 64>(), std::integral_constant<int, 1>());
     else if (K <= 2048) typed(std::integral_constant<int, 256>(), std::integral_constant<int, 1>());
@@ -324,9 +343,9 @@ extern "C" int spqt_i8_quantize(const void *x, int64_t x_row, int64_t rows, int6
     if (rc == SPQT_OK) rc = check_scales(scales);
     if (rc != SPQT_OK) return rc;
     const Quantize a = {(const uint16_t *)x, codes, scales, x_row, codes_row, (int)rows, (int)K};
-    dispatch<false>(K, type, [&](auto t, auto v, auto bf16) {
+    dispatch<false>(K, type, [&](auto t, auto v, auto bf16, auto whole) {
         typedef Shape<decltype(t)::value> S;
-        hipLaunchKernelGGL((spqt_i8_quantize_kernel<decltype(t)::value, decltype(v)::value, decltype(bf16)::value>), grid_of<S>(rows), dim3(S::kThreads), 0,
+        hipLaunchKernelGGL((spqt_i8_quantize_kernel<decltype(t)::value, decltype(v)::value, decltype(bf16)::value, decltype(whole)::value>), grid_of<S>(rows), dim3(S::kThreads), 0,
                            (hipStream_t)stream, a);
     });
     return launched();
@@ -367,10 +386,10 @@ extern "C" int spqt_i8_norm(const spqt_i8_norm_call *c, void *stream) {
     if (rc != SPQT_OK) return rc;
     const Norm a = {(const uint16_t *)c->h, (const uint16_t *)c->block, (const uint16_t *)c->block_gain, (const uint16_t *)c->gate, (const uint16_t *)c->gain,
                     (uint16_t *)c->h_out, (uint16_t *)c->out, c->codes, c->scales, c->h_row, c->block_row, c->gate_row, c->h_out_row, c->out_row, c->codes_row,
-                    (int)rows, (int)K, c->residual, c->eps, c->offset};
-    dispatch<true>(K, c->type, [&](auto t, auto v, auto bf16) {
+                    (int)rows, (int)K, c->residual, c->eps, c->offset, 1.0f / (float)K};
+    dispatch<true>(K, c->type, [&](auto t, auto v, auto bf16, auto whole) {
         typedef Shape<decltype(t)::value> S;
-        hipLaunchKernelGGL((spqt_i8_norm_kernel<decltype(t)::value, decltype(v)::value, decltype(bf16)::value>), grid_of<S>(rows), dim3(S::kThreads), 0,
+        hipLaunchKernelGGL((spqt_i8_norm_kernel<decltype(t)::value, decltype(v)::value, decltype(bf16)::value, decltype(whole)::value>), grid_of<S>(rows), dim3(S::kThreads), 0,
                            (hipStream_t)stream, a);
     });
     return launched();
