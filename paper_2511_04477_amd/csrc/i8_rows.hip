@@ -18,7 +18,7 @@ __device__ __forceinline__ int place(int v) {
 }
 
 // Rows of whole 512s (WHOLE) end between two wavefronts' eights: whether a wavefront has its v-th ones is one question for all its lanes, and nothing needs to be moved or
-// masked. With that question asked lane by lane a norm of 4001 rows of 8192 took 57 us.
+// masked. With that question asked lane by lane 4001 rows of 8192 took a norm 56 us in place of 53, 20000 of 512 22.4 in place of 19.1, and codes of 4001 rows of 14336 34.5 in place of 32.5.
 template <int T, bool WHOLE>
 __device__ __forceinline__ bool has(int v, int K) {
     if (!WHOLE) return place<T>(v) < K;
@@ -174,7 +174,7 @@ struct Quantize {
 };
 
 // A row is in the registers of its threads: read once, its largest magnitude found, its codes written.
-// What bounds it: 2 bytes in and 1 out a number: 4001 rows of 14336 34.4 us = 5.0 TB/s, of 8192 20.5 = 4.8 (a copy: 4.83); 40 of 28672 4.4 us; one of 4096 2.2.
+// What bounds it: 2 bytes in and 1 out a number: 4001 rows of 14336 32.5 us = 5.3 TB/s, of 8192 20.5 = 4.8 (a copy: 5.1); 40 of 28672 3.7 us; one of 4096 2.1.
 template <int T, int V, bool BF16, bool WHOLE>
 __global__ __launch_bounds__(Shape<T>::kThreads) void spqt_i8_quantize_kernel(Quantize a) {
     typedef Shape<T> S;
@@ -204,15 +204,16 @@ struct Norm {
 };
 
 // One pass: what a block has made, the stream and the vectors are read once, and the sum stays in registers, in 32 bits, from the join over both norms to the codes.
-// What bounds it: 4 bytes in and 3 out a number, and three sums over a row that follow each other: 4001 rows of 8192 with both norms and a gate 56 us = 4.1 TB/s; with loads where they are
-// used and sums over lanes by way of shared memory 82. One row of 4096 4.0 us: loads, three sums, stores.
-template <int T, int V, bool BF16, bool WHOLE>
+// TOGETHER: everything is asked for before any of it is used. That takes half as many registers again, with which a CU holds fewer wavefronts: of 512 and 1024 threads, two workgroups and one in
+// place of four and two. Together / not: one row of 8192 4.2 / 4.7 us, 40 rows 4.5 / 5.1, 256 rows 6.3 / 6.8, 512 rows 9.2 / 8.9, 4001 rows 53.0 / 48.1; 300 rows of 14336 13.1 / 10.8, 1000 rows
+// 33.7 / 26.6; of 256 threads, 4001 rows of 4096 26.5 / 27.4.
+// What bounds it: 4 bytes in and 3 out a number, and three sums over a row that follow each other: 4001 rows of 8192 with both norms and a gate 48 us = 4.8 TB/s; with sums over lanes by way of
+// shared memory 82. One row of 4096 3.7 us: loads, three sums, stores.
+template <int T, int V, bool BF16, bool WHOLE, bool TOGETHER>
 __global__ __launch_bounds__(Shape<T>::kThreads) void spqt_i8_norm_kernel(Norm a) {
     typedef Shape<T> S;
-    constexpr bool kTogether = V <= 2;
     __shared__ uint32_t shared[5 * S::kWaves];
     for (int64_t row = (int64_t)blockIdx.x * S::kRows + (S::kRows > 1 ? threadIdx.x / T : 0); row < a.rows; row += (int64_t)gridDim.x * S::kRows) {
-        // everything is asked for before any of it is used, where there are registers for that
         u32x4 h[V], block[V], block_gain[V], gate[V], gain[V];
         const uint16_t *const h_at = a.h + row * a.h_row, *const gate_at = a.gate + row * a.gate_row;
         auto fetch_row = [&](u32x4 (&w)[V], const uint16_t *from) {
@@ -220,7 +221,7 @@ __global__ __launch_bounds__(Shape<T>::kThreads) void spqt_i8_norm_kernel(Norm a
             for (int v = 0; v < V; ++v) w[v] = fetch<T, WHOLE>(from, v, a.K);
         };
         if (a.block) fetch_row(block, a.block + row * a.block_row);
-        if (kTogether) {
+        if (TOGETHER) {
             fetch_row(h, h_at);
             if (a.block_gain) fetch_row(block_gain, a.block_gain);
             if (a.gate) fetch_row(gate, gate_at);
@@ -228,7 +229,7 @@ __global__ __launch_bounds__(Shape<T>::kThreads) void spqt_i8_norm_kernel(Norm a
             __builtin_amdgcn_sched_barrier(0);
         }
         auto numbers = [&](const u32x4 (&w)[V], const uint16_t *from, int v, float (&x)[8]) {
-            widen8<BF16>(settle<T, WHOLE>(kTogether ? w[v] : fetch<T, WHOLE>(from, v, a.K), v, a.K), x);
+            widen8<BF16>(settle<T, WHOLE>(TOGETHER ? w[v] : fetch<T, WHOLE>(from, v, a.K), v, a.K), x);
         };
         auto gains = [&](const u32x4 (&w)[V], const uint16_t *from, int v, float (&x)[8]) {
             numbers(w, from, v, x);
@@ -307,7 +308,7 @@ __global__ __launch_bounds__(256) void spqt_i8_read_kernel(Read a) {
     }
 }
 
-// f(threads, eights a thread, BF16, whole 512s) for rows of K numbers: a norm's threads hold two eights up to where a workgroup ends, since they have five tensors to ask for. Codes of 4001 rows of 14336
+// f(threads, eights a thread, BF16, whole 512s) for rows of K numbers: a norm's threads hold two eights up to where a workgroup ends, since they have five tensors to ask for. With rows' ends asked for lane by lane, codes of 4001 rows of 14336
 // with 512 x 4 / 1024 x 2 / 256 x 8 34.4 / 40.3 / 35.9 us, of 8192 with 256 x 4 / 512 x 2 / 1024 x 1 20.5 / 21.2 / 24.2; norms of 4001 rows of 4096 with 256 x 2 / 512 x 1 27.8 / 34.5.
 template <bool NORM, class F>
 void dispatch(int64_t K, int type, F f) {
@@ -388,9 +389,15 @@ extern "C" int spqt_i8_norm(const spqt_i8_norm_call *c, void *stream) {
                     (uint16_t *)c->h_out, (uint16_t *)c->out, c->codes, c->scales, c->h_row, c->block_row, c->gate_row, c->h_out_row, c->out_row, c->codes_row,
                     (int)rows, (int)K, c->residual, c->eps, c->offset, 1.0f / (float)K};
     dispatch<true>(K, c->type, [&](auto t, auto v, auto bf16, auto whole) {
-        typedef Shape<decltype(t)::value> S;
-        hipLaunchKernelGGL((spqt_i8_norm_kernel<decltype(t)::value, decltype(v)::value, decltype(bf16)::value, decltype(whole)::value>), grid_of<S>(rows), dim3(S::kThreads), 0,
-                           (hipStream_t)stream, a);
+        constexpr int T = decltype(t)::value, V = decltype(v)::value;
+        auto launch = [&](auto together) {
+            hipLaunchKernelGGL((spqt_i8_norm_kernel<T, V, decltype(bf16)::value, decltype(whole)::value, decltype(together)::value>), grid_of<Shape<T>>(rows), dim3(Shape<T>::kThreads), 0,
+                               (hipStream_t)stream, a);
+        };
+        // together while a CU has a row at most, where nothing else runs beside a load's way, and always where that leaves wavefronts enough
+        if constexpr (V > 2) launch(std::false_type());
+        else if constexpr (T < 512) launch(std::true_type());
+        else rows <= 256 ? launch(std::true_type()) : launch(std::false_type());
     });
     return launched();
 }

@@ -253,7 +253,7 @@ def test_norm_of_the_largest_numbers(gpu, K):
     assert bool(((scales.double().cpu() * 127 - top).abs() <= far.max(dim=1)[0] + 2 * oracle.U * top).all())
 
 
-@pytest.mark.parametrize("rows,K", [(5001, 24), (3001, 1000), (1500, 4096)])
+@pytest.mark.parametrize("rows,K", [(5001, 24), (3001, 1000), (1500, 4096), (300, 8192), (333, 5003), (257, 14336), (261, 9007), (258, 20000)])
 def test_norm_of_many_rows(gpu, rows, K):
     given, more = norm_inputs(rows, K, torch.float16, dict(block_gain=True, gate="channel"))
     on = {n: t.cuda() for n, t in given.items()}
@@ -265,6 +265,9 @@ def test_norm_of_many_rows(gpu, rows, K):
         one = torch.zeros((1, K), dtype=torch.float16, device="cuda")
         gpu.spqt_i8_norm(on["h"][r : r + 1], on["gain"], block=on["block"][r : r + 1], block_gain=on["block_gain"], gate=on["gate"], h_out=torch.zeros_like(one), out=one)
         assert same(one[0], outputs["out"][r])
+    # in place
+    gpu.spqt_i8_norm(**on, h_out=on["h"], out=on["block"])
+    assert same(on["h"], outputs["h_out"]) and same(on["block"], outputs["out"])
 
 
 # ------------------------------------------------------------------------- products
