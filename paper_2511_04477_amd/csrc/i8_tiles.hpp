@@ -18,11 +18,24 @@
 namespace spqt {
 namespace i8 {
 
+// A divisor with floor(2^32 / by), or 2^32 - 1 for 1: n times that is the quotient's 2^32 or up to n less, so that its upper half is the quotient or one less.
+struct Divisor {
+    uint32_t by, inverse;
+};
+inline Divisor divisor(uint32_t by) { return {by, by == 1 ? 0xFFFFFFFFu : (uint32_t)(((uint64_t)1 << 32) / by)}; }
+__device__ __forceinline__ int divided(uint32_t n, Divisor d, int &rest) {
+    uint32_t q = __umulhi(n, d.inverse), r = n - q * d.by;
+    const bool more = r >= d.by;
+    rest = (int)(more ? r - d.by : r);
+    return (int)(more ? q + 1 : q);
+}
+
 // What a launch's workgroups do: units of a tile and a part of K each.
 struct Tiling {
     int row_tiles, channel_tiles, wide;
     int tiles, parts, units;
     int steps;                           // of K
+    Divisor by_tiles, by_parts, by_group, by_wide, by_last;      // by_group: tiles of `wide` row tiles; by_last: row tiles that are left behind whole groups
     i32x4 *sums;                         // of the parts, where there are several: a unit's lanes one after the other
     uint32_t *head;                      // of the workspace
 };
@@ -40,14 +53,13 @@ struct Unit {
     int row_tile, channel_tile, begin, end;      // steps
 };
 __device__ __forceinline__ Unit unit_at(const Tiling &t, int at) {
-    const int part = __builtin_amdgcn_readfirstlane(at / t.tiles), tile = at - part * t.tiles;
-    const int per = t.wide * t.channel_tiles, group = tile / per, in = tile - group * per;
-    const int left = t.row_tiles - group * t.wide, here = left < t.wide ? left : t.wide;
+    int tile, in, rest;
+    const int part = divided(at, t.by_tiles, tile), group = divided(tile, t.by_group, in);
     Unit u;
-    u.channel_tile = __builtin_amdgcn_readfirstlane(in / here);
-    u.row_tile = __builtin_amdgcn_readfirstlane(group * t.wide + in - u.channel_tile * here);
-    u.begin = t.parts == 1 ? 0 : __builtin_amdgcn_readfirstlane(t.steps * part / t.parts);
-    u.end = t.parts == 1 ? t.steps : __builtin_amdgcn_readfirstlane(t.steps * (part + 1) / t.parts);
+    u.channel_tile = divided(in, (group + 1) * t.wide <= t.row_tiles ? t.by_wide : t.by_last, rest);
+    u.row_tile = group * t.wide + rest;
+    u.begin = t.parts == 1 ? 0 : divided(t.steps * part, t.by_parts, rest);
+    u.end = t.parts == 1 ? t.steps : divided(t.steps * (part + 1), t.by_parts, rest);
     return u;
 }
 
@@ -371,13 +383,14 @@ __global__ __launch_bounds__(WM * WN * 64, 1) void spqt_i8_tiles_kernel(Product 
         advance_b(no);
     };
     if constexpr (S::kAhead) {
+#pragma unroll 1
         for (int j = 0; j < NA; ++j) {
             all_b();
             all_a();
         }
         meet(std::integral_constant<int, (NA - 1) * (S::kLoadsA + S::kLoadsB)>());
     } else {
-#pragma unroll
+#pragma unroll 1
         for (int j = -(NA > NB ? NA : NB); j < -1; ++j) {
             if (j + NA >= 0) all_a();
             if (j + NB >= 0) all_b();
@@ -526,6 +539,11 @@ void launch_tiles(const Product &p, bool gated, int parts, void *workspace, hipS
     t.parts = parts;
     t.units = t.tiles * parts;
     t.steps = (p.K + kStep - 1) / kStep;
+    t.by_tiles = divisor(t.tiles);
+    t.by_parts = divisor(parts);
+    t.by_group = divisor(t.wide * t.channel_tiles);
+    t.by_wide = divisor(t.wide);
+    t.by_last = divisor(t.row_tiles % t.wide > 0 ? t.row_tiles % t.wide : t.wide);
     t.head = (uint32_t *)workspace;
     t.sums = (i32x4 *)((uint8_t *)workspace + kWorkspaceHead);
     auto typed = [&](auto yt) {
