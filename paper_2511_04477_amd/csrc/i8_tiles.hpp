@@ -8,7 +8,7 @@
 // 4001 x 28672 x 4096 with the gate 396 to 411 us = 2.3 POPS, the clock down to 1.7 GHz, matrix units busy for 0.73 of the time, shared memory for 0.30, without conflicts but for the outputs.
 // The matrix instructions alone, with the same codes, come to 3.5 POPS, with the reads of shared memory to 2.85. Wavefronts of 128 x 128 in place of 128 x 64 read a third less from it: 206 us
 // for 190, the registers do not suffice for the outputs. 128 x 256 tiles are 0.9 as fast, 128 x 128 0.7 (with two workgroups a CU, of two and three steps' room, 0.78: 6396 x 8192 x 698 96 -> 74 us, where
-// 256 x 256 takes 69). Small sizes: some 7 us of a launch, a first step's way from memory and a last tile's outputs, and with parts the sums' way there and back: of the 34 us of
+// 256 x 256 takes 67). Small sizes: some 7 us of a launch, a first step's way from memory and a last tile's outputs, and with parts the sums' way there and back: of the 33 us of
 // 250 x 4096 x 14336 24 are this kernel's (weights at 3.5 TB/s in the loop), 5.5 the join's. Few rows: the weights' way from memory, 40 x 8192 x 28672 47 us of this kernel = 5.0 TB/s.
 #ifndef SPQT_I8_TILES_HPP
 #define SPQT_I8_TILES_HPP
