@@ -101,7 +101,10 @@ __global__ __launch_bounds__(W * 64) void spqt_i8_few_kernel(Product p) {
         const int n = n0 + made * 16 + 4 * quarter + e;
         if (n >= p.outputs) break;
         float v = scaled(p, first[e], scale, n);
-        if (GATED) v = gated_by(v, scaled(p, second[e], scale, n + p.outputs));
+        if (GATED) {
+            const float up = scaled(p, second[e], scale, n + p.outputs);
+            v = p.y_type == SPQT_I8_FP32 ? gated_by<true>(v, up) : gated_by<false>(v, up);
+        }
         store_one(p, row, n, v);
     }
 }

@@ -159,7 +159,7 @@ struct Finish {
                     if (GATED) {
                         const f32x4 u = values(part * kN + n + S::NI / 2, q);
 #pragma unroll
-                        for (int e = 0; e < 4; ++e) v[e] = gated_by(v[e], u[e]);
+                        for (int e = 0; e < 4; ++e) v[e] = gated_by<YT == SPQT_I8_FP32>(v[e], u[e]);
                     }
                     uint8_t *to = put + (put_at ^ ((n * 32 + q * 8) * kBytes));
                     if (YT == SPQT_I8_FP32) *reinterpret_cast<f32x4 *>(to) = v;

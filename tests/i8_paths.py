@@ -1,0 +1,18 @@
+"""Sizes of 8-bit products that take every way through the kernels, gated or not, with rows of codes and weights that begin at multiples of 16 bytes.
+
+"one": a tile to a workgroup, at most; "parts": K is divided, and the sums are joined (with a workspace); "rounds": workgroups go on to further tiles.
+"""
+
+# (tile, way): (rows, N, K), each with edges in every dimension; the K of "rounds" is a step of 128 or two, or several.
+PATHS = {
+    ("256x256", "one"): (131, 33770, 247), ("256x256", "parts"): (132, 17224, 5410), ("256x256", "rounds"): (398, 34898, 119),
+    ("128x256", "one"): (77, 32868, 249), ("128x256", "parts"): (271, 3988, 6971), ("128x256", "rounds"): (262, 34722, 189),
+    ("128x128", "one"): (65, 21084, 372), ("128x128", "parts"): (65, 1556, 13336), ("128x128", "rounds"): (8373, 856, 1207),
+    ("64x128", "one"): (461, 1054, 1278), ("64x128", "parts"): (55, 62, 3919), ("64x128", "rounds"): (150, 16708, 2290),
+}
+# Without shared memory: up to 16 rows, up to 32, more.
+FEW = [(1, 40, 300), (15, 66, 1000), (29, 130, 700), (70, 94, 333)]
+
+
+def pitch(K):
+    return -(-K // 16) * 16
