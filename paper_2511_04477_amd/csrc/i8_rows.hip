@@ -102,8 +102,9 @@ __device__ __forceinline__ uint32_t most_over_row(uint32_t v, uint32_t *shared, 
     return over_row<T>(v, [](uint32_t a, uint32_t b) { return a > b ? a : b; }, shared, slot);
 }
 
-// 1 / sqrt(mean x^2 + eps), within 3.5 halves of fp32's steps behind the sum: 1 / K and its product, the sum with eps, these by the root's half, and two of the hardware's reciprocal root.  Squares of numbers from 2^64 on, and sums of 2^16 of them from 2^56 on, leave fp32: such a row is summed in units of 2^80, in which eps is nothing,
-// its largest number is from 2^-24 to 2^48.
+// 1 / sqrt(mean x^2 + eps), within 3.5 halves of fp32's steps behind the sum: 1 / K and its product, the sum with eps, these by the root's half, and two of the hardware's reciprocal root. Where the mean
+// is over 2^252 the result is a subnormal number, 4 more of them. Squares of numbers from 2^64 on, and sums of 2^16 of them from 2^56 on, leave fp32, as mean + eps may: such a row is summed in
+// units of 2^80, in which its largest number is from 2^-24 to 2^48, or eps is 2^-33 and more.
 template <int T, int V>
 __device__ __forceinline__ float inverse_rms(const float (&x)[V][8], float per, float eps, uint32_t *shared, int slot) {
     float sum = 0.0f;
@@ -112,7 +113,8 @@ __device__ __forceinline__ float inverse_rms(const float (&x)[V][8], float per, 
 #pragma unroll
         for (int e = 0; e < 8; ++e) sum = __builtin_fmaf(x[v][e], x[v][e], sum);
     sum = sum_over_row<T>(sum, shared, slot);
-    if (sum < __builtin_inff() || sum != sum) return __builtin_amdgcn_rsqf(sum * per + eps);
+    const float mean = sum * per + eps;
+    if (mean < __builtin_inff() || mean != mean) return __builtin_amdgcn_rsqf(mean);
     sum = 0.0f;
 #pragma unroll
     for (int v = 0; v < V; ++v)
@@ -122,7 +124,7 @@ __device__ __forceinline__ float inverse_rms(const float (&x)[V][8], float per, 
             sum = __builtin_fmaf(y, y, sum);
         }
     sum = sum_over_row<T>(sum, shared, slot + 1);
-    return 0x1p-80f * __builtin_amdgcn_rsqf(sum * per);
+    return 0x1p-80f * __builtin_amdgcn_rsqf(sum * per + eps * 0x1p-80f * 0x1p-80f);
 }
 
 // Codes of a row, from the largest magnitude of this thread's numbers: magnitudes order as their bits do, infinities and NaN above all numbers.
