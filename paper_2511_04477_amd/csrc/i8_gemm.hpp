@@ -17,8 +17,9 @@ struct Product {
     int y_type;
 };
 
-// A sum of channel n and a row with this scale.
+// A sum of channel n and a row with this scale. Each step is rounded, here and where the tiles' outputs are made, so that all ways give the same bits.
 __device__ __forceinline__ float scaled(const Product &p, int sum, float scale, int n) {
+#pragma clang fp contract(off)
     float v = (float)sum * scale * p.weight_scales[n];
     if (p.bias) v += p.bias[n];
     return v;

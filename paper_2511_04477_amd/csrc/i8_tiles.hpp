@@ -130,6 +130,7 @@ struct Finish {
     // stage: where this wavefront has kilobytes of shared memory of its own, `apart` bytes from each other
     __device__ __forceinline__ void rows(const i32x16 (&acc)[S::NI], int first, float scale, const Scales &by, uint8_t *stage, int apart, int lane) const {
         auto values = [&](int n, int q) {
+#pragma clang fp contract(off)
             f32x4 v;
 #pragma unroll
             for (int e = 0; e < 4; ++e) v[e] = (float)acc[n][q * 4 + e] * scale * by.of[n][q][e];
