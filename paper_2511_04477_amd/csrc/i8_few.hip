@@ -127,15 +127,6 @@ void launch(const Product &p, hipStream_t stream) {
 namespace spqt {
 namespace i8 {
 
-// Of more than sixteen rows, in us: an instruction reads 16 rows, each a line of its own, which takes a CU as many cycles: 35 KB a us, of codes and weights alike; not before the weights are
-// read, and 3 for the launch. Measured / this: 64 x 4096 x 4096 12.7 / 12.4, 128 x 4096 x 4096 21.7 / 21.7, 32 x 12288 x 4096 21.2 / 19.9, 300 x 520 x 2000 6.9 / 7.6.
-double few_us(const Product &p, bool gated) {
-    const int R = p.rows <= 32 ? 2 : 4;
-    const int64_t groups = (int64_t)((p.outputs + 15) / 16) * ((p.rows + 16 * R - 1) / (16 * R));
-    const double turns = (double)((groups + 255) / 256), read = turns * ((p.rows < 16 * R ? p.rows : 16 * R) + (gated ? 32 : 16)) * p.K / 35e3, weights = p.N * (double)p.K / 4.7e6;
-    return 3.0 + (read > weights ? read : weights);
-}
-
 // Sixteen channels a workgroup, thirty-two where sixteen rows' codes are so many that reading them for every sixteen channels counts, and there are workgroups enough all the same: rows x
 // channels x K, us of 16 / 32 channels: 16 x 8192 x 28672 65.3 / 51.0, 4 x 8192 x 28672 50.0 / 47.8, 16 x 57344 x 8192 with the gate 105 / 96; the other way round 1 x 28672 x 4096 25.7 / 27.4,
 // 16 x 4096 x 14336 (few workgroups) 19.7 / 24.1, 1 x 22016 x 4096 22.6 / 27.4.

@@ -4,21 +4,13 @@
 using namespace spqt;
 using namespace spqt::i8;
 
-namespace {
-constexpr int kFewRows = 16;         // that always go through i8_few.hip
-}
-
 extern "C" int spqt_i8_workspace_bytes(int64_t rows, int64_t N, int64_t K, size_t *out_bytes) {
     if (!out_bytes) return SPQT_EINVAL;
     if (N < 1 || N > 1 << 24) return SPQT_ESHAPE;
     const int rc = check_extents(rows, K, SPQT_I8_MAX_K);
     if (rc != SPQT_OK) return rc;
-    *out_bytes = 0;
-    if (rows <= kFewRows) return SPQT_OK;
-    // as much for larger numbers as for smaller ones, at least: a workspace for more serves less
-    const int64_t tiles = ((rows + 63) / 64) * ((N + 127) / 128), steps = (K + 127) / 128, parts = steps < 16 ? steps : 16;
-    const int64_t sums = tiles * parts * (64 * 128 * 4), most = (int64_t)64 << 20;
-    *out_bytes = parts > 1 ? kWorkspaceHead + (size_t)(sums < most ? sums : most) : 0;
+    const size_t sums = most_sums(rows, N, K);
+    *out_bytes = sums ? kWorkspaceHead + sums : 0;
     return SPQT_OK;
 }
 
@@ -40,13 +32,8 @@ extern "C" int spqt_i8_gemm(const spqt_i8_product *c, void *workspace, size_t wo
     if (workspace && workspace_bytes < need) return SPQT_ESIZE;
     const Product p = {c->codes, c->weights, c->scales, c->weight_scales, c->bias, c->y, c->codes_row, c->weights_row, c->y_row,
                        (int)c->rows, (int)c->N, (int)c->K, (int)outputs, c->y_type};
-    if (p.rows > kFewRows) {
-        const Plan plan = plan_tiles(p, c->gated != 0, workspace && need > kWorkspaceHead ? need - kWorkspaceHead : 0);
-        if (plan.shape >= 0 && plan.us < few_us(p, c->gated != 0)) {
-            launch_tiles_of(plan, p, c->gated != 0, workspace, (hipStream_t)stream);
-            return launched();
-        }
-    }
-    launch_few(p, c->gated != 0, (hipStream_t)stream);
+    const Plan plan = plan_of(p, c->gated != 0, workspace && need ? need - kWorkspaceHead : 0);
+    if (plan.shape >= 0) launch_tiles_of(plan, p, c->gated != 0, workspace, (hipStream_t)stream);
+    else launch_few(p, c->gated != 0, (hipStream_t)stream);
     return launched();
 }

@@ -3,19 +3,10 @@
 #define SPQT_I8_GEMM_HPP
 
 #include "i8_common.hpp"
+#include "i8_plan.hpp"
 
 namespace spqt {
 namespace i8 {
-
-struct Product {
-    const int8_t *codes, *weights;
-    const float *scales, *weight_scales, *bias;
-    void *y;
-    int64_t codes_row, weights_row, y_row;
-    int rows, N, K;
-    int outputs;             // of a row: N, gated N / 2
-    int y_type;
-};
 
 // A sum of channel n and a row with this scale. Each step is rounded, here and where the tiles' outputs are made, so that all ways give the same bits.
 __device__ __forceinline__ float scaled(const Product &p, int sum, float scale, int n) {
@@ -51,16 +42,6 @@ __device__ __forceinline__ i32x4 masked(i32x4 x, int k, int K) {
 }
 
 void launch_few(const Product &p, bool gated, hipStream_t stream);
-
-// What launch_few is expected to take.
-double few_us(const Product &p, bool gated);
-
-// A shape of tiles (i8_tiles.hip has them) and the parts that K is divided into, and what that is expected to take.
-struct Plan {
-    int shape, parts;
-    double us;
-};
-Plan plan_tiles(const Product &p, bool gated, size_t room);       // room: bytes for the parts' sums; shape -1: none can
 void launch_tiles_of(const Plan &plan, const Product &p, bool gated, void *workspace, hipStream_t stream);
 
 }  // namespace i8

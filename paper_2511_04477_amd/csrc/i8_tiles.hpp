@@ -39,7 +39,6 @@ struct Tiling {
     i32x4 *sums;                         // of the parts, where there are several: a unit's lanes one after the other
     uint32_t *head;                      // of the workspace
 };
-constexpr int kGroups = 256;             // workgroups of a launch, at most: one a CU
 
 // The unit of a workgroup in a round of kGroups, or -1. Workgroups go to the eight XCDs in turn: each of them gets neighbours, which share rows and channels in its cache.
 __device__ __forceinline__ int unit_of(const Tiling &t, int round) {
@@ -75,7 +74,6 @@ __device__ __forceinline__ int anew(int v) {
 }
 
 // TM rows by TN channels, WM by WN wavefronts of MI by NI matrix instructions' 32 by 32 each. Shared memory has room for NA steps of the rows and NB of the channels.
-constexpr int kStep = 128;               // bytes of K that a tile takes at a time: a line of memory
 template <int TM, int TN, int WM, int WN, int NA, int NB>
 struct Shape {
     static constexpr int kWaves = WM * WN, kThreads = kWaves * 64;

@@ -1,6 +1,7 @@
 """Sizes of 8-bit products that take every way through the kernels, gated or not, with rows of codes and weights that begin at multiples of 16 bytes.
 
-"one": a tile to a workgroup, at most; "parts": K is divided, and the sums are joined (with a workspace); "rounds": workgroups go on to further tiles.
+"one": a tile to a workgroup, at most; "parts": K is divided, and the sums are joined (with a workspace); "rounds": workgroups go on to further tiles; "long": more than twice,
+with many steps each.  tests/test_host_i8_plan.py holds them to that.
 """
 
 # (tile, way): (rows, N, K), each with edges in every dimension; the K of "rounds" is a step of 128 or two, or several.
@@ -8,6 +9,7 @@ PATHS = {
     ("256x256", "one"): (131, 33770, 247), ("256x256", "parts"): (132, 17224, 5410), ("256x256", "rounds"): (398, 34898, 119),
     ("128x256", "one"): (77, 32868, 249), ("128x256", "parts"): (271, 3988, 6971), ("128x256", "rounds"): (262, 34722, 189),
     ("128x128", "one"): (65, 21084, 372), ("128x128", "parts"): (65, 1556, 13336), ("128x128", "rounds"): (8373, 856, 1207),
+    ("256x256", "long"): (2585, 12600, 898), ("128x256", "long"): (1039, 15378, 1065), ("128x128", "long"): (8410, 1834, 1420), ("64x128", "long"): (67, 49062, 3194),
     ("64x128", "one"): (461, 1054, 1278), ("64x128", "parts"): (55, 62, 3919), ("64x128", "rounds"): (150, 16708, 2290),
 }
 # Without shared memory: up to 16 rows, up to 32, more.
