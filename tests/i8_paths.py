@@ -18,3 +18,13 @@ FEW = [(1, 40, 300), (15, 66, 1000), (29, 130, 700), (70, 94, 333)]
 
 def pitch(K):
     return -(-K // 16) * 16
+
+
+# A layer (hidden, heads, kv heads, dim, inner) and prompts whose products go by tiles, the last one in parts. Rows of codes begin at multiples of 128 bytes there.
+LAYER = (2048, 16, 4, 128, 5632)
+PROMPTS = [200, 150]
+
+
+def layer_products(hidden, heads, kv_heads, dim, inner):
+    """(N, K, gated) of a layer's products."""
+    return [((heads + 2 * kv_heads) * dim, hidden, False), (hidden, heads * dim, False), (2 * inner, hidden, True), (hidden, inner, False)]

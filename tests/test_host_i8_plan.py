@@ -7,7 +7,7 @@ import subprocess
 import pytest
 
 import paper_2511_04477_amd as spqt
-from i8_paths import FEW, PATHS, pitch
+from i8_paths import FEW, LAYER, PATHS, PROMPTS, layer_products, pitch
 
 ROOT = os.path.dirname(os.path.dirname(os.path.abspath(__file__)))
 SOURCE = """
@@ -76,6 +76,12 @@ def test_the_sizes_of_the_gpu_tests_take_every_way(rules, gated):
             assert {"one": units <= 256, "parts": units <= 256, "rounds": 256 < units, "long": 512 < units and K > 6 * 128}[kind], (tile, kind, units)
     for rows, N, K in FEW:
         assert way(rules, rows, N, K, gated)[0] == "few"
+
+
+def test_the_layer_of_the_gpu_tests_goes_by_tiles(rules):
+    for rows in PROMPTS:
+        took = [way(rules, rows, N, K, gated, codes_row=-(-K // 128) * 128, weights_row=-(-K // 128) * 128) for N, K, gated in layer_products(*LAYER)]
+        assert all(tile != "few" for tile, *_ in took) and took[3][1] > 1 and len({tile for tile, *_ in took}) > 1
 
 
 def test_every_tile_has_every_way():
