@@ -28,3 +28,17 @@ PROMPTS = [200, 150]
 def layer_products(hidden, heads, kv_heads, dim, inner):
     """(N, K, gated) of a layer's products."""
     return [((heads + 2 * kv_heads) * dim, hidden, False), (hidden, heads * dim, False), (2 * inner, hidden, True), (hidden, inner, False)]
+
+# Rows as far apart as tiles take them, whose places pass 2^31: (rows, N, K, gated, strides of codes, weights and y, tile). The last of each pair of gated ones is just too far for tiles.
+_FAR = (1 << 23) - 128
+
+
+def _reach(N):
+    return ((1 << 32) - 1) // (N + 256) // 128 * 128
+
+
+FAR = [
+    (398, 34898, 119, False, _FAR, 128, _FAR, "256x256"), (461, 1054, 1278, False, _FAR, _FAR, _FAR, "64x128"),
+    (398, 34898, 119, True, 128, _reach(34898), _FAR, "256x256"), (398, 34898, 119, True, 128, _reach(34898) + 128, 17449, "few"),
+    (262, 34722, 189, True, _FAR, _reach(34722), 34722, "128x256"), (461, 1054, 1278, True, _FAR, _FAR, _FAR, "few"),
+]

@@ -7,7 +7,7 @@ import subprocess
 import pytest
 
 import paper_2511_04477_amd as spqt
-from i8_paths import FEW, LAYER, PATHS, PROMPTS, layer_products, pitch
+from i8_paths import FAR, FEW, LAYER, PATHS, PROMPTS, layer_products, pitch
 
 ROOT = os.path.dirname(os.path.dirname(os.path.abspath(__file__)))
 SOURCE = """
@@ -121,3 +121,9 @@ def test_places_within_a_tile_are_32_bits(rules):
         assert (N // 2 + 256) * last + pitch(K) < 1 << 32
         assert way(rules, rows, N, K, True, weights_row=last + 128)[0] == "few"
         assert way(rules, rows, N, K, False, weights_row=last + 128)[0] != "few"
+
+
+def test_the_sizes_of_the_gpu_tests_reach_the_limits(rules):
+    for rows, N, K, gated, codes_row, weights_row, y_row, tile in FAR:
+        assert way(rules, rows, N, K, gated, False, codes_row, weights_row, y_row)[0] == tile
+        assert max(rows * codes_row, N * weights_row, rows * y_row) > 1 << 31
