@@ -83,7 +83,9 @@ typedef struct {
     int y_type, gated;
 } spqt_i8_product;
 
-/* Bytes of the workspace with which spqt_i8_gemm may divide K where rows and channels alone do not fill the chip; 0 where it never would. */
+/* Bytes of the workspace with which spqt_i8_gemm may divide K where rows and channels alone do not fill the chip: a bound that depends on rows, N and K only, no less for
+ * more of any of them, so that a workspace for more serves less, and at most 64 MiB and 256 bytes. 0 for up to 16 rows and for K up to 128; sizes that fill the chip
+ * by themselves have the bound of smaller ones, of which they use nothing (NULL serves them as well). */
 int spqt_i8_workspace_bytes(int64_t rows, int64_t N, int64_t K, size_t *out_bytes);
 
 /* workspace: 256-byte aligned, at least spqt_i8_workspace_bytes, or NULL, with which K is not divided and y is the same.  It needs no preparation and

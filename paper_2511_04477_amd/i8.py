@@ -132,6 +132,7 @@ def spqt_i8_norm(h, gain, out=None, codes=None, scales=None, block=None, block_g
 
 
 def spqt_i8_workspace_bytes(rows: int, N: int, K: int) -> int:
+    """Bytes of a workspace for products of this size and of every smaller one."""
     out = ctypes.c_size_t()
     _check(lib().spqt_i8_workspace_bytes(rows, N, K, ctypes.byref(out)))
     return out.value

@@ -127,3 +127,14 @@ def test_the_sizes_of_the_gpu_tests_reach_the_limits(rules):
     for rows, N, K, gated, codes_row, weights_row, y_row, tile in FAR:
         assert way(rules, rows, N, K, gated, False, codes_row, weights_row, y_row)[0] == tile
         assert max(rows * codes_row, N * weights_row, rows * y_row) > 1 << 31
+
+
+def test_a_workspace_for_more_is_no_smaller(rules):
+    """Along each of rows, N and K; 0 where K cannot be divided, and never over 64 MiB and a head."""
+    size = spqt.spqt_i8_workspace_bytes
+    for rows, N, K in sizes(1000, 2):
+        here = size(rows, N, K)
+        assert (here == 0) == (rows <= 16 or K <= 128) and here <= (64 << 20) + HEAD
+        for more in ((rows + 1, N, K), (2 * rows, N, K), (rows, N + 1, K), (rows, 2 * N, K), (rows, N, K + 1), (rows, N, K + 129)):
+            if more[0] <= 1 << 24 and more[1] <= 1 << 24 and more[2] <= 131071:
+                assert size(*more) >= here, (rows, N, K, more)
