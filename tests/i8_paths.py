@@ -42,3 +42,6 @@ FAR = [
     (398, 34898, 119, True, 128, _reach(34898), _FAR, "256x256"), (398, 34898, 119, True, 128, _reach(34898) + 128, 17449, "few"),
     (262, 34722, 189, True, _FAR, _reach(34722), 34722, "128x256"), (461, 1054, 1278, True, _FAR, _FAR, _FAR, "few"),
 ]
+
+# More rows than one launch without shared memory takes (1048560), and tiles that go on 17 times and more.
+MANY = [(1048579, 24, 40, "few"), (2100003, 16, 16, "few"), (1048579, 40, 700, "128x128"), (1048579, 300, 130, "256x256")]

@@ -7,7 +7,7 @@ import subprocess
 import pytest
 
 import paper_2511_04477_amd as spqt
-from i8_paths import FAR, FEW, LAYER, PATHS, PROMPTS, layer_products, pitch
+from i8_paths import FAR, FEW, LAYER, MANY, PATHS, PROMPTS, layer_products, pitch
 
 ROOT = os.path.dirname(os.path.dirname(os.path.abspath(__file__)))
 SOURCE = """
@@ -138,3 +138,10 @@ def test_a_workspace_for_more_is_no_smaller(rules):
         for more in ((rows + 1, N, K), (2 * rows, N, K), (rows, N + 1, K), (rows, 2 * N, K), (rows, N, K + 1), (rows, N, K + 129)):
             if more[0] <= 1 << 24 and more[1] <= 1 << 24 and more[2] <= 131071:
                 assert size(*more) >= here, (rows, N, K, more)
+
+
+def test_the_sizes_of_the_gpu_tests_have_many_rows(rules):
+    for rows, N, K, tile in MANY:
+        for gated in (False, True):
+            took, _, units, _ = way(rules, rows, N, K, gated, False)
+            assert took == tile and rows > 65535 * 16 and (tile == "few" or units > 17 * 256)
