@@ -48,7 +48,7 @@ int spqt_i8_read(const int8_t *codes, int64_t codes_row, const float *scales, in
  *   x = s * r(s) * (offset + gain)
  *
  * h_out = s, out = x in the 16-bit type, codes and scales those of x: all arithmetic is fp32, x is made of s and codes are made of x as they are before
- * they are rounded.  h_out may be h or block, and out may be h or block, element for element; h_out and out are two tensors. */
+ * they are rounded.  h_out may be h or block, and out may be h or block, element for element (with several rows, of the same stride); h_out and out are two tensors. */
 typedef struct {
     const void *h;          /* [rows][K]: the residual stream */
     const void *block;      /* [rows][K] or NULL: what a block has made */

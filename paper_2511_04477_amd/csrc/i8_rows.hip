@@ -1,6 +1,8 @@
 // Rows of numbers to 8-bit codes and back, and the norms before and after a block (spqt_i8.h has the definitions).
 #include "i8_common.hpp"
 
+#include <utility>
+
 namespace {
 
 using namespace spqt;
@@ -376,6 +378,11 @@ extern "C" int spqt_i8_norm(const spqt_i8_norm_call *c, void *stream) {
     if (!(c->eps >= 1e-30f) || !__builtin_isfinite(c->eps) || !__builtin_isfinite(c->residual) || !__builtin_isfinite(c->offset)) return SPQT_EINVAL;
     if (c->h_out && c->h_out == c->out) return SPQT_EINVAL;
     const int64_t rows = c->rows, K = c->K;
+    // in place means element for element: other rows' workgroups may not read what one of them writes
+    for (const auto &w : {std::make_pair(c->h_out, c->h_out_row), std::make_pair(c->out, c->out_row)}) {
+        const auto clash = [&](const void *read, int64_t row) { return w.first && w.first == read && rows > 1 && w.second != row; };
+        if (clash(c->h, c->h_row) || clash(c->block, c->block_row) || clash(c->gate, c->gate_row) || clash(c->gain, 0) || clash(c->block_gain, 0)) return SPQT_EINVAL;
+    }
     int rc = check_extents(rows, K, SPQT_I8_MAX_NORM);
     if (rc == SPQT_OK) rc = check_matrix(c->h, c->h_row, rows, K, 2, false);
     if (rc == SPQT_OK) rc = check_matrix(c->gain, 0, 1, K, 2, false);
