@@ -70,7 +70,8 @@ int spqt_i8_norm(const spqt_i8_norm_call *call, void *stream);
  * The sum is exact; it is rounded to fp32, so is each step after it, and the result to y's type.
  * gated: weights, weight_scales and bias are those of N / 2 rows of a gate and, behind them, N / 2 rows of an up projection (N even), and with v the above
  *   y[r][f] = v[r][f] / (1 + exp(-v[r][f])) * v[r][N / 2 + f],   f < N / 2
- * in fp32, rounded once; for 16-bit outputs exponential and quotient are the hardware's, which are off by 2^-24 (1.3 |v| + 11) relative at most. */
+ * in fp32, rounded once. Exponential and quotient are the hardware's: v / (1 + exp(-v)) is off by 2^-24 times 8 relative at most (12 where v < -87.3) for 32-bit
+ * outputs, by 2^-24 times 1.3 |v| + 11 for 16-bit ones. */
 typedef struct {
     const int8_t *codes;    /* [rows][K] */
     const float *scales;    /* [rows] */

@@ -15,13 +15,23 @@ __device__ __forceinline__ float scaled(const Product &p, int sum, float scale, 
     if (p.bias) v += p.bias[n];
     return v;
 }
-// gate / (1 + exp(-gate)) * up. For 32-bit outputs step by step. For 16 bits by the hardware's power of two and reciprocal, off by 1.3 |gate| + 11 halves of fp32's
-// steps at most, which are nothing next to half a step of the output. The divisor is in sixteenths: the instruction gives 0 in place of reciprocals under 2^-126,
-// which those of gates from -87.4 on would be. Where 1 + exp(-gate) leaves fp32, from -88.8 on, the quotient is 0 (with 16 bits from -90.2 on).
+// gate / (1 + exp(-gate)) * up by the hardware's power of two and reciprocal. The divisor is in sixteenths: the instruction gives 0 in place of
+// reciprocals under 2^-126, which those of gates from -87.4 on would be. Where 1 + exp(-gate) leaves fp32, from -88.8 on, the quotient is 0 (with 16
+// bits from -90.2 on).
+// Halves of fp32's steps that it may be off by: for 16-bit outputs 1.3 |gate| + 11, of the exponential's argument most of them, which are nothing next to
+// half a step of the output. For 32-bit ones (WIDE) what the argument lost is a factor of the power: 8, and 4 more where the reciprocal is subnormal.
+// 4001 x 28672 x 4096 / 6396 x 8192 x 698 with the gate, 32-bit outputs: 421 / 76 us; with the argument as it is 417 / 73, with expf and a division 441 / 89.
 template <bool WIDE>
 __device__ __forceinline__ float gated_by(float gate, float up) {
-    if (WIDE) return gate / (1.0f + expf(-gate)) * up;
-    const float sixteenths = __builtin_amdgcn_exp2f(__builtin_fmaf(gate, -1.44269504f, -4.0f)) + 0.0625f;
+    constexpr float kLog2 = 1.44269502f, kLog2Rest = 1.92596303e-8f, kLn2 = 0.69314718f;
+    float sixteenths;
+    if (WIDE) {
+        const float least = __builtin_amdgcn_fmed3f(gate, -128.0f, 128.0f), power = -least * kLog2;       // (infinities would leave no rest)
+        const float rest = __builtin_fmaf(-least, kLog2Rest, __builtin_fmaf(-least, kLog2, -power));
+        sixteenths = __builtin_fmaf(__builtin_amdgcn_exp2f(power), __builtin_fmaf(rest, kLn2 / 16, 0.0625f), 0.0625f);
+    } else {
+        sixteenths = __builtin_amdgcn_exp2f(__builtin_fmaf(gate, -kLog2, -4.0f)) + 0.0625f;
+    }
     return gate * (__builtin_amdgcn_rcpf(sixteenths) * 0.0625f) * up;
 }
 

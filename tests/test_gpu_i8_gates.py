@@ -19,9 +19,10 @@ def bounds(dtype):
     u = (g32 * torch.tensor(UPS)).double()
     g = g32.double()
     y = g * torch.sigmoid(g) * u
-    # 32 bits: exponential (2), sum, quotient and product, in halves of fp32's steps. 16 bits: the exponential's argument is off by 1.3 |g| + 3 of them, the hardware's two functions
-    # by 2 each, a sum and three products by 4. Steps of subnormal numbers on the way are 2^-149.
-    steps = 5.0 if dtype == torch.float32 else 1.3 * g.abs().clamp(max=100.0) + 11.0
+    # Halves of fp32's steps. 32 bits: the hardware's power and reciprocal (2 each), the factor beside the power, the sum, and two products: 8; where the reciprocal is a subnormal
+    # number, of 2^-128 and more, half a step of 2^-149 is 4 of them. 16 bits: the power's argument is off by 1.3 |g| + 3, power and reciprocal by 2 each, a sum and three products by 4.
+    # Steps of subnormal numbers on the way are 2^-149.
+    steps = torch.where(g < -87.3, 12.0, 8.0).double() if dtype == torch.float32 else 1.3 * g.abs().clamp(max=100.0) + 11.0
     off = y.abs() * steps * U * 1.001 + (g.abs().clamp(max=100.0) + 1.0) * 2.0**-149 * (1.0 + u.abs().clamp(max=2.0**128))
     off = torch.where(y.isinf(), torch.zeros_like(off), off)
     low, high = y - off, y + off
