@@ -1,11 +1,12 @@
 // The product in 8-bit integers, few rows or little of everything: each weight goes from memory to the matrix instruction of one wavefront.
 //
-// With the weights as its first operand v_mfma_i32_16x16x64_i8 gives a lane four channels of one row. The wavefronts of a workgroup take K in turn, 128 bytes each time, and add their
-// sums up in shared memory: whole numbers, whose order does not matter.
+// With the weights as its first operand v_mfma_i32_16x16x64_i8 gives a lane four channels of one row. The wavefronts of a workgroup take K in turn,
+// 128 bytes each time, and add their sums up in shared memory: whole numbers, whose order does not matter.
 //
-// What bounds it: reading the weights. 57344 x 8192 with the gate, one row 82 to 86 us = 5.5 to 5.7 TB/s; 28672 x 4096 25.7 us = 4.6; 6144 x 4096 8.5 us (a launch in a graph is 2 to 3 of that).
-// A lane takes the 16 bytes that follow its neighbour's, so that an instruction reads whole halves of lines: with 32 bytes of a lane one after the other the former was 91 us, 28672 x 4096 30.8.
-// Loads that pass the caches by (non-temporal) 93 and 27.0; two chunks on their way for four 81.8 and 26.0, and 6144 x 4096 8.9; 16 wavefronts 81.1 and 25.8.
+// What bounds it: reading the weights. 57344 x 8192 with the gate, one row 82 to 86 us = 5.5 to 5.7 TB/s; 28672 x 4096 25.7 us = 4.6; 6144 x 4096 8.5
+// us (a launch in a graph is 2 to 3 of that). A lane takes the 16 bytes that follow its neighbour's, so that an instruction reads whole halves of
+// lines: with 32 bytes of a lane one after the other the former was 91 us, 28672 x 4096 30.8. Loads that pass the caches by (non-temporal) 93 and
+// 27.0; two chunks on their way for four 81.8 and 26.0, and 6144 x 4096 8.9; 16 wavefronts 81.1 and 25.8.
 #include "i8_gemm.hpp"
 
 namespace {
@@ -15,7 +16,8 @@ using namespace spqt::i8;
 
 constexpr int kChunk = 128;
 
-// W wavefronts, 16 R rows, 16 C channels (gated: half of them the gate's, half of them those of the up projection), D chunks of a wavefront on their way together.
+// W wavefronts, 16 R rows, 16 C channels (gated: half of them the gate's, half of them those of the up projection), D chunks of a wavefront on their
+// way together.
 template <int W, int R, int C, int D, bool GATED>
 __global__ __launch_bounds__(W * 64) void spqt_i8_few_kernel(Product p) {
     constexpr int kMade = GATED ? C / 2 : C;                      // sixteens of outputs
@@ -127,9 +129,13 @@ void launch(const Product &p, hipStream_t stream) {
 namespace spqt {
 namespace i8 {
 
-// Sixteen channels a workgroup, thirty-two where sixteen rows' codes are so many that reading them for every sixteen channels counts, and there are workgroups enough all the same: rows x
-// channels x K, us of 16 / 32 channels: 16 x 8192 x 28672 65.3 / 51.0, 4 x 8192 x 28672 50.0 / 47.8, 16 x 57344 x 8192 with the gate 105 / 96; the other way round 1 x 28672 x 4096 25.7 / 27.4,
-// 16 x 4096 x 14336 (few workgroups) 19.7 / 24.1, 1 x 22016 x 4096 22.6 / 27.4.
+// Sixteen channels a workgroup, thirty-two where sixteen rows' codes are so many that reading them for every sixteen channels counts, and there are
+// workgroups enough all the same. Rows x channels x K, us of 16 / 32 channels:
+//   at the rule's bound of 112 K codes    4 x 8192 x 28672 44.9 / 44.0      8 x 8192 x 14336 28.1 / 26.2      12 x 57344 x 8192 with the gate (96 K) 98.2 / 94.3
+//   over it    16 x 8192 x 28672 61.2 / 47.1      16 x 57344 x 8192 with the gate 105 / 100      16 x 8192 x 8192 20.8 / 18.9
+//   under it   4 x 8192 x 8192 17.0 / 17.9      8 x 57344 x 8192 with the gate 91.9 / 95.4      1 x 28672 x 4096 24.7 / 28.7      1 x 57344 x 8192 with the gate 84.0 / 92.7
+// Under it and without the gate the other way round from 8 to 12 rows on, by up to 12 %: 8 x 14336 x 4096 18.4 / 17.2, 16 x 28672 x 4096 33.9 / 30.3. Few workgroups:
+// 16 x 4096 x 14336 19.7 / 24.1.
 void launch_few(const Product &p, bool gated, hipStream_t stream) {
     if (p.rows > 32) return gated ? launch<8, 4, 2, 1, true>(p, stream) : launch<8, 4, 1, 1, false>(p, stream);
     if (p.rows > 16) return gated ? launch<8, 2, 2, 2, true>(p, stream) : launch<8, 2, 1, 2, false>(p, stream);

@@ -37,12 +37,14 @@ inline size_t most_sums(int64_t rows, int64_t N, int64_t K) {
     return (size_t)(sums < most ? sums : most);
 }
 
-// Of more than sixteen rows, in us: an instruction reads 16 rows, each a line of its own, which takes a CU as many cycles: 35 KB a us, of codes and weights alike; not before the weights are
-// read, and 3 for the launch. Measured / this: 64 x 4096 x 4096 12.7 / 12.4, 128 x 4096 x 4096 21.7 / 21.7, 32 x 12288 x 4096 21.2 / 19.9, 300 x 520 x 2000 6.9 / 7.6.
+// Of more than sixteen rows, in us: an instruction reads 16 rows, each a line of its own, which takes a CU as many cycles: 35 KB a us, of codes and
+// weights alike; not before the weights are read, and 3 for the launch. Measured / this: 64 x 4096 x 4096 12.7 / 12.4, 128 x 4096 x 4096 21.7 / 21.7,
+// 32 x 12288 x 4096 21.2 / 19.9, 300 x 520 x 2000 6.9 / 7.6.
 inline double few_us(const Product &p, bool gated) {
     const int R = p.rows <= 32 ? 2 : 4;
     const int64_t groups = (int64_t)((p.outputs + 15) / 16) * ((p.rows + 16 * R - 1) / (16 * R));
-    const double turns = (double)((groups + 255) / 256), read = turns * ((p.rows < 16 * R ? p.rows : 16 * R) + (gated ? 32 : 16)) * p.K / 35e3, weights = p.N * (double)p.K / 4.7e6;
+    const double turns = (double)((groups + 255) / 256), weights = p.N * (double)p.K / 4.7e6;
+    const double read = turns * ((p.rows < 16 * R ? p.rows : 16 * R) + (gated ? 32 : 16)) * p.K / 35e3;
     return 3.0 + (read > weights ? read : weights);
 }
 
@@ -53,7 +55,8 @@ struct Cost {
     int rows, channels;
     float step, step_full, fixed, within;
 };
-constexpr Cost kShapes[] = {{256, 256, 0.95f, 1.62f, 2.5f, 1.35f}, {128, 256, 0.55f, 0.93f, 2.5f, 1.5f}, {128, 128, 0.30f, 0.57f, 2.5f, 1.45f}, {64, 128, 0.22f, 0.36f, 2.0f, 1.7f}};
+constexpr Cost kShapes[] = {
+    {256, 256, 0.95f, 1.62f, 2.5f, 1.35f}, {128, 256, 0.55f, 0.93f, 2.5f, 1.5f}, {128, 128, 0.30f, 0.57f, 2.5f, 1.45f}, {64, 128, 0.22f, 0.36f, 2.0f, 1.7f}};
 constexpr int kCount = sizeof(kShapes) / sizeof(kShapes[0]);
 
 inline int64_t tiles_of(const Cost &s, const Product &p, bool gated) {
@@ -61,14 +64,17 @@ inline int64_t tiles_of(const Cost &s, const Product &p, bool gated) {
     return (int64_t)((p.rows + s.rows - 1) / s.rows) * ((p.outputs + made - 1) / made);
 }
 
-// The one that is expected to be done first: rounds of 256 workgroups, a tile's steps each; with parts, 3 us for the second launch and a us for every 3.5 MB of sums. Where one
-// tile has all rows and the weights are more than the caches keep, no sooner than 4.7 MB of weights a us, and 33 KB a us for a workgroup. Steps of rows that begin
-// within a line are in two: 270 x 11008 x 12800 / 12801 with 256 x 256 in two parts 83 / 105 us, 128 x 256 80 / 122, 128 x 128 100 / 138, 64 x 128 84 / 127;
-// where the caches keep the weights a quarter longer: 777 x 1111 x 5003 in rows of 5120 / 5008 bytes 20.0 / 24.6.
+// The one that is expected to be done first:
+//   - rounds of 256 workgroups, a tile's steps each;
+//   - with parts, 3 us for the second launch and a us for every 3.5 MB of sums;
+//   - where one tile has all rows and the weights are more than the caches keep, no sooner than 4.7 MB of weights a us, and 33 KB a us for a workgroup;
+//   - steps of rows that begin within a line are in two lines: `within` times as long, a quarter where the caches keep the weights.
+// Rows within lines: 270 x 11008 x 12800 / 12801 with 256 x 256 in two parts 83 / 105 us, 128 x 256 80 / 122, 128 x 128 100 / 138, 64 x 128 84 / 127;
+// weights in caches: 777 x 1111 x 5003 in rows of 5120 / 5008 bytes 20.0 / 24.6. One size stands for all here: 17 x 8839 x 26019 took 67 us before and takes 69 to 71 by this rule.
 // Rows x channels x K, us of 256 x 256 / 128 x 256 / 128 x 128 / 64 x 128 with the best number of parts each (the one taken is the least, or within 7 % of it):
 //   4001 x 4096 x 14336   188 / 210 / 268 / 343        1500 x 5120 x 5120   52.0 / 43.1 / 49.4 / 64.0      1024 x 4096 x 4096   38.2 / 28.5 / 24.2 / 31.1
 //   1024 x 8192 x 28672   207 (2 parts; one 283) / 211 / 276 / 386       250 x 4096 x 14336    36.8 (10) / 33.2 (7) / 32.3 (4; two 42.5) / 35.5 (2)
-//   512 x 4096 x 4096     29.4 (3) / 25.3 / 19.3 / 17.1                  40 x 8192 x 28672    - / - / - / 50.4 (4; three 52.0, two 63.6, one 103)
+//   512 x 4096 x 4096     29.4 (3) / 25.3 / 19.3 / 17.1                  40 x 8192 x 28672    - / - / - / 50.4 (4; three, which are taken, 52.0; two 63.6, one 103)
 inline Plan plan_tiles(const Product &p, bool gated, size_t room) {
     // places within a tile, with the gate's and the up projection's channels in one, are 32 bits
     const int64_t widest = (int64_t)1 << 23;

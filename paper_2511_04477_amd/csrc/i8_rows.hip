@@ -19,16 +19,17 @@ __device__ __forceinline__ int place(int v) {
     return ((int)(threadIdx.x % T) + v * T) * 8;
 }
 
-// Rows of whole 512s (WHOLE) end between two wavefronts' eights: whether a wavefront has its v-th ones is one question for all its lanes, and nothing needs to be moved or
-// masked. With that question asked lane by lane 4001 rows of 8192 took a norm 56 us in place of 53, 20000 of 512 22.4 in place of 19.1, and codes of 4001 rows of 14336 34.5 in place of 32.5.
+// Rows of whole 512s (WHOLE) end between two wavefronts' eights: whether a wavefront has its v-th ones is one question for all its lanes, and nothing
+// needs to be moved or masked. With that question asked lane by lane 4001 rows of 8192 took a norm 56 us in place of 53, 20000 of 512 22.4 in place
+// of 19.1, and codes of 4001 rows of 14336 34.5 in place of 32.5.
 template <int T, bool WHOLE>
 __device__ __forceinline__ bool has(int v, int K) {
     if (!WHOLE) return place<T>(v) < K;
     return (__builtin_amdgcn_readfirstlane((int)(threadIdx.x % T) / 64) * 64 + v * T) * 8 < K;
 }
 
-// Eight 16-bit numbers from element k on, as they lie. At a row's end the row's last eight, which settle() moves to their places, with 0 from element K on; rows of less than eight
-// are put together from single ones.
+// Eight 16-bit numbers from element k on, as they lie. At a row's end the row's last eight, which settle() moves to their places, with 0 from element
+// K on; rows of less than eight are put together from single ones.
 template <int T, bool WHOLE>
 __device__ __forceinline__ u32x4 fetch(const uint16_t *row, int v, int K) {
     const int k = place<T>(v);
@@ -75,8 +76,8 @@ __device__ __forceinline__ void put(uint16_t *row, int k, int K, const float (&x
         if (k + e < K) row[k + e] = (uint16_t)(w[e / 2] >> (16 * (e % 2)));
 }
 
-// A value of every thread of a row together, 0 leaving any other as it is: over the lanes of a wavefront first, then the wavefronts' through shared memory, `slot` being
-// another one than the last time.
+// A value of every thread of a row together, 0 leaving any other as it is: over the lanes of a wavefront first, then the wavefronts' through shared
+// memory, `slot` being another one than the last time.
 template <int T, class F>
 __device__ __forceinline__ uint32_t over_row(uint32_t v, F f, uint32_t *shared, int slot) {
     v = f(v, (uint32_t)__builtin_amdgcn_update_dpp(0, (int)v, 0x111, 0xf, 0xf, false));      // row_shr:1
@@ -104,9 +105,10 @@ __device__ __forceinline__ uint32_t most_over_row(uint32_t v, uint32_t *shared, 
     return over_row<T>(v, [](uint32_t a, uint32_t b) { return a > b ? a : b; }, shared, slot);
 }
 
-// 1 / sqrt(mean x^2 + eps), within 3.5 halves of fp32's steps behind the sum: 1 / K and its product, the sum with eps, these by the root's half, and two of the hardware's reciprocal root. Where the mean
-// is over 2^252 the result is a subnormal number, 4 more of them. Squares of numbers from 2^64 on, and sums of 2^16 of them from 2^56 on, leave fp32, as mean + eps may: such a row is summed in
-// units of 2^80, in which its largest number is from 2^-24 to 2^48, or eps is 2^-33 and more.
+// 1 / sqrt(mean x^2 + eps), within 3.5 halves of fp32's steps behind the sum: 1 / K and its product, the sum with eps, these by the root's half, and
+// two of the hardware's reciprocal root. Where the mean is over 2^252 the result is a subnormal number, 4 more of them. Squares of numbers from 2^64
+// on, and sums of 2^16 of them from 2^56 on, leave fp32, as mean + eps may: such a row is summed in units of 2^80, in which its largest number is
+// from 2^-24 to 2^48, or eps is 2^-33 and more.
 template <int T, int V>
 __device__ __forceinline__ float inverse_rms(const float (&x)[V][8], float per, float eps, uint32_t *shared, int slot) {
     float sum = 0.0f;
@@ -178,7 +180,9 @@ struct Quantize {
 };
 
 // A row is in the registers of its threads: read once, its largest magnitude found, its codes written.
-// What bounds it: 2 bytes in and 1 out a number: 4001 rows of 14336 32.5 us = 5.3 TB/s, of 8192 20.5 = 4.8 (a copy: 5.1); 40 of 28672 3.7 us; one of 4096 2.1.
+// What bounds it: 2 bytes in and 1 out a number. Call after call over tensors of 860 MB, which no cache keeps: 4001 rows of 14336 32.5 us = 5.3 TB/s, of
+// 8192 20.5 = 4.8 (a copy: 5.1); 300 of 65536 17.7 = 3.3; 40 of 28672 3.7 us; one of 4096 2.1. In turn with calls that read the codes back, which writes
+// 115 MB in between, 4001 rows of 14336 take 36 to 38.
 template <int T, int V, bool BF16, bool WHOLE>
 __global__ __launch_bounds__(Shape<T>::kThreads) void spqt_i8_quantize_kernel(Quantize a) {
     typedef Shape<T> S;
@@ -207,12 +211,14 @@ struct Norm {
     float residual, eps, offset, per;              // per: 1 / K
 };
 
-// One pass: what a block has made, the stream and the vectors are read once, and the sum stays in registers, in 32 bits, from the join over both norms to the codes.
-// TOGETHER: everything is asked for before any of it is used. That takes half as many registers again, with which a CU holds fewer wavefronts: of 512 and 1024 threads, two workgroups and one in
-// place of four and two. Together / not: one row of 8192 4.2 / 4.7 us, 40 rows 4.5 / 5.1, 256 rows 6.3 / 6.8, 512 rows 9.2 / 8.9, 4001 rows 53.0 / 48.1; 300 rows of 14336 13.1 / 10.8, 1000 rows
-// 33.7 / 26.6; of 256 threads, 4001 rows of 4096 26.5 / 27.4.
-// What bounds it: 4 bytes in and 3 out a number, and three sums over a row that follow each other: 4001 rows of 8192 with both norms and a gate 48 us = 4.8 TB/s; with sums over lanes by way of
-// shared memory 82. One row of 4096 3.7 us: loads, three sums, stores.
+// One pass: what a block has made, the stream and the vectors are read once, and the sum stays in registers, in 32 bits, from the join over both
+// norms to the codes. TOGETHER: everything is asked for before any of it is used. That takes half as many registers again, with which a CU holds
+// fewer wavefronts: of 512 and 1024 threads, two workgroups and one in place of four and two. Together / not: one row of 8192 4.2 / 4.7 us, 40 rows
+// 4.5 / 5.1, 256 rows 6.3 / 6.8, 512 rows 9.2 / 8.9, 4001 rows 53.0 / 48.1; 300 rows of 14336 13.1 / 10.8, 1000 rows 33.7 / 26.6; of 256 threads,
+// 4001 rows of 4096 26.5 / 27.4. What bounds it: 4 bytes in and 3 out a number, and three sums over a row that follow each other: 4001 rows of 8192
+// with both norms and a gate 48 us = 4.8 TB/s; with sums over lanes by way of shared memory 82. One row of 4096 3.7 us: loads, three sums, stores.
+// Rows of more than 32768 have more numbers than registers (17 to 163 of them in scratch memory): 300 rows of 65536 59 us = 2.3 TB/s, two 14.6 us;
+// 300 of 32768 27 us = 2.5 TB/s.
 template <int T, int V, bool BF16, bool WHOLE, bool TOGETHER>
 __global__ __launch_bounds__(Shape<T>::kThreads) void spqt_i8_norm_kernel(Norm a) {
     typedef Shape<T> S;
@@ -285,7 +291,8 @@ __global__ __launch_bounds__(Shape<T>::kThreads) void spqt_i8_norm_kernel(Norm a
     }
 }
 
-// What codes stand for: eight a thread. 1 byte in and 2 out: 4001 rows of 14336 33.9 us = 5.1 TB/s.
+// What codes stand for: eight a thread. 1 byte in and 2 out: 4001 rows of 14336 33.8 us = 5.1 TB/s from memory (860 MB in turn), 27 to 28 where the codes
+// were just written and are partly in the cache behind memory.
 struct Read {
     const int8_t *codes;
     const float *scales;
@@ -312,8 +319,9 @@ __global__ __launch_bounds__(256) void spqt_i8_read_kernel(Read a) {
     }
 }
 
-// f(threads, eights a thread, BF16, whole 512s) for rows of K numbers: a norm's threads hold two eights up to where a workgroup ends, since they have five tensors to ask for. With rows' ends asked for lane by lane, codes of 4001 rows of 14336
-// with 512 x 4 / 1024 x 2 / 256 x 8 34.4 / 40.3 / 35.9 us, of 8192 with 256 x 4 / 512 x 2 / 1024 x 1 20.5 / 21.2 / 24.2; norms of 4001 rows of 4096 with 256 x 2 / 512 x 1 27.8 / 34.5.
+// f(threads, eights a thread, BF16, whole 512s) for rows of K numbers: a norm's threads hold two eights up to where a workgroup ends, since they have
+// five tensors to ask for. With rows' ends asked for lane by lane, codes of 4001 rows of 14336 with 512 x 4 / 1024 x 2 / 256 x 8 34.4 / 40.3 / 35.9
+// us, of 8192 with 256 x 4 / 512 x 2 / 1024 x 1 20.5 / 21.2 / 24.2; norms of 4001 rows of 4096 with 256 x 2 / 512 x 1 27.8 / 34.5.
 template <bool NORM, class F>
 void dispatch(int64_t K, int type, F f) {
     auto typed = [&](auto t, auto v) {

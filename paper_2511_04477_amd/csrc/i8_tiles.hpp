@@ -1,15 +1,18 @@
 // The product in 8-bit integers, a tile of rows and channels a workgroup: codes and weights go through shared memory.
 //
-// With the weights as its first operand v_mfma_i32_32x32x32_i8 gives a lane four channels of one row in turn, which belong next to each other in y. Sums of products are whole numbers under
-// 2^31, so that neither the order of K nor its parts change a result. A workgroup goes from unit to unit (a tile, and a part of K) without a pause: loads of the next unit's first steps are on
-// their way while the last one's outputs are made. Loads go past the registers to shared memory, a line of memory a row and step, and are waited for by their number, with one barrier a step.
+// With the weights as its first operand v_mfma_i32_32x32x32_i8 gives a lane four channels of one row in turn, which belong next to each other in y.
+// Sums of products are whole numbers under 2^31, so that neither the order of K nor its parts change a result. A workgroup goes from unit to unit (a
+// tile, and a part of K) without a pause: loads of the next unit's first steps are on their way while the last one's outputs are made. Loads go past
+// the registers to shared memory, a line of memory a row and step, and are waited for by their number, with one barrier a step.
 //
-// What bounds it: 256 x 256 tiles the power of the card. 4001 x 4096 x 14336 190 to 195 us and 8192 x 8192 x 8192 445 us = 2.4 to 2.5 POPS (a library's product of the latter 440 to 462);
-// 4001 x 28672 x 4096 with the gate 396 to 411 us = 2.3 POPS, the clock down to 1.7 GHz, matrix units busy for 0.73 of the time, shared memory for 0.30, without conflicts but for the outputs.
-// The matrix instructions alone, with the same codes, come to 3.5 POPS, with the reads of shared memory to 2.85. Wavefronts of 128 x 128 in place of 128 x 64 read a third less from it: 206 us
-// for 190, the registers do not suffice for the outputs. 128 x 256 tiles are 0.9 as fast, 128 x 128 0.7 (with two workgroups a CU, of two and three steps' room, 0.78: 6396 x 8192 x 698 96 -> 74 us, where
-// 256 x 256 takes 67). Small sizes: some 7 us of a launch, a first step's way from memory and a last tile's outputs, and with parts the sums' way there and back: of the 33 us of
-// 250 x 4096 x 14336 24 are this kernel's (weights at 3.5 TB/s in the loop), 5.5 the join's. Few rows: the weights' way from memory, 40 x 8192 x 28672 47 us of this kernel = 5.0 TB/s.
+// What bounds it: 256 x 256 tiles the power of the card. 4001 x 4096 x 14336 190 to 195 us and 8192 x 8192 x 8192 415 to 445 us = 2.4 to 2.6 POPS, by
+// the card (a library's product of the latter 440 to 462); 4001 x 28672 x 4096 with the gate 384 to 414 us = 2.3 to 2.4 POPS, the clock down to 1.7 GHz, matrix units
+// busy for 0.73 of the time, shared memory for 0.30, without conflicts but for the outputs. The matrix instructions alone, with the same codes, come
+// to 3.5 POPS, with the reads of shared memory to 2.85. Wavefronts of 128 x 128 in place of 128 x 64 read a third less from it: 206 us for 190, the
+// registers do not suffice for the outputs. 128 x 256 tiles are 0.9 as fast, 128 x 128 0.7 (with two workgroups a CU, of two and three steps' room,
+// 0.78: 6396 x 8192 x 698 96 -> 74 us, where 256 x 256 takes 67). Small sizes: some 7 us of a launch, a first step's way from memory and a last
+// tile's outputs, and with parts the sums' way there and back: 250 x 4096 x 14336 takes 25 to 30 us with weights that are partly in the cache behind
+// memory, 23 of them this kernel's and 5.2 the join's, and 32 with weights from memory. Few rows: the weights' way from memory, 40 x 8192 x 28672 46 to 48 us of this kernel = 4.9 to 5.1 TB/s.
 #ifndef SPQT_I8_TILES_HPP
 #define SPQT_I8_TILES_HPP
 
@@ -40,7 +43,8 @@ struct Tiling {
     uint32_t *head;                      // of the workspace
 };
 
-// The unit of a workgroup in a round of kGroups, or -1. Workgroups go to the eight XCDs in turn: each of them gets neighbours, which share rows and channels in its cache.
+// The unit of a workgroup in a round of kGroups, or -1. Workgroups go to the eight XCDs in turn: each of them gets neighbours, which share rows and
+// channels in its cache.
 __device__ __forceinline__ int unit_of(const Tiling &t, int round) {
     const int first = round * kGroups, left = t.units - first, here = left < kGroups ? left : kGroups, each = (here + 7) >> 3;
     const int in = ((int)blockIdx.x & 7) * each + ((int)blockIdx.x >> 3);
@@ -67,13 +71,15 @@ __device__ __forceinline__ void load_to_shared(const int8_t *base, uint32_t offs
     asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, %2" : : "s"(to), "v"(offset), "s"(base) : "memory");
 }
 
-// The same number, as one that is not known from before: what depends on it is worked out where it is used, since there are no registers for it in the loop over K.
+// The same number, as one that is not known from before: what depends on it is worked out where it is used, since there are no registers for it in
+// the loop over K.
 __device__ __forceinline__ int anew(int v) {
     asm("" : "+v"(v));
     return v;
 }
 
-// TM rows by TN channels, WM by WN wavefronts of MI by NI matrix instructions' 32 by 32 each. Shared memory has room for NA steps of the rows and NB of the channels.
+// TM rows by TN channels, WM by WN wavefronts of MI by NI matrix instructions' 32 by 32 each. Shared memory has room for NA steps of the rows and NB
+// of the channels.
 template <int TM, int TN, int WM, int WN, int NA, int NB>
 struct Shape {
     static constexpr int kWaves = WM * WN, kThreads = kWaves * 64;
@@ -87,7 +93,8 @@ struct Shape {
     static_assert((!kAhead || NB == NA + 1) && NA >= 2 && NB >= 2 && kShared <= 160 * 1024 && kYounger < 64 && kWaves % 2 == 0 && 64 * kChannels <= kLoadsB * 1024);
 };
 
-// What becomes of the sums of 32 rows and a wavefront's channels, from channel n0 on: a lane has fours of channels of one row. They go through shared memory and leave 16 bytes a lane.
+// What becomes of the sums of 32 rows and a wavefront's channels, from channel n0 on: a lane has fours of channels of one row. They go through shared
+// memory and leave 16 bytes a lane.
 template <class S, int YT, bool GATED>
 struct Finish {
     static constexpr int kOut = GATED ? S::kChannels / 2 : S::kChannels, kBytes = YT == SPQT_I8_FP32 ? 4 : 2;
@@ -204,7 +211,8 @@ __global__ __launch_bounds__(WM * WN * 64, 1) void spqt_i8_tiles_kernel(Product 
     constexpr int kMade = GATED ? TN / 2 : TN;                    // outputs of a row
     const bool ragged = p.K % kStep != 0;
 
-    // Loading: eight rows an instruction, a row's 16s in an order that differs from row to row, so that 16 rows' 16s of one place of K lie in 16 different sets of banks.
+    // Loading: eight rows an instruction, a row's 16s in an order that differs from row to row, so that 16 rows' 16s of one place of K lie in 16
+    // different sets of banks.
     auto swizzle = [](int row) { return row >> 1 & 7; };
     const int row_in = lane >> 3, sixteen = (lane & 7) ^ swizzle(wave * 8 + row_in);
     // Where the loads of one operand are: a unit's step, its room in shared memory, and what the lanes' offsets are from.
@@ -353,7 +361,8 @@ __global__ __launch_bounds__(WM * WN * 64, 1) void spqt_i8_tiles_kernel(Product 
             advance_b(inner);
             advance_a(inner);
         } else {
-            // Step t: B(t - 1 + NB) is loaded beside its first three 32s of K, where step t - 1 has left room; then A(t + NA) beside the fourth, for which everyone has read step t.
+            // Step t: B(t - 1 + NB) is loaded beside its first three 32s of K, where step t - 1 has left room; then A(t + NA) beside the fourth, for
+            // which everyone has read step t.
             multiply(std::integral_constant<int, 0>(), step, tail);
             multiply(std::integral_constant<int, 1>(), step, tail);
             multiply(std::integral_constant<int, 2>(), step, tail);
@@ -407,7 +416,8 @@ __global__ __launch_bounds__(WM * WN * 64, 1) void spqt_i8_tiles_kernel(Product 
         for (int m = 0; m < S::MI; ++m)
 #pragma unroll
             for (int n = 0; n < S::NI; ++n) acc[m][n] = i32x16{};
-        // (a unit's first operands are read here, the others beside the products before them: what is read after a unit's outputs needs no registers while these are made)
+        // (a unit's first operands are read here, the others beside the products before them: what is read after a unit's outputs needs no registers
+        // while these are made)
         const std::integral_constant<int, 0> even;
         const std::integral_constant<int, 1> odd;
 #pragma unroll
@@ -431,7 +441,8 @@ __global__ __launch_bounds__(WM * WN * 64, 1) void spqt_i8_tiles_kernel(Product 
         }
         const int here = anew(lane);
         const Finish<S, YT, GATED> finish(p, u.channel_tile * kMade + wn * (S::kChannels / (GATED ? 2 : 1)), here & 31, here >> 5);
-        // Asked for before the last step, used after it. A load that no one waited for would make the compiler wait in the next unit's loop, for the loads that are on their way there.
+        // Asked for before the last step, used after it. A load that no one waited for would make the compiler wait in the next unit's loop, for the
+        // loads that are on their way there.
         typename Finish<S, YT, GATED>::Scales by;
         float scales[S::MI];
         if (t.parts == 1 && finish.inside) finish.scales(by);
@@ -470,7 +481,8 @@ __global__ __launch_bounds__(WM * WN * 64, 1) void spqt_i8_tiles_kernel(Product 
     asm volatile("s_waitcnt vmcnt(0)" ::: "memory");              // no load may arrive after the workgroup has left its shared memory
 }
 
-// The parts' sums together, and what becomes of them: a workgroup takes 32 rows of what a wavefront of the other kernel had, each of its four wavefronts every fourth part.
+// The parts' sums together, and what becomes of them: a workgroup takes 32 rows of what a wavefront of the other kernel had, each of its four
+// wavefronts every fourth part.
 template <int TM, int TN, int WM, int WN, int NA, int NB, int YT, bool GATED>
 __global__ __launch_bounds__(256) void spqt_i8_join_kernel(Product p, Tiling t) {
     typedef Shape<TM, TN, WM, WN, NA, NB> S;
